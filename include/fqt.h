@@ -314,6 +314,47 @@ FQT_API fqt_status fqt_grad_w_fixed_scratch(const fqt_qtensor *q_b1,
                                             const fqt_qtensor *qx, float *grad_W,
                                             void *stream);
 
+/* --- a training step around the quantized layers -------------------------
+ * The operators below have no counterpart in the paper: they are what a
+ * program runs between its quantized linear layers.  The conventions above
+ * hold, but their tensors need only the alignment of their entries, and rows
+ * may be any number of entries apart (`ld...`, at least the number of columns
+ * where there is more than one row).  Entries on 16 bytes are read faster, and
+ * the order of an fp32 sum goes by that and by the sizes, never by timing.
+ * Outputs may not overlap inputs.
+ */
+
+/*
+ * Layer norm of the rows of X (rows x cols, fp32 or bf16):
+ *   mean_i = sum_j x_ij / cols, var_i = sum_j (x_ij - mean_i)^2 / cols,
+ *   rstd_i = (var_i + eps)^(-1/2), y_ij = (x_ij - mean_i) rstd_i gamma_j + beta_j,
+ * statistics and sums in fp32, Y in X's type rounded once.  gamma, beta (cols
+ * entries, fp32): NULL = 1 and 0.  mean, rstd (rows entries): written when
+ * non-NULL.  A NaN or infinity makes its own row NaN.  eps >= 0.
+ */
+FQT_API fqt_status fqt_layer_norm_forward(const void *X, int64_t ldx, fqt_dtype dtype,
+                                          int64_t rows, int64_t cols, const float *gamma,
+                                          const float *beta, float eps, void *Y, int64_t ldy,
+                                          float *mean, float *rstd, void *stream);
+
+/*
+ * Its backward pass, with xh_ij = (x_ij - mean_i) rstd_i and g_ij = dy_ij gamma_j:
+ *   dx_ij = rstd_i (g_ij - sum_j g_ij / cols - xh_ij sum_j (g_ij xh_ij) / cols)
+ *   dgamma_j = sum_i dy_ij xh_ij,  dbeta_j = sum_i dy_ij
+ * dX in X's type, the sums over rows in fp32 in an order that does not change
+ * from call to call.  mean, rstd: the forward's.  dX, dgamma and dbeta are
+ * written when non-NULL (no rows: dgamma = dbeta = 0).  The workspace
+ * (fqt_layer_norm_workspace_size bytes) holds partial sums and is needed for
+ * dgamma or dbeta only.
+ */
+FQT_API size_t fqt_layer_norm_workspace_size(int64_t rows, int64_t cols);
+FQT_API fqt_status fqt_layer_norm_backward(const void *dY, int64_t lddy, const void *X,
+                                           int64_t ldx, fqt_dtype dtype, int64_t rows,
+                                           int64_t cols, const float *mean, const float *rstd,
+                                           const float *gamma, void *dX, int64_t lddx,
+                                           float *dgamma, float *dbeta, void *workspace,
+                                           size_t ws_bytes, void *stream);
+
 /* Synchronises `stream`, returns the first device-side condition recorded by
  * fqt_grad_w_fixed_scratch calls on the current device since the previous
  * call of this function (or FQT_OK) and clears it.  Allocates nothing; like

@@ -162,6 +162,14 @@ static int tail(PyObject *const *a, Tail *t) {
   return PyErr_Occurred() ? -1 : 0;
 }
 
+/* the same where the workspace may be None */
+static int tail_optional(PyObject *const *a, Tail *t) {
+  if (tensor_ptr(a[0], &t->ws)) return -1;
+  t->bytes = PyLong_AsSize_t(a[1]);
+  t->stream = PyLong_AsVoidPtr(a[2]);
+  return PyErr_Occurred() ? -1 : 0;
+}
+
 /* quantize_fwd(weight, X, dtype, rows, cols, bits, out, ws, bytes, stream) */
 static PyObject *py_quantize_fwd(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
@@ -273,6 +281,39 @@ static PyObject *py_linear_forward(PyObject *self, PyObject *const *a, Py_ssize_
   CALL(fqt_linear_forward(q[0], q[1], h, t.ws, t.bytes, t.stream))
 }
 
+/* layer_norm_forward(X, ldx, dtype, rows, cols, gamma, beta, eps, Y, ldy, mean, rstd, stream) */
+static PyObject *py_layer_norm_forward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(13)
+  void *x, *ga, *be, *y, *mean, *rstd;
+  const int64_t ldx = I64(1), rows = I64(3), cols = I64(4), ldy = I64(9);
+  const fqt_dtype dt = (fqt_dtype)INT(2);
+  const float eps = (float)PyFloat_AsDouble(a[7]);
+  void *stream = PyLong_AsVoidPtr(a[12]);
+  if (PyErr_Occurred() || tensor_ptr(a[0], &x) || tensor_ptr(a[5], &ga) || tensor_ptr(a[6], &be) ||
+      tensor_ptr(a[8], &y) || tensor_ptr(a[10], &mean) || tensor_ptr(a[11], &rstd))
+    return NULL;
+  CALL(fqt_layer_norm_forward(x, ldx, dt, rows, cols, ga, be, eps, y, ldy, mean, rstd, stream))
+}
+
+/* layer_norm_backward(dY, lddy, X, ldx, dtype, rows, cols, mean, rstd, gamma, dX, lddx, dgamma,
+ * dbeta, ws, bytes, stream) */
+static PyObject *py_layer_norm_backward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(17)
+  void *dy, *x, *mean, *rstd, *ga, *dx, *dg, *db;
+  Tail t;
+  const int64_t lddy = I64(1), ldx = I64(3), rows = I64(5), cols = I64(6), lddx = I64(11);
+  const fqt_dtype dt = (fqt_dtype)INT(4);
+  if (PyErr_Occurred() || tensor_ptr(a[0], &dy) || tensor_ptr(a[2], &x) ||
+      tensor_ptr(a[7], &mean) || tensor_ptr(a[8], &rstd) || tensor_ptr(a[9], &ga) ||
+      tensor_ptr(a[10], &dx) || tensor_ptr(a[12], &dg) || tensor_ptr(a[13], &db) ||
+      tail_optional(a + 14, &t))
+    return NULL;
+  CALL(fqt_layer_norm_backward(dy, lddy, x, ldx, dt, rows, cols, mean, rstd, ga, dx, lddx, dg, db,
+                               t.ws, t.bytes, t.stream))
+}
+
 /* workspace_size(N, C, D) */
 static PyObject *py_workspace_size(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
@@ -291,6 +332,10 @@ static PyMethodDef kMethods[] = {
     {"quantize_grad", (PyCFunction)(void (*)(void))py_quantize_grad, METH_FASTCALL, NULL},
     {"linear_backward", (PyCFunction)(void (*)(void))py_linear_backward, METH_FASTCALL, NULL},
     {"linear_forward", (PyCFunction)(void (*)(void))py_linear_forward, METH_FASTCALL, NULL},
+    {"layer_norm_forward", (PyCFunction)(void (*)(void))py_layer_norm_forward, METH_FASTCALL,
+     NULL},
+    {"layer_norm_backward", (PyCFunction)(void (*)(void))py_layer_norm_backward, METH_FASTCALL,
+     NULL},
     {"workspace_size", (PyCFunction)(void (*)(void))py_workspace_size, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 

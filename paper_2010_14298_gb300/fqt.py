@@ -9,6 +9,7 @@ calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.machinery
 import importlib.util
@@ -100,6 +101,14 @@ def load(build_if_missing: bool = True):
         lib.fqt_linear_forward.restype = i32
         lib.fqt_grad_w_fixed_scratch.argtypes = [QP, QP, P, P]
         lib.fqt_grad_w_fixed_scratch.restype = i32
+        f32 = ctypes.c_float
+        lib.fqt_layer_norm_workspace_size.argtypes = [i64, i64]
+        lib.fqt_layer_norm_workspace_size.restype = sz
+        lib.fqt_layer_norm_forward.argtypes = [P, i64, i32, i64, i64, P, P, f32, P, i64, P, P, P]
+        lib.fqt_layer_norm_forward.restype = i32
+        lib.fqt_layer_norm_backward.argtypes = [P, i64, P, i64, i32, i64, i64, P, P, P, P, i64,
+                                                P, P, P, sz, P]
+        lib.fqt_layer_norm_backward.restype = i32
         lib.fqt_sync_status.argtypes = [P, P]
         lib.fqt_sync_status.restype = i32
         lib.fqt_fixed_scratch_sync_status.argtypes = [P]
@@ -223,6 +232,14 @@ class Workspace:
             self.nbytes = need
             self.buf = torch.zeros(need, dtype=torch.uint8, device=self.buf.device)
         return self
+
+    @classmethod
+    def of_size(cls, nbytes: int, device="cuda"):
+        """A workspace of so many bytes (the ..._workspace_size of a call)."""
+        ws = cls.__new__(cls)
+        ws.nbytes = int(nbytes)
+        ws.buf = torch.zeros(ws.nbytes, dtype=torch.uint8, device=device)
+        return ws
 
     @property
     def ptr(self):
@@ -538,6 +555,122 @@ def grad_w_fixed_scratch(q_b1: QTensor, qx: QTensor, out: torch.Tensor = None,
                                       _stream(stream))
     _check(st, "fqt_grad_w_fixed_scratch")
     return out
+
+
+# --- a training step around the quantized layers ---------------------------
+def _on(stream):
+    """Copies and new tensors of a call belong to the stream that it runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _new(shape, dtype, like, stream):
+    with _on(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _row_stride(t, name):
+    """The row pitch of a matrix whose rows are contiguous, or None."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not on a GPU")
+    if t.dim() != 2:
+        raise ValueError(f"{name} has {t.dim()} dimensions, not two")
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+        return None
+    return ld if rows > 1 else cols
+
+
+def _rows_in(t, name, stream):
+    """A matrix to read, and its row pitch; one laid out otherwise is copied."""
+    ld = _row_stride(t, name)
+    if ld is None:
+        with _on(stream):
+            t = t.contiguous()
+        ld = t.shape[1]
+    return t, ld
+
+
+def _rows_out(t, name, shape, dtype, like, stream):
+    """A matrix to write (a new one for None), and its row pitch."""
+    if t is None:
+        return _new(shape, dtype, like, stream), shape[1]
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
+    ld = _row_stride(t, name)
+    if ld is None:
+        raise ValueError(f"the rows of {name} are not contiguous")
+    return t, ld
+
+
+def _vector(t, name, n, dtype=torch.float32):
+    """A contiguous vector of n entries on the GPU."""
+    if t.dtype != dtype or t.shape != (n,) or not t.is_cuda or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} is no contiguous {dtype} vector of {n} entries on the GPU")
+    return t
+
+
+def layer_norm_forward(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                       beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                       out: torch.Tensor = None, mean: torch.Tensor = None,
+                       rstd: torch.Tensor = None, stream=None):
+    """(Y, mean, rstd): layer norm of the rows of X (fqt_layer_norm_forward).
+    gamma and beta are fp32 (None: 1 and 0); Y has X's type."""
+    X, ldx = _rows_in(X, "X", stream)
+    rows, cols = X.shape
+    if gamma is not None:
+        _vector(gamma, "gamma", cols)
+    if beta is not None:
+        _vector(beta, "beta", cols)
+    Y, ldy = _rows_out(out, "out", X.shape, X.dtype, X, stream)
+    mean = (_vector(mean, "mean", rows) if mean is not None
+            else _new((rows,), torch.float32, X, stream))
+    rstd = (_vector(rstd, "rstd", rows) if rstd is not None
+            else _new((rows,), torch.float32, X, stream))
+    st = native().layer_norm_forward(X, ldx, _dtype_code(X), rows, cols, gamma, beta, eps, Y, ldy,
+                                     mean, rstd, _raw_stream(stream))
+    if st:
+        _check(st, "fqt_layer_norm_forward")
+    return Y, mean, rstd
+
+
+def layer_norm_workspace_size(rows: int, cols: int) -> int:
+    return int(load().fqt_layer_norm_workspace_size(rows, cols))
+
+
+def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
+                        rstd: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                        grad_x: bool = True, grad_w: bool = True, ws: Workspace = None,
+                        out_x: torch.Tensor = None, out_gamma: torch.Tensor = None,
+                        out_beta: torch.Tensor = None, stream=None):
+    """(dX, dgamma, dbeta) of layer_norm_forward (fqt_layer_norm_backward); grad_x
+    and grad_w choose them, None stands for one that was not asked for."""
+    if dY.shape != X.shape or dY.dtype != X.dtype:
+        raise ValueError(f"dY is {dY.dtype} {tuple(dY.shape)}, X {X.dtype} {tuple(X.shape)}")
+    X, ldx = _rows_in(X, "X", stream)
+    dY, lddy = _rows_in(dY, "dY", stream)
+    rows, cols = X.shape
+    _vector(mean, "mean", rows)
+    _vector(rstd, "rstd", rows)
+    if gamma is not None:
+        _vector(gamma, "gamma", cols)
+    dX, lddx, dgamma, dbeta, nbytes = None, cols, None, None, 0
+    if grad_x:
+        dX, lddx = _rows_out(out_x, "out_x", X.shape, X.dtype, X, stream)
+    if grad_w:
+        dgamma = (_vector(out_gamma, "out_gamma", cols) if out_gamma is not None
+                  else _new((cols,), torch.float32, X, stream))
+        dbeta = (_vector(out_beta, "out_beta", cols) if out_beta is not None
+                 else _new((cols,), torch.float32, X, stream))
+        if ws is None:
+            with _on(stream):
+                ws = Workspace.of_size(layer_norm_workspace_size(rows, cols), X.device)
+        nbytes = ws.nbytes
+    st = native().layer_norm_backward(dY, lddy, X, ldx, _dtype_code(X), rows, cols, mean, rstd,
+                                      gamma, dX, lddx, dgamma, dbeta,
+                                      ws.buf if grad_w else None, nbytes, _raw_stream(stream))
+    if st:
+        _check(st, "fqt_layer_norm_backward")
+    return dX, dgamma, dbeta
 
 
 def debug_int_gemm(A: torch.Tensor, a_kmajor: bool, a_bits: int, B: torch.Tensor,

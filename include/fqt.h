@@ -355,6 +355,53 @@ FQT_API fqt_status fqt_layer_norm_backward(const void *dY, int64_t lddy, const v
                                            float *dgamma, float *dbeta, void *workspace,
                                            size_t ws_bytes, void *stream);
 
+/*
+ * A matrix in 8-bit floating point (E4M3: 4 exponent bits, 3 of the significand,
+ * largest value 448, no infinities, NaN 0x7F / 0xFF) with one scale for each
+ * block of 128 consecutive entries of a row, or of 128 x 128 entries:
+ *     value_rc = E4M3(codes_rc) scales[c / 128][r].
+ * The caller allocates both arrays (device memory) and sets the pointers and the
+ * pitch; fqt_quantize_fp8 fills the rest.  Blocks at the ends hold what is left.
+ */
+typedef struct fqt_fp8 {
+  int64_t rows, cols;
+  int64_t pitch;       /* bytes between rows of codes: a multiple of 16, >= cols */
+  int32_t block_rows;  /* rows that share a scale: 1 or 128 */
+  int32_t reserved;
+  uint8_t *codes;      /* rows x pitch bytes, 16-byte aligned (bytes past cols are not read) */
+  float *scales;       /* ceil(cols / 128) times P entries, P = rows rounded up to a
+                          multiple of 128: scales[kb P + r] of block kb of row r (with
+                          block_rows 128 the same for the block's rows), 16-byte
+                          aligned; entries past rows need only be there */
+} fqt_fp8;
+
+/*
+ * X (rows x cols, fp32 or bf16) as such matrices: q = X, its blocks along the
+ * columns, and qt = X^T (cols x rows), its blocks along X's rows, from one read
+ * of X; either may be NULL.  block_rows 1 or 128.  A block's scale is the least
+ * power of two 2^e, -127 <= e <= 127, with max |x| <= 448 2^e (1 for a block of
+ * zeros), a code the E4M3 value nearest to x / 2^e, ties to even: both the same
+ * in any arithmetic.  Entries that are not finite record FQT_ENONFINITE, take the
+ * NaN code and count for no scale.  rows, cols <= 2^22.  The workspace holds the
+ * status word only (256 bytes).
+ */
+FQT_API fqt_status fqt_quantize_fp8(const void *X, int64_t ldx, fqt_dtype dtype, int64_t rows,
+                                    int64_t cols, int block_rows, fqt_fp8 *q, fqt_fp8 *qt,
+                                    void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * out = A B^T (M x N, fp32 or bf16) of A (M x K) and B (N x K):
+ *   out_mn = sum over K blocks of sa sb sum_(k in block) E4M3(a_mk) E4M3(b_nk),
+ * a block's products and their sum on the tensor cores in fp32, the sums over
+ * blocks in fp32, one rounding to bf16.  The scales may be any fp32 values.  A
+ * linear layer's passes, for X (tokens x D), W (C x D) and dH (tokens x C): the
+ * forward from X and W, grad_X from dH and W^T, grad_W from dH^T and X^T.
+ * M, N, K <= 2^22.  Workspace: fqt_fp8_matmul_workspace_size(M, N, K) bytes.
+ */
+FQT_API size_t fqt_fp8_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
+FQT_API fqt_status fqt_fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, fqt_dtype dtype, void *out,
+                                  int64_t ldo, void *workspace, size_t ws_bytes, void *stream);
+
 /* Synchronises `stream`, returns the first device-side condition recorded by
  * fqt_grad_w_fixed_scratch calls on the current device since the previous
  * call of this function (or FQT_OK) and clears it.  Allocates nothing; like

@@ -17,12 +17,13 @@ enum {
   A_CODES, A_CODES16, A_INV_S, A_ZERO, A_ROW_SUM, A_COL_SUM, A_LEAD, A_HZ, A_HR, A_PERM,
   A_GSTART, A_GSIZE, A_SHIFT16, A_SHIFT, A_SHIFT_COL_SUM, A_SHIFT_SCALE, A_POINTERS,
   A_BITS = A_POINTERS, A_KIND, A_BLOCK, A_ROWS_PER_SAMPLE, A_CONV, A_LOGICAL, A_SHAPE,
-  A_DATA_PTR, A_COUNT
+  A_DATA_PTR, A_SCALES, A_ROWS, A_COLS, A_PITCH, A_BLOCK_ROWS, A_COUNT
 };
 static const char *const kNames[A_COUNT] = {
     "codes", "codes16", "inv_s", "zero", "row_sum", "col_sum", "lead", "hz", "hr", "perm",
     "gstart", "gsize", "shift16", "shift", "shift_col_sum", "shift_scale", "bits", "kind",
-    "block", "rows_per_sample", "conv", "logical", "shape", "data_ptr"};
+    "block", "rows_per_sample", "conv", "logical", "shape", "data_ptr",
+    "scales", "rows", "cols", "pitch", "block_rows"};
 static PyObject *g_name[A_COUNT];
 
 /* data_ptr() of a tensor; -1 with an exception set on failure (AttributeError
@@ -131,6 +132,38 @@ static int fill(PyObject *q, fqt_qtensor *s, fqt_qtensor **out) {
 static int fill_optional(PyObject *q, fqt_qtensor *s, fqt_qtensor **out) {
   *out = NULL;
   return q == Py_None ? 0 : fill(q, s, out);
+}
+
+static int i64_attr(PyObject *o, int name, int64_t *out) {
+  PyObject *v = PyObject_GetAttr(o, g_name[name]);
+  if (!v) return -1;
+  *out = PyLong_AsLongLong(v);
+  Py_DECREF(v);
+  return PyErr_Occurred() ? -1 : 0;
+}
+
+static int ptr_attr(PyObject *o, int name, void **out) {
+  PyObject *v = PyObject_GetAttr(o, g_name[name]);
+  if (!v) return -1;
+  const int bad = needed_ptr(v, out);
+  Py_DECREF(v);
+  return bad;
+}
+
+/* An Fp8Tensor object as the C struct; NULL for None. */
+static int fill_fp8(PyObject *q, fqt_fp8 *s, fqt_fp8 **out) {
+  memset(s, 0, sizeof(*s));
+  *out = NULL;
+  if (q == Py_None) return 0;
+  void *codes, *scales;
+  if (ptr_attr(q, A_CODES, &codes) || ptr_attr(q, A_SCALES, &scales) ||
+      i64_attr(q, A_ROWS, &s->rows) || i64_attr(q, A_COLS, &s->cols) ||
+      i64_attr(q, A_PITCH, &s->pitch) || int_attr(q, A_BLOCK_ROWS, &s->block_rows))
+    return -1;
+  s->codes = codes;
+  s->scales = scales;
+  *out = s;
+  return 0;
 }
 
 #define NARGS(k)                                                     \
@@ -314,6 +347,37 @@ static PyObject *py_layer_norm_backward(PyObject *self, PyObject *const *a, Py_s
                                t.ws, t.bytes, t.stream))
 }
 
+/* quantize_fp8(X, ldx, dtype, rows, cols, block_rows, q, qt, ws, bytes, stream) */
+static PyObject *py_quantize_fp8(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(11)
+  void *x;
+  fqt_fp8 s[2], *q, *qt;
+  Tail t;
+  const int64_t ldx = I64(1), rows = I64(3), cols = I64(4);
+  const fqt_dtype dt = (fqt_dtype)INT(2);
+  const int block_rows = INT(5);
+  if (PyErr_Occurred() || tensor_ptr(a[0], &x) || fill_fp8(a[6], &s[0], &q) ||
+      fill_fp8(a[7], &s[1], &qt) || tail(a + 8, &t))
+    return NULL;
+  CALL(fqt_quantize_fp8(x, ldx, dt, rows, cols, block_rows, q, qt, t.ws, t.bytes, t.stream))
+}
+
+/* fp8_matmul(A, B, dtype, out, ldo, ws, bytes, stream) */
+static PyObject *py_fp8_matmul(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(8)
+  void *out;
+  fqt_fp8 s[2], *A, *B;
+  Tail t;
+  const fqt_dtype dt = (fqt_dtype)INT(2);
+  const int64_t ldo = I64(4);
+  if (PyErr_Occurred() || fill_fp8(a[0], &s[0], &A) || fill_fp8(a[1], &s[1], &B) ||
+      tensor_ptr(a[3], &out) || tail(a + 5, &t))
+    return NULL;
+  CALL(fqt_fp8_matmul(A, B, dt, out, ldo, t.ws, t.bytes, t.stream))
+}
+
 /* workspace_size(N, C, D) */
 static PyObject *py_workspace_size(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
@@ -336,6 +400,8 @@ static PyMethodDef kMethods[] = {
      NULL},
     {"layer_norm_backward", (PyCFunction)(void (*)(void))py_layer_norm_backward, METH_FASTCALL,
      NULL},
+    {"quantize_fp8", (PyCFunction)(void (*)(void))py_quantize_fp8, METH_FASTCALL, NULL},
+    {"fp8_matmul", (PyCFunction)(void (*)(void))py_fp8_matmul, METH_FASTCALL, NULL},
     {"workspace_size", (PyCFunction)(void (*)(void))py_workspace_size, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 

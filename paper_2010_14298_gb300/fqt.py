@@ -54,6 +54,12 @@ class _QT(ctypes.Structure):
                 ("conv", ctypes.c_int32 * 8)]
 
 
+class _F8(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("pitch", ctypes.c_int64),
+                ("block_rows", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
 def library_path() -> str:
     return _build.LIB
 
@@ -109,6 +115,13 @@ def load(build_if_missing: bool = True):
         lib.fqt_layer_norm_backward.argtypes = [P, i64, P, i64, i32, i64, i64, P, P, P, P, i64,
                                                 P, P, P, sz, P]
         lib.fqt_layer_norm_backward.restype = i32
+        FP = ctypes.POINTER(_F8)
+        lib.fqt_quantize_fp8.argtypes = [P, i64, i32, i64, i64, i32, FP, FP, P, sz, P]
+        lib.fqt_quantize_fp8.restype = i32
+        lib.fqt_fp8_matmul_workspace_size.argtypes = [i64, i64, i64]
+        lib.fqt_fp8_matmul_workspace_size.restype = sz
+        lib.fqt_fp8_matmul.argtypes = [FP, FP, i32, P, i64, P, sz, P]
+        lib.fqt_fp8_matmul.restype = i32
         lib.fqt_sync_status.argtypes = [P, P]
         lib.fqt_sync_status.restype = i32
         lib.fqt_fixed_scratch_sync_status.argtypes = [P]
@@ -150,7 +163,7 @@ class _CtypesCalls:
 def _c_arg(a):
     if isinstance(a, torch.Tensor):
         return ctypes.c_void_p(a.data_ptr())
-    return ctypes.byref(a.c_struct()) if isinstance(a, QTensor) else a
+    return ctypes.byref(a.c_struct()) if isinstance(a, (QTensor, Fp8Tensor)) else a
 
 
 def native():
@@ -671,6 +684,133 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
     if st:
         _check(st, "fqt_layer_norm_backward")
     return dX, dgamma, dbeta
+
+
+FP8_BLOCK = 128
+
+
+@dataclass
+class Fp8Tensor:
+    """A matrix in 8-bit floating point with a scale for each block of 128 (the
+    fqt_fp8 of include/fqt.h).
+
+    ``codes`` holds the E4M3 codes, rows of ``pitch`` bytes of which the first
+    ``cols`` count; ``scales`` one row per block of columns, of which the first
+    ``rows`` entries count.  ``block_rows``: rows that share a scale, 1 or 128.
+    """
+    codes: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+    block_rows: int = 1
+
+    def __post_init__(self):
+        c, s = self.codes, self.scales
+        if c.dtype != torch.uint8 or s.dtype != torch.float32:
+            raise ValueError(f"codes are uint8 and scales float32, not {c.dtype} and {s.dtype}")
+        if c.dim() != 2 or c.shape[0] != self.rows or c.shape[1] < self.cols or c.shape[1] % 16:
+            raise ValueError(f"{self.rows} x {self.cols} codes do not lie in {tuple(c.shape)} bytes")
+        if s.shape != self.scale_shape(self.rows, self.cols):
+            raise ValueError(f"scales are {self.scale_shape(self.rows, self.cols)}, "
+                             f"not {tuple(s.shape)}")
+        if not (c.is_contiguous() and s.is_contiguous()):
+            raise ValueError("codes and scales are contiguous")
+        if c.device != s.device:
+            raise ValueError("codes and scales are on one device")
+        if self.block_rows not in (1, FP8_BLOCK):
+            raise ValueError(f"block_rows is 1 or {FP8_BLOCK}, not {self.block_rows}")
+
+    @staticmethod
+    def scale_shape(rows: int, cols: int):
+        return -(-cols // FP8_BLOCK), -(-rows // FP8_BLOCK) * FP8_BLOCK
+
+    @staticmethod
+    def empty(rows: int, cols: int, block_rows: int = 1, device="cuda"):
+        return Fp8Tensor(
+            torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device),
+            torch.empty(Fp8Tensor.scale_shape(rows, cols), dtype=torch.float32, device=device),
+            rows, cols, block_rows)
+
+    @property
+    def shape(self):
+        return self.rows, self.cols
+
+    @property
+    def pitch(self):
+        return self.codes.shape[1]
+
+    def c_struct(self) -> _F8:
+        return _F8(self.rows, self.cols, self.pitch, self.block_rows, 0, self.codes.data_ptr(),
+                   self.scales.data_ptr())
+
+    def dequantize(self) -> torch.Tensor:
+        """The values (fp32): code times scale."""
+        v = self.codes[:, :self.cols].contiguous().view(torch.float8_e4m3fn).float()
+        s = self.scales[:, :self.rows].t().repeat_interleave(FP8_BLOCK, 1)
+        return v * s[:, :self.cols]
+
+
+def _fp8_out(t, name, rows, cols, block_rows, like, stream):
+    if t is None:
+        with _on(stream):
+            return Fp8Tensor.empty(rows, cols, block_rows, like.device)
+    if t.rows != rows or t.cols != cols:
+        raise ValueError(f"{name} is {t.rows} x {t.cols}, not {rows} x {cols}")
+    if not t.codes.is_cuda:
+        raise ValueError(f"{name} is not on a GPU")
+    return t
+
+
+def quantize_fp8(X: torch.Tensor, block_rows: int = 1, q: Fp8Tensor = None, qt: Fp8Tensor = None,
+                 rows: bool = True, cols: bool = False, ws: Workspace = None, stream=None):
+    """(X, X^T) in 8-bit floating point (fqt_quantize_fp8): the blocks of the first
+    run along X's rows, those of the second along its columns.  `rows` and `cols` ask
+    for them (a tensor given for one does too), None stands for one that was not."""
+    X, ldx = _rows_in(X, "X", stream)
+    n, k = X.shape
+    if rows or q is not None:
+        q = _fp8_out(q, "q", n, k, block_rows, X, stream)
+    if cols or qt is not None:
+        qt = _fp8_out(qt, "qt", k, n, block_rows, X, stream)
+    if ws is None:
+        with _on(stream):
+            ws = Workspace.of_size(256, X.device)
+    st = native().quantize_fp8(X, ldx, _dtype_code(X), n, k, block_rows, q, qt, ws.buf, ws.nbytes,
+                               _raw_stream(stream))
+    if st:
+        _check(st, "fqt_quantize_fp8")
+    for t in (q, qt):
+        if t is not None:
+            t.block_rows = block_rows
+    return q, qt
+
+
+def fp8_matmul_workspace_size(M: int, N: int, K: int) -> int:
+    return int(load().fqt_fp8_matmul_workspace_size(M, N, K))
+
+
+def fp8_matmul(A: Fp8Tensor, B: Fp8Tensor, out: torch.Tensor = None, dtype=torch.float32,
+               ws: Workspace = None, stream=None) -> torch.Tensor:
+    """A B^T (fqt_fp8_matmul) in out's type, or a new tensor of `dtype`."""
+    if A.cols != B.cols:
+        raise ValueError(f"A has {A.cols} columns, B {B.cols}")
+    if not (A.codes.is_cuda and B.codes.is_cuda):
+        raise ValueError("A and B are not on a GPU")
+    shape = (A.rows, B.rows)
+    if out is not None:
+        dtype = out.dtype
+        if out.shape != shape:
+            raise ValueError(f"out is {tuple(out.shape)}, not {shape}")
+    out, ldo = _rows_out(out, "out", torch.Size(shape), dtype, A.codes, stream)
+    if ws is None:
+        with _on(stream):
+            ws = Workspace.of_size(fp8_matmul_workspace_size(A.rows, B.rows, A.cols),
+                                   A.codes.device)
+    st = native().fp8_matmul(A, B, _dtype_code(out), out, ldo, ws.buf, ws.nbytes,
+                             _raw_stream(stream))
+    if st:
+        _check(st, "fqt_fp8_matmul")
+    return out
 
 
 def debug_int_gemm(A: torch.Tensor, a_kmajor: bool, a_bits: int, B: torch.Tensor,

@@ -49,3 +49,60 @@ def test_layer_norm_refusals():
     assert bwd(ws=None) == EWORKSPACE and bwd(nbytes=256) == EWORKSPACE
     assert bwd(ws=_at(p, 16)) == EWORKSPACE
     del raw
+
+
+def test_fp8_refusals():
+    lib = fqt.load()
+    raw, p = _aligned()
+
+    def f8(rows, cols, pitch=None, block_rows=1, codes=p.value, scales=p.value):
+        return fqt._F8(rows, cols, -(-cols // 16) * 16 if pitch is None else pitch, block_rows, 0,
+                       codes, scales)
+
+    def quant(q, qt=None, X=p, ldx=64, dtype=0, rows=4, cols=64, br=1, ws=p, nbytes=256):
+        return lib.fqt_quantize_fp8(X, ldx, dtype, rows, cols, br,
+                                    ctypes.byref(q) if q else None,
+                                    ctypes.byref(qt) if qt else None, ws, nbytes, None)
+
+    good = f8(0, 0, 64)
+    assert quant(None) == EINVAL
+    assert quant(good, X=None) == EINVAL and quant(good, X=_at(p, 2)) == EINVAL
+    assert quant(good, br=64) == EINVAL and quant(good, dtype=3) == EINVAL
+    assert quant(good, rows=-1) == EINVAL and quant(good, cols=0) == EINVAL
+    assert quant(good, rows=(1 << 22) + 1) == EINVAL and quant(good, ldx=60) == EINVAL
+    assert quant(f8(0, 0, 48)) == EINVAL              # rows of 64 codes in 48 bytes
+    assert quant(f8(0, 0, 72)) == EINVAL              # no multiple of 16
+    assert quant(f8(0, 0, 64, codes=p.value + 8)) == EINVAL
+    assert quant(f8(0, 0, 64, scales=None)) == EINVAL
+    assert quant(good, qt=f8(0, 0, 0)) == EINVAL      # 4 codes in no bytes
+    assert quant(good, ws=None) == EWORKSPACE and quant(good, nbytes=128) == EWORKSPACE
+    assert quant(good, ws=_at(p, 8)) == EWORKSPACE
+    assert quant(good, rows=0, X=None) == 0 and (good.rows, good.cols) == (0, 64)
+
+    def mm(A, B, dtype=0, out=p, ldo=None, ws=p, nbytes=1 << 30):
+        return lib.fqt_fp8_matmul(ctypes.byref(A) if A else None, ctypes.byref(B) if B else None,
+                                  dtype, out, B.rows if ldo is None and B else ldo or 0, ws,
+                                  nbytes, None)
+
+    A, B = f8(10, 64), f8(20, 64)
+    assert mm(None, B) == EINVAL and mm(A, None) == EINVAL and mm(A, B, dtype=2) == EINVAL
+    assert mm(A, f8(20, 65)) == EINVAL and mm(A, f8(-1, 64)) == EINVAL
+    assert mm(A, f8(20, 64, block_rows=2)) == EINVAL
+    assert mm(A, f8(20, 64, pitch=48)) == EINVAL and mm(A, f8(20, 64, codes=None)) == EINVAL
+    assert mm(A, B, out=None) == EINVAL and mm(A, B, out=_at(p, 2)) == EINVAL
+    assert mm(A, B, ldo=19) == EINVAL
+    assert mm(f8((1 << 22) + 1, 64), B) == EINVAL
+    assert mm(A, B, ws=None) == EWORKSPACE and mm(A, B, nbytes=16) == EWORKSPACE
+    assert mm(f8(0, 64), B) == 0 and mm(A, f8(0, 64)) == 0
+    del raw
+
+
+def test_fp8_tensors_that_do_not_fit_are_refused():
+    codes, scales = torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((1, 128))
+    fqt.Fp8Tensor(codes, scales, 4, 64)
+    for bad in (dict(codes=codes.int()), dict(scales=scales.double()), dict(rows=5),
+                dict(cols=65), dict(codes=torch.zeros((4, 60), dtype=torch.uint8)),
+                dict(scales=torch.zeros((1, 64))), dict(scales=torch.zeros((2, 128))),
+                dict(codes=torch.zeros((64, 4), dtype=torch.uint8).t()), dict(block_rows=2)):
+        with pytest.raises(ValueError):
+            fqt.Fp8Tensor(**{**dict(codes=codes, scales=scales, rows=4, cols=64), **bad})

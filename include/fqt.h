@@ -402,6 +402,31 @@ FQT_API size_t fqt_fp8_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
 FQT_API fqt_status fqt_fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, fqt_dtype dtype, void *out,
                                   int64_t ldo, void *workspace, size_t ws_bytes, void *stream);
 
+/* A dense tensor: `count` entries (fp32 or bf16) at `data`, in one run. */
+typedef struct fqt_tensor {
+  void *data;
+  int64_t count;
+  int32_t dtype;     /* fqt_dtype */
+  int32_t reserved;
+} fqt_tensor;
+
+/*
+ * The global norm of n tensors and the tensors scaled to a largest norm:
+ *   norm = sqrt(sum of g^2 over all entries of all tensors)
+ *   out = g max_norm / norm where norm > max_norm, else g
+ * grads and out are host arrays of n, read during the call; out[i] has
+ * grads[i]'s count and type and may be grads[i] itself, else they may not
+ * overlap.  out NULL: the norm alone.  norm (one fp32 entry, device memory):
+ * written when non-NULL.  Sums keep more than 32 bits and every entry's square
+ * (fp32's whole range), in an order that goes by the sizes alone.  A norm that is
+ * not finite records FQT_ENONFINITE and leaves the entries as they are.
+ * n <= 2^24.  Workspace: fqt_clip_grad_norm_workspace_size(n) bytes.
+ */
+FQT_API size_t fqt_clip_grad_norm_workspace_size(int64_t n);
+FQT_API fqt_status fqt_clip_grad_norm(const fqt_tensor *grads, const fqt_tensor *out, int64_t n,
+                                      float max_norm, float *norm, void *workspace,
+                                      size_t ws_bytes, void *stream);
+
 /* Synchronises `stream`, returns the first device-side condition recorded by
  * fqt_grad_w_fixed_scratch calls on the current device since the previous
  * call of this function (or FQT_OK) and clears it.  Allocates nothing; like

@@ -378,6 +378,20 @@ static PyObject *py_fp8_matmul(PyObject *self, PyObject *const *a, Py_ssize_t n)
   CALL(fqt_fp8_matmul(A, B, dt, out, ldo, t.ws, t.bytes, t.stream))
 }
 
+/* clip_grad_norm(grads, out, n, max_norm, norm, ws, bytes, stream), the lists by address */
+static PyObject *py_clip_grad_norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(8)
+  void *norm;
+  Tail t;
+  const fqt_tensor *grads = PyLong_AsVoidPtr(a[0]);
+  const fqt_tensor *out = a[1] == Py_None ? NULL : PyLong_AsVoidPtr(a[1]);
+  const int64_t count = I64(2);
+  const float max_norm = (float)PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred() || tensor_ptr(a[4], &norm) || tail(a + 5, &t)) return NULL;
+  CALL(fqt_clip_grad_norm(grads, out, count, max_norm, norm, t.ws, t.bytes, t.stream))
+}
+
 /* workspace_size(N, C, D) */
 static PyObject *py_workspace_size(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
@@ -402,6 +416,7 @@ static PyMethodDef kMethods[] = {
      NULL},
     {"quantize_fp8", (PyCFunction)(void (*)(void))py_quantize_fp8, METH_FASTCALL, NULL},
     {"fp8_matmul", (PyCFunction)(void (*)(void))py_fp8_matmul, METH_FASTCALL, NULL},
+    {"clip_grad_norm", (PyCFunction)(void (*)(void))py_clip_grad_norm, METH_FASTCALL, NULL},
     {"workspace_size", (PyCFunction)(void (*)(void))py_workspace_size, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 

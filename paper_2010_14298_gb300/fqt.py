@@ -60,6 +60,11 @@ class _F8(ctypes.Structure):
                 ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 def library_path() -> str:
     return _build.LIB
 
@@ -122,6 +127,10 @@ def load(build_if_missing: bool = True):
         lib.fqt_fp8_matmul_workspace_size.restype = sz
         lib.fqt_fp8_matmul.argtypes = [FP, FP, i32, P, i64, P, sz, P]
         lib.fqt_fp8_matmul.restype = i32
+        lib.fqt_clip_grad_norm_workspace_size.argtypes = [i64]
+        lib.fqt_clip_grad_norm_workspace_size.restype = sz
+        lib.fqt_clip_grad_norm.argtypes = [P, P, i64, f32, P, P, sz, P]
+        lib.fqt_clip_grad_norm.restype = i32
         lib.fqt_sync_status.argtypes = [P, P]
         lib.fqt_sync_status.restype = i32
         lib.fqt_fixed_scratch_sync_status.argtypes = [P]
@@ -811,6 +820,76 @@ def fp8_matmul(A: Fp8Tensor, B: Fp8Tensor, out: torch.Tensor = None, dtype=torch
     if st:
         _check(st, "fqt_fp8_matmul")
     return out
+
+
+class TensorList:
+    """Tensors that a call takes together, such as a model's gradients: dense fp32 or
+    bf16 tensors on one GPU.  The list keeps them, and their addresses as they are
+    now; a program that keeps its gradients makes it once."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self._array = (_Tensor * max(1, len(self.tensors)))()
+        for i, t in enumerate(self.tensors):
+            if not t.is_cuda or t.device != self.tensors[0].device:
+                raise ValueError(f"tensor {i} is not on the list's GPU")
+            if not t.is_contiguous():
+                raise ValueError(f"tensor {i} is not contiguous")
+            self._array[i] = _Tensor(t.data_ptr(), t.numel(), _dtype_code(t), 0)
+        self._kinds = [(t.numel(), t.dtype) for t in self.tensors]
+        self.address = ctypes.addressof(self._array)
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def __iter__(self):
+        return iter(self.tensors)
+
+    def __getitem__(self, i):
+        return self.tensors[i]
+
+
+def clip_grad_norm_workspace_size(grads) -> int:
+    return int(load().fqt_clip_grad_norm_workspace_size(len(grads)))
+
+
+def _clip(grads, out, max_norm, norm, ws, stream):
+    if not isinstance(grads, TensorList):
+        grads = TensorList(grads)
+    if not len(grads):
+        raise ValueError("the list of gradients is empty")
+    if out is not None:
+        if not isinstance(out, TensorList):
+            out = TensorList(out)
+        if out is not grads and (out._kinds != grads._kinds
+                                 or out[0].device != grads[0].device):
+            raise ValueError("out has other sizes, types or another GPU than the gradients")
+    norm = _vector(norm, "norm", 1) if norm is not None else _new((1,), torch.float32, grads[0],
+                                                                  stream)
+    if ws is None:
+        with _on(stream):
+            ws = Workspace.of_size(clip_grad_norm_workspace_size(grads), grads[0].device)
+    st = native().clip_grad_norm(grads.address, out.address if out is not None else None,
+                                 len(grads), max_norm, norm, ws.buf, ws.nbytes,
+                                 _raw_stream(stream))
+    if st:
+        _check(st, "fqt_clip_grad_norm")
+    return norm
+
+
+def grad_norm(grads, norm: torch.Tensor = None, ws: Workspace = None, stream=None):
+    """The norm (one fp32 entry on the GPU) of all entries of a list of tensors."""
+    return _clip(grads, None, 0.0, norm, ws, stream)
+
+
+def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor = None,
+                   ws: Workspace = None, stream=None):
+    """Scales a list of gradients (a TensorList, or tensors) to a global norm of at most
+    max_norm, in place or into the tensors of `out`; returns the norm that they had
+    (fqt_clip_grad_norm)."""
+    if not isinstance(grads, TensorList):
+        grads = TensorList(grads)
+    return _clip(grads, grads if out is None else out, max_norm, norm, ws, stream)
 
 
 def debug_int_gemm(A: torch.Tensor, a_kmajor: bool, a_bits: int, B: torch.Tensor,

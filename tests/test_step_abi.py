@@ -106,3 +106,35 @@ def test_fp8_tensors_that_do_not_fit_are_refused():
                 dict(codes=torch.zeros((64, 4), dtype=torch.uint8).t()), dict(block_rows=2)):
         with pytest.raises(ValueError):
             fqt.Fp8Tensor(**{**dict(codes=codes, scales=scales, rows=4, cols=64), **bad})
+
+
+def test_clip_refusals():
+    lib = fqt.load()
+    raw, p = _aligned()
+
+    def lst(*entries):
+        a = (fqt._Tensor * max(1, len(entries)))()
+        for i, e in enumerate(entries):
+            a[i] = fqt._Tensor(*e)
+        return a
+
+    def call(grads, out=None, n=1, max_norm=1.0, norm=p, ws=p, nbytes=1 << 30):
+        return lib.fqt_clip_grad_norm(grads, out, n, max_norm, norm, ws, nbytes, None)
+
+    good = lst((p.value, 8, 0, 0))
+    assert call(None) == EINVAL and call(good, n=-1) == EINVAL
+    assert call(good, norm=None) == EINVAL           # nothing asked for
+    assert call(good, norm=_at(p, 2)) == EINVAL
+    assert call(lst((p.value, 8, 2, 0))) == EINVAL
+    assert call(lst((p.value, -1, 0, 0))) == EINVAL
+    assert call(lst((p.value, 1 << 41, 0, 0))) == EINVAL
+    assert call(lst((None, 8, 0, 0))) == EINVAL
+    assert call(lst((p.value + 2, 8, 0, 0))) == EINVAL
+    assert call(lst((p.value + 1, 8, 1, 0))) == EINVAL
+    assert call(good, out=lst((p.value, 7, 0, 0))) == EINVAL
+    assert call(good, out=lst((p.value, 8, 1, 0))) == EINVAL
+    assert call(good, out=good, max_norm=-1.0) == EINVAL
+    assert call(good, out=good, max_norm=float("nan")) == EINVAL
+    assert call(good, ws=None) == EWORKSPACE and call(good, nbytes=256) == EWORKSPACE
+    assert call(good, ws=_at(p, 8)) == EWORKSPACE
+    del raw

@@ -358,8 +358,9 @@ FQT_API fqt_status fqt_layer_norm_backward(const void *dY, int64_t lddy, const v
 /*
  * A matrix in 8-bit floating point (E4M3: 4 exponent bits, 3 of the significand,
  * largest value 448, no infinities, NaN 0x7F / 0xFF) with one scale for each
- * block of 128 consecutive entries of a row, or of 128 x 128 entries:
- *     value_rc = E4M3(codes_rc) scales[c / 128][r].
+ * block of 128 consecutive entries of a row, or of 128 x 128 entries, a power of
+ * two (E8M0):
+ *     value_rc = E4M3(codes_rc) 2^(scale byte of block c / 128 of row r - 127).
  * The caller allocates both arrays (device memory) and sets the pointers and the
  * pitch; fqt_quantize_fp8 fills the rest.  Blocks at the ends hold what is left.
  */
@@ -369,10 +370,11 @@ typedef struct fqt_fp8 {
   int32_t block_rows;  /* rows that share a scale: 1 or 128 */
   int32_t reserved;
   uint8_t *codes;      /* rows x pitch bytes, 16-byte aligned (bytes past cols are not read) */
-  float *scales;       /* ceil(cols / 128) times P entries, P = rows rounded up to a
-                          multiple of 128: scales[kb P + r] of block kb of row r (with
-                          block_rows 128 the same for the block's rows), 16-byte
-                          aligned; entries past rows need only be there */
+  uint8_t *scales;     /* 4 ceil(cols / 512) P bytes, P = rows rounded up to a multiple
+                          of 128: the byte of block kb of row r at
+                          ((kb / 4) P + r) 4 + kb % 4 (with block_rows 128 the same for
+                          the block's rows), 16-byte aligned; bytes past rows or past
+                          the last block need only be there; 255 is no scale */
 } fqt_fp8;
 
 /*
@@ -392,8 +394,9 @@ FQT_API fqt_status fqt_quantize_fp8(const void *X, int64_t ldx, fqt_dtype dtype,
 /*
  * out = A B^T (M x N, fp32 or bf16) of A (M x K) and B (N x K):
  *   out_mn = sum over K blocks of sa sb sum_(k in block) E4M3(a_mk) E4M3(b_nk),
- * a block's products and their sum on the tensor cores in fp32, the sums over
- * blocks in fp32, one rounding to bf16.  The scales may be any fp32 values.  A
+ * exact products summed on the tensor cores in fp32 (which drop what lies below
+ * an accumulator's last bit; at most 8192 terms to an accumulator, or K / 16
+ * where that is more, the accumulators then added in fp32), one rounding to bf16.  A
  * linear layer's passes, for X (tokens x D), W (C x D) and dH (tokens x C): the
  * forward from X and W, grad_X from dH and W^T, grad_W from dH^T and X^T.
  * M, N, K <= 2^22.  Workspace: fqt_fp8_matmul_workspace_size(M, N, K) bytes.

@@ -1,13 +1,8 @@
 // fqt_fp8.cu -- matrix products of 8-bit floating-point codes (E4M3) with one
-// scale for each block of 128 entries along the contraction, and their quantizer.
+// power-of-two scale for each block of 128 entries along the contraction, and their
+// quantizer.
 //
-//   out_mn = sum_kb sa[kb][m] sb[kb][n] sum_(k in block kb) a_mk b_nk
-//
-// The inner sum of a block runs on the tensor cores (tcgen05 kind::f8f6f4, products
-// exact, fp32 accumulators in tensor memory); the scales belong to blocks, so each
-// block's sums are read back, multiplied by their two scales and added to fp32
-// running sums in registers: 128 sums a thread, two accumulators in tensor memory in
-// turn, so that the fold of one block overlaps the next block's products.
+//   out_mn = sum_kb 2^(ea[kb][m] + eb[kb][n]) sum_(k in block kb) a_mk b_nk
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -34,7 +29,8 @@ __device__ __forceinline__ int f8_exponent(uint32_t amax) {
   const int e = (int)(amax >> 23) - 127 - 8 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   return max(e, -127);  // subnormal amax too
 }
-__device__ __forceinline__ float pow2(int e) {  // -127 <= e <= 127
+// 2^e, -127 <= e <= 127
+__device__ __forceinline__ float pow2(int e) {
   return __uint_as_float(e > -127 ? (uint32_t)(e + 127) << 23 : 1u << 22);
 }
 
@@ -51,11 +47,15 @@ struct F8QuantArgs {
   int cols;
   uint8_t *c, *ct;  // codes by rows, and of the transpose (either may be null)
   int64_t pitch, pitch_t;
-  float *s, *st;  // scales [column block][row], [row block][column]
-  int64_t sp, spt;
+  uint8_t *s, *st;  // scales, four blocks of a row side by side (fqt.h)
+  int64_t sp, spt;  // rows of scales
   int whole;  // one scale for the 128 x 128 block
   int *status;
 };
+
+__device__ __forceinline__ int64_t scale_at(int64_t block, int64_t rows, int64_t row) {
+  return ((block >> 2) * rows + row) * 4 + (block & 3);
+}
 
 constexpr int kF8Pitch = kF8Block + 16;  // bytes of a transposed row in shared memory
 
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256) k_f8_quant(const F8QuantArgs a, const boo
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int e = f8_exponent(rm[i]);
-      if (cg == 0) a.s[blockIdx.x * a.sp + row + i] = row + i < a.rows ? pow2(e) : 0.0f;
+      if (cg == 0) a.s[scale_at(blockIdx.x, a.sp, row + i)] = (uint8_t)(e + 127);
       if (row + i >= a.rows || col >= a.cols) continue;
       const float inv = pow2(-e);
       uint32_t w[2];
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(256) k_f8_quant(const F8QuantArgs a, const boo
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int e = f8_exponent(cm[j]);
-      if (rg == 0) a.st[blockIdx.y * a.spt + col + j] = col + j < a.cols ? pow2(e) : 0.0f;
+      if (rg == 0) a.st[scale_at(blockIdx.y, a.spt, col + j)] = (uint8_t)(e + 127);
       const float inv = pow2(-e);
       uint32_t w[2];
 #pragma unroll
@@ -181,24 +181,26 @@ __global__ void __launch_bounds__(256) k_f8_quant(const F8QuantArgs a, const boo
 // ---------------------------------------------------------------------------
 // Product
 // ---------------------------------------------------------------------------
-constexpr int kF8EpiWarps = 8, kF8Epi0 = 4;  // warps 0 loads, 1 products, 2 and 3 none
+// The scales are powers of two, so the tensor cores apply them themselves: tcgen05
+// kind::mxf8f6f4 multiplies the sum of 32 products by 2^(ea + eb), with ea and eb read
+// from tensor memory, before it adds it to the fp32 accumulator.  Its scales belong to
+// 32 entries of K; a block's four steps use the same ones.  (With unscaled products,
+// each block's sums read back and folded into registers, the hand-over of an
+// accumulator for every 128 entries of K bound the kernel: 172 us for 8192 x 4096 x
+// 4096, with per-row scales on both sides 232.)
+constexpr int kF8EpiWarps = 8, kF8Epi0 = 4;  // warps 0 loads, 1 products, 2 and 3 scales
 constexpr int kF8Threads = 32 * (kF8Epi0 + kF8EpiWarps);
-constexpr int kF8RegsCtl = 64, kF8RegsEpi = 216;
-static_assert(128 * kF8RegsCtl + 256 * kF8RegsEpi <= kF8Threads * ((65536 / kF8Threads) / 8 * 8),
-              "register shares exceed the launch's");
-constexpr int kF8Band = 8;  // row tiles of a band of tiles
-// Scales: an epilogue warp keeps those of four K blocks (32 of A's rows, then up to 128
-// of B's) in shared memory and the next four on their way in registers; a read from L2
-// takes as long as two or three K blocks of products.
-constexpr int kF8Ahead = 4;
-constexpr size_t kF8ScaleBytes = 640;
-constexpr size_t kF8OffBar = kF8Ahead * kF8EpiWarps * kF8ScaleBytes;
-constexpr size_t kF8Bars = 2 * kMaxStages + 5;
+constexpr int kF8Group = 4;             // K blocks whose scales share a 32-bit word
+constexpr int kF8Ring = 4;              // groups of scales in shared memory
+constexpr size_t kF8RingBytes = 1536;   // 128 of A's rows, up to 256 of B's
+constexpr size_t kF8OffBar = kF8Ring * kF8RingBytes;
+constexpr size_t kF8Bars = 2 * kMaxStages + 2 * kF8Ring + 5;
 constexpr size_t kF8Fixed = (kF8OffBar + kF8Bars * 8 + 16 + 1023) & ~(size_t)1023;
-constexpr size_t kF8BoxBytes = 4096;    // an epilogue warp's 32 rows x 128 bytes of output
+constexpr size_t kF8BoxBytes = 4096;    // an epilogue warp's boxes of output
+constexpr int kF8Band = 8;              // row tiles of a band of tiles
 
 struct F8Args {
-  const float *sa, *sb;  // scales, K blocks spa / spb entries apart
+  const uint32_t *sa, *sb;  // scales of four K blocks a word, groups spa / spb words apart
   int64_t spa, spb;
   int64_t M, N;  // rows of A and of B
   int nkb;       // K blocks
@@ -210,7 +212,6 @@ struct F8Args {
   int boxes;       // out is written in boxes by TMA
   float *part;     // splits > 1: fp32 partial outputs, one after another
   int stages;
-  int b_whole;  // B's scale is one for 128 rows
   int *status;
 };
 
@@ -223,9 +224,32 @@ __device__ __forceinline__ bool f8_wait(uint64_t *bar, uint32_t parity, int *sta
   return mbar_wait(bar, parity, status);
 }
 
+// A wait that acquires what the pair's other CTA has written.
+__device__ __forceinline__ bool f8_wait_cluster(uint64_t *bar, uint32_t parity, int *status) {
+  uint64_t t0 = 0;
+  for (int i = 0;; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(20000u)
+        : "memory");
+    if (ok) return true;
+    if ((i & 3) == 3) {
+      const uint64_t t = global_ns();
+      if (t0 == 0) t0 = t;
+      if (t - t0 > kWaitLimitNs) {
+        record_status(status, FQT_ETIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+
 // The accumulator's reader is done with it (the pair's leader counts both CTAs).  What
-// it read is ordered by tcgen05.wait and tcgen05.fence; a releasing arrival would also
-// wait for the scales on their way.
+// it read is ordered by tcgen05.wait and tcgen05.fence.
 template <bool PAIR>
 __device__ __forceinline__ void f8_release(uint64_t *bar) {
   if constexpr (PAIR)
@@ -237,27 +261,47 @@ __device__ __forceinline__ void f8_release(uint64_t *bar) {
                  : "memory");
 }
 
+// 32 entries of K: D (+)= 2^(ea + eb) A B^T, the exponents in the bytes of the
+// tensor-memory words at sa and sb that the instruction descriptor names.
 template <bool PAIR>
 __device__ __forceinline__ void f8_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t accumulate) {
+                                       uint32_t sa, uint32_t sb, uint32_t accumulate) {
   if constexpr (PAIR)
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X "
+        "[%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
         : "memory");
   else
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X "
+        "[%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
         : "memory");
 }
 
-// An item: this CTA's 128 rows of A against NT rows of B over some K blocks.  The
-// two CTAs of a pair take the same item, each its 128 of the super tile's 256 rows.
+// Scales of 128 rows from shared memory (32 rows of 16 bytes: word w of row r is that
+// of row 32 w + r) to four columns of tensor memory, in every quadrant of its lanes.
+template <bool PAIR>
+__device__ __forceinline__ void f8_copy_scales(uint32_t taddr, uint32_t saddr) {
+  // 8 x 16 byte core matrices 128 bytes apart, no swizzle, descriptor version 1
+  const uint64_t desc = (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 |
+                        (uint64_t)1 << 46;
+  if constexpr (PAIR)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc)
+                 : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc)
+                 : "memory");
+}
+
+// An item: this CTA's 128 rows of A against NT rows of B over some K blocks (from a
+// multiple of kF8Group).  The two CTAs of a pair take the same item, each its 128 of
+// the super tile's 256 rows.
 struct F8Item {
   int64_t m0, n0;
   int kb0, kb1, split;
@@ -288,170 +332,103 @@ __device__ __forceinline__ T f8_out(float v) {
   else return __float2bfloat16_rn(v);
 }
 
-// 16 bytes of output from the sums at acc.
+// 16 bytes of output from the sums at v (fp32 bits).
 template <typename T>
-__device__ __forceinline__ uint4 f8_pack(const f32x2 *acc) {
-  uint32_t w[4];
+__device__ __forceinline__ uint4 f8_pack(const uint32_t *v) {
+  if constexpr (sizeof(T) == 4) {
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  } else {
+    uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float u, v;
-    if constexpr (sizeof(T) == 4) {
-      unpack2(acc[i / 2], u, v);
-      w[i] = __float_as_uint(i & 1 ? v : u);
-    } else {
-      unpack2(acc[i], u, v);
-      const __nv_bfloat162 b = __floats2bfloat162_rn(u, v);
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b =
+          __floats2bfloat162_rn(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
       w[i] = *reinterpret_cast<const uint32_t *>(&b);
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// This thread's W sums: row m of the tile's rows, columns n .. n + W - 1.
-template <typename T, int W>
+// This thread's 32 sums: row m of the tile's rows, columns n ..
+template <typename T>
 __device__ __forceinline__ void f8_store(const F8Args &g, T *out, int64_t ld, int64_t m,
-                                         int64_t n, const f32x2 (&acc)[W / 2]) {
+                                         int64_t n, const uint32_t (&v)[32], int W) {
   if (m >= g.M) return;
   if (g.swap) {
 #pragma unroll
-    for (int j = 0; j < W / 2; ++j) {
-      float u, v;
-      unpack2(acc[j], u, v);
-      if (n + 2 * j < g.N) out[(n + 2 * j) * ld + m] = f8_out<T>(u);
-      if (n + 2 * j + 1 < g.N) out[(n + 2 * j + 1) * ld + m] = f8_out<T>(v);
-    }
+    for (int j = 0; j < 32; ++j)
+      if (j < W && n + j < g.N) out[(n + j) * ld + m] = f8_out<T>(__uint_as_float(v[j]));
     return;
   }
   T *p = out + m * ld + n;
   constexpr int E = 16 / sizeof(T);
   const bool vec = (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 #pragma unroll
-  for (int j = 0; j < W; j += E) {
+  for (int j = 0; j < 32; j += E) {
+    if (j >= W) break;
     if (vec && n + j + E <= g.N) {
-      *reinterpret_cast<uint4 *>(p + j) = f8_pack<T>(&acc[j / 2]);
+      *reinterpret_cast<uint4 *>(p + j) = f8_pack<T>(&v[j]);
     } else {
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        float u, v;
-        unpack2(acc[(j + i) / 2], u, v);
-        if (n + j + i < g.N) p[j + i] = f8_out<T>(i & 1 ? v : u);
-      }
+      for (int i = 0; i < E; ++i)
+        if (n + j + i < g.N) p[j + i] = f8_out<T>(__uint_as_float(v[j + i]));
     }
   }
 }
 
-// The same through boxes of 32 rows x 128 bytes: a warp lays its rows' 128 bytes in
-// shared memory (128-byte swizzle) and TMA writes them, leaving out what lies past
-// the output's ends.  (Stored from registers, a warp's 16-byte pieces of 32 rows
-// take half a sector each.)
-template <typename T, int W>
-__device__ __forceinline__ void f8_store_boxes(const F8Args &g, const CUtensorMap *map,
-                                               uint8_t *box, int lane, int64_t m0, int64_t n,
-                                               const f32x2 (&acc)[W / 2]) {
-  constexpr int E = 16 / sizeof(T), C = 8 * E;  // columns of a box
-  if (m0 >= g.M) return;
+// The same for a warp's 32 rows at once, through a box in shared memory that TMA writes
+// (it leaves out what lies past the output's ends): 32 columns of fp32 in rows of 128
+// bytes (128-byte swizzle), or of bf16 in rows of 64 (64-byte swizzle).  Stored from
+// registers, a warp's 16-byte pieces of 32 rows take half a sector each.
+template <typename T>
+__device__ __forceinline__ void f8_store_box(const F8Args &g, const CUtensorMap *map,
+                                             uint8_t *box, int lane, int64_t m0, int64_t n,
+                                             const uint32_t (&v)[32]) {
+  constexpr int E = 16 / sizeof(T);
+  constexpr int kBoxes = sizeof(T) == 4 ? 1 : 2;  // boxes of a warp
+  if (m0 >= g.M || n >= g.N) return;
+  if (lane == 0) bulk_wait_read(kBoxes - 1);
+  __syncwarp();
 #pragma unroll
-  for (int j = 0; j < W; j += C) {
-    if (n + j >= g.N) break;
-    if (lane == 0) bulk_wait_read(0);
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      *reinterpret_cast<uint4 *>(box + sw128_off(lane, k)) = f8_pack<T>(&acc[(j + k * E) / 2]);
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      tma_store_2d(map, (int32_t)(n + j), (int32_t)m0, box);
-      bulk_commit();
-    }
+  for (int k = 0; k < 32 / E; ++k) {
+    const uint32_t at = sizeof(T) == 4 ? sw128_off(lane, k)
+                                       : (uint32_t)(lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4));
+    *reinterpret_cast<uint4 *>(box + at) = f8_pack<T>(&v[k * E]);
   }
-}
-
-// The scales of kF8Ahead K blocks on their way: this lane's row of A, and four of B's
-// columns a lane (or, with one scale for 128 of B's rows, the one of the first column).
-// Entries past the ends of the scales are others' and belong to no output.
-template <int W>
-struct F8Ahead {
-  float a[kF8Ahead];
-  float4 b[kF8Ahead];
-  __device__ __forceinline__ void get(const F8Args &g, int64_t m, int64_t n, int kb, int kb1,
-                                      int lane) {
-    const float *pa = g.sa + min(m + lane, g.spa - 1);
-    const float *pb = g.sb + (g.b_whole ? min(n, g.spb - 1) : min(n + 4 * lane, g.spb - 4));
-#pragma unroll
-    for (int i = 0; i < kF8Ahead; ++i) {
-      if (kb + i >= kb1) break;
-      a[i] = __ldg(pa + (kb + i) * g.spa);
-      if (g.b_whole) b[i].x = __ldg(pb + (kb + i) * g.spb);
-      else if (4 * lane < W) b[i] = __ldg(reinterpret_cast<const float4 *>(pb + (kb + i) * g.spb));
-    }
-  }
-  __device__ __forceinline__ void put(float *sc, int lane, bool whole) const {
-#pragma unroll
-    for (int i = 0; i < kF8Ahead; ++i) {
-      float *to = sc + i * (int)(kF8ScaleBytes / 4);
-      to[lane] = a[i];
-      if (whole) to[32] = b[i].x;
-      else if (4 * lane < W) reinterpret_cast<float4 *>(to + 32)[lane] = b[i];
-    }
-  }
-};
-
-// Adds one accumulator's W columns, scaled, to the sums.  The columns come in pieces
-// of 16, the next one on its way while this one is added.
-template <int W>
-__device__ __forceinline__ void f8_fold(uint32_t taddr, float sa, const float *sb, bool whole,
-                                        f32x2 (&acc)[W / 2]) {
-  constexpr int CH = 16;
-  const float s1 = sa * sb[0];
-  const f32x2 s2 = pack2(s1, s1), sa2 = pack2(sa, sa);
-  uint32_t r[2][CH];
-  tmem_ldw_nw<CH>(taddr, r[0]);
-  tmem_wait_ld(r[0]);
-#pragma unroll
-  for (int j = 0; j < W; j += CH) {
-    const uint32_t(&v)[CH] = r[(j / CH) & 1];
-    if (j + CH < W) tmem_ldw_nw<CH>(taddr + (uint32_t)(j + CH), r[(j / CH + 1) & 1]);
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < CH; i += 2)
-        acc[(j + i) / 2] =
-            fma2(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), s2, acc[(j + i) / 2]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < CH; i += 4) {
-        const float4 b = *reinterpret_cast<const float4 *>(sb + j + i);
-        acc[(j + i) / 2] = fma2(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])),
-                                mul2(sa2, pack2(b.x, b.y)), acc[(j + i) / 2]);
-        acc[(j + i) / 2 + 1] = fma2(pack2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])),
-                                    mul2(sa2, pack2(b.z, b.w)), acc[(j + i) / 2 + 1]);
-      }
-    }
-    if (j + CH < W) tmem_wait_ld(r[(j / CH + 1) & 1]);
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_2d(map, (int32_t)n, (int32_t)m0, box);
+    bulk_commit();
   }
 }
 
 // One CTA per 128 x NT tile (and split of the K blocks), persistent, or a pair of CTAs
-// per 256 x 256 super tile: each loads its 128 rows of A and 128 of B's 256 rows, and
+// per 256 x NT super tile: each loads its 128 rows of A and half of B's NT rows, and
 // the leader issues products over both (cta_group::2), so an operand byte is loaded
-// for twice the products.  Warp 0 feeds operand stages of one K block by TMA, warp 1
-// issues a K block's four products into one of two accumulators; the eight epilogue
-// warps (quadrant of rows x half of the columns) read the blocks' scales ahead and
-// fold each K block into their sums.
-template <int NT, bool PAIR>
+// for twice the products.  Warp 0 feeds operand stages of one K block by TMA, warps 2
+// and 3 in turn the scales of four K blocks, warp 1 issues a K block's four products;
+// the eight epilogue warps (quadrant of rows x half of the columns) take an accumulator
+// into registers, hand it back and store it.  ACCS accumulators of NT columns: with two
+// a tile's products overlap the epilogue of the one before.
+template <int NT, int ACCS, bool PAIR>
 __global__ void __launch_bounds__(kF8Threads, 1)
     k_f8_mm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
             const __grid_constant__ CUtensorMap tmOut, const F8Args g) {
-  static_assert(!PAIR || NT == 256, "a pair's super tile has 256 columns");
-  constexpr int W = NT / 2;                 // columns of an epilogue warp
+  // columns of an epilogue warp: a multiple of 32 for the first half's
+  constexpr int W0 = NT <= 64 ? NT / 2 : (NT / 2 + 31) / 32 * 32, W1 = NT - W0;
   constexpr int NB = PAIR ? NT / 2 : NT;    // rows of B that this CTA loads
   constexpr uint32_t kStage = (uint32_t)(kTileBytes + NB * kF8Block);
-  constexpr uint32_t kCols = 2 * NT < 32 ? 32 : 2 * NT;
+  constexpr int kSbCols = (NT + 127) / 128 * 4;       // columns of B's scales
+  constexpr uint32_t kScales = ACCS * NT;             // two buffers of A's and B's scales
+  constexpr uint32_t kUsed = kScales + 2 * (4 + kSbCols);
+  constexpr uint32_t kCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+  static_assert(kUsed <= 512, "tensor memory has 512 columns");
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t *full = reinterpret_cast<uint64_t *>(smem + kF8OffBar), *empty = full + kMaxStages;
   uint64_t *accf = empty + kMaxStages, *acce = accf + 2;
-  uint64_t *drain = acce + 2;
+  uint64_t *sfull = acce + 2, *sempty = sfull + kF8Ring, *drain = sempty + kF8Ring;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(full + kF8Bars);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   uint8_t *ops = smem + kF8Fixed;
@@ -467,6 +444,10 @@ __global__ void __launch_bounds__(kF8Threads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(&accf[i], 1);
       mbar_init(&acce[i], (PAIR ? 2 : 1) * kF8EpiWarps);
+    }
+    for (int i = 0; i < kF8Ring; ++i) {
+      mbar_init(&sfull[i], PAIR ? 2 : 1);
+      mbar_init(&sempty[i], 1);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -494,68 +475,60 @@ __global__ void __launch_bounds__(kF8Threads, 1)
   const uint32_t tmem = *tmem_slot;
 
   if (warp >= kF8Epi0) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kF8RegsEpi));
     const int q = warp & 3, h = (warp - kF8Epi0) >> 2;
-    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * W);
+    const int W = h ? W1 : W0;
+    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * W0);
     uint8_t *box = ops + (size_t)g.stages * kStage + (size_t)(warp - kF8Epi0) * kF8BoxBytes;
-    float *sc = reinterpret_cast<float *>(smem + kF8Ahead * (warp - kF8Epi0) * kF8ScaleBytes);
-    F8Ahead<W> ahead;
-    if (first < g.items) {
-      const F8Item t = f8_item<NT, PAIR>(g, first);
-      ahead.get(g, t.m0 + q * 32, t.n0 + h * W, t.kb0, t.kb1, lane);
-    }
-    uint32_t c = 0;  // K blocks so far
-    bool ok = true;
-    for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step) {
+    uint32_t c = 0;  // tiles so far
+    int nbox = 0;
+    for (int64_t it = first; it < g.items && !*abort_flag; it += step, ++c) {
       const F8Item t = f8_item<NT, PAIR>(g, it);
-      f32x2 acc[W / 2];
-#pragma unroll
-      for (int j = 0; j < W / 2; ++j) acc[j] = pack2(0.0f, 0.0f);
-      const int64_t m = t.m0 + q * 32, n = t.n0 + h * W;
-      for (int kb = t.kb0; kb < t.kb1; ++kb, ++c) {
-        const int buf = c & 1, at = (kb - t.kb0) % kF8Ahead;
-        if (at == 0) {
-          __syncwarp();
-          ahead.put(sc, lane, g.b_whole);
-          __syncwarp();
-          if (kb + kF8Ahead < t.kb1) {
-            ahead.get(g, m, n, kb + kF8Ahead, t.kb1, lane);
-          } else if (it + step < g.items) {
-            const F8Item u = f8_item<NT, PAIR>(g, it + step);
-            ahead.get(g, u.m0 + q * 32, u.n0 + h * W, u.kb0, u.kb1, lane);
-          }
-        }
-        if (!f8_wait(&accf[buf], (c >> 1) & 1u, g.status)) {
-          *abort_flag = 1;
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        const float *mine = sc + at * (int)(kF8ScaleBytes / 4);
-        f8_fold<W>(lane_base + (uint32_t)(buf * NT), mine[lane], mine + 32, g.b_whole, acc);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) f8_release<PAIR>(&acce[buf]);
+      const int buf = c % ACCS;
+      if (!f8_wait(&accf[buf], (c / ACCS) & 1u, g.status)) {
+        *abort_flag = 1;
+        break;
       }
-      if (!ok) break;
-      if (W >= 64 && g.boxes) {
-        if constexpr (W >= 64) {
-          if (g.bf16) f8_store_boxes<__nv_bfloat16, W>(g, &tmOut, box, lane, m, n, acc);
-          else f8_store_boxes<float, W>(g, &tmOut, box, lane, m, n, acc);
+      tc_fence_after();
+      constexpr int P = (W0 + 31) / 32;  // pieces of up to 32 columns
+      uint32_t v[P][32];
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        if (32 * p < W) {
+          if constexpr (W0 < 32)
+            tmem_ld16_nw(lane_base + (uint32_t)(buf * NT),
+                         *reinterpret_cast<uint32_t(*)[16]>(v[0]));
+          else
+            tmem_ld32_nw(lane_base + (uint32_t)(buf * NT + 32 * p), v[p]);
         }
-      } else if (g.splits > 1) {
-        f8_store<float, W>(g, g.part + t.split * g.M * g.N, g.swap ? g.M : g.N, m + lane, n, acc);
-      } else if (g.bf16) {
-        f8_store<__nv_bfloat16, W>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, m + lane, n,
-                                   acc);
-      } else {
-        f8_store<float, W>(g, static_cast<float *>(g.out), g.ldo, m + lane, n, acc);
+#pragma unroll
+      for (int p = 0; p < P; ++p) tmem_wait_ld(v[p]);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) f8_release<PAIR>(&acce[buf]);
+      const int64_t m = t.m0 + q * 32, n = t.n0 + h * W0;
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        if (32 * p >= W) break;
+        const int64_t np = n + 32 * p;
+        if (NT > 64 && g.boxes) {
+          if (g.bf16)
+            f8_store_box<__nv_bfloat16>(g, &tmOut, box + (nbox ^= 1) * 2048, lane, m, np, v[p]);
+          else
+            f8_store_box<float>(g, &tmOut, box, lane, m, np, v[p]);
+        } else if (g.splits > 1) {
+          f8_store<float>(g, g.part + t.split * g.M * g.N, g.swap ? g.M : g.N, m + lane, np, v[p],
+                          W);
+        } else if (g.bf16) {
+          f8_store<__nv_bfloat16>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, m + lane, np,
+                                  v[p], W);
+        } else {
+          f8_store<float>(g, static_cast<float *>(g.out), g.ldo, m + lane, np, v[p], W);
+        }
       }
     }
     if (lane == 0) bulk_wait_all();
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kF8RegsCtl));
-    if (warp == 0 && lane == 0) {
+  } else if (warp == 0) {
+    if (lane == 0) {
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
@@ -590,19 +563,44 @@ __global__ void __launch_bounds__(kF8Threads, 1)
           if (++s == g.stages) { s = 0; ph ^= 1u; }
         }
       }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
       int s = 0;
-      uint32_t ph = 0, c = 0;
+      uint32_t ph = 0, c = 0, grp = 0;
       bool ok = true;
-      // D fp32; A, B E4M3 (format 0), both K-major
-      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(NT >> 3) << 17) |
-                                 ((uint32_t)((PAIR ? 2 * BM : BM) >> 4) << 24);
-      for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step) {
+      // D fp32; A, B E4M3 (format 0), both K-major; E8M0 scales; bits 4-5 and 29-30: the
+      // byte of B's and A's scale words
+      constexpr uint32_t idesc0 = ((uint32_t)(NT >> 3) << 17) | (1u << 23) |
+                                  ((uint32_t)(PAIR ? 2 : 1) << 27);
+      for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step, ++c) {
         const F8Item t = f8_item<NT, PAIR>(g, it);
-        for (int kb = t.kb0; kb < t.kb1; ++kb, ++c) {
-          const int buf = c & 1;
-          if (!f8_wait(&acce[buf], ((c >> 1) & 1u) ^ 1u, g.status) ||
-              !f8_wait(&full[s], ph, g.status)) {
+        const int buf = c % ACCS;
+        if (!f8_wait(&acce[buf], ((c / ACCS) & 1u) ^ 1u, g.status)) {
+          *abort_flag = 1;
+          break;
+        }
+        uint32_t sa = 0;
+        for (int kb = t.kb0; kb < t.kb1; ++kb) {
+          if ((kb & (kF8Group - 1)) == 0) {  // the next group's scales
+            const int slot = grp % kF8Ring;
+            if (!f8_wait_cluster(&sfull[slot], (grp / kF8Ring) & 1u, g.status)) {
+              *abort_flag = 1;
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            sa = tmem + kScales + (grp & 1u) * (4 + kSbCols);
+            const uint32_t src = smem_u32(smem + slot * kF8RingBytes);
+            f8_copy_scales<PAIR>(sa, src);
+#pragma unroll
+            for (int i = 0; i < kSbCols / 4; ++i)
+              f8_copy_scales<PAIR>(sa + 4 + 4 * i, src + 512 + 512 * i);
+            if constexpr (PAIR) umma_commit_pair(&sempty[slot]);
+            else umma_commit(&sempty[slot]);
+            ++grp;
+          }
+          if (!f8_wait(&full[s], ph, g.status)) {
             *abort_flag = 1;
             ok = false;
             break;
@@ -610,19 +608,19 @@ __global__ void __launch_bounds__(kF8Threads, 1)
           tc_fence_after();
           const uint32_t a_addr = smem_u32(ops + (size_t)s * kStage);
           const uint64_t da = sw128_desc(a_addr), db = sw128_desc(a_addr + (uint32_t)kTileBytes);
+          const uint32_t id = (uint32_t)kb & (kF8Group - 1);
+          const uint32_t idesc = idesc0 | id << 4 | id << 29;
 #pragma unroll
           for (int k = 0; k < 4; ++k)  // 32 entries each
-            f8_mma<PAIR>(tmem + (uint32_t)(buf * NT), da + 2 * k, db + 2 * k, idesc,
-                         k > 0 ? 1u : 0u);
-          if constexpr (PAIR) {
-            umma_commit_pair(&empty[s]);
-            umma_commit_pair(&accf[buf]);
-          } else {
-            umma_commit(&empty[s]);
-            umma_commit(&accf[buf]);
-          }
+            f8_mma<PAIR>(tmem + (uint32_t)(buf * NT), da + 2 * k, db + 2 * k, idesc, sa, sa + 4,
+                         (k > 0 || kb > t.kb0) ? 1u : 0u);
+          if constexpr (PAIR) umma_commit_pair(&empty[s]);
+          else umma_commit(&empty[s]);
           if (++s == g.stages) { s = 0; ph ^= 1u; }
         }
+        if (!ok) break;
+        if constexpr (PAIR) umma_commit_pair(&accf[buf]);
+        else umma_commit(&accf[buf]);
       }
       // every product has completed before tensor memory is released
       if constexpr (PAIR)
@@ -634,6 +632,46 @@ __global__ void __launch_bounds__(kF8Threads, 1)
         umma_commit(drain);
       f8_wait(drain, 0, g.status);
     }
+  } else {
+    // scales: words of four K blocks, warps 2 and 3 a group in turn
+    uint32_t grp = 0;
+    bool ok = true;
+    for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step) {
+      const F8Item t = f8_item<NT, PAIR>(g, it);
+      for (int kb = t.kb0; kb < t.kb1; kb += kF8Group, ++grp) {
+        if ((grp & 1u) != (uint32_t)(warp - 2)) continue;
+        const int slot = grp % kF8Ring;
+        const int64_t kg = kb / kF8Group;
+        uint32_t w[4 + kSbCols];
+#pragma unroll
+        for (int i = 0; i < 4 + kSbCols; ++i) {  // row 32 i + lane of A's, then of B's
+          const bool in_a = i < 4;
+          const int64_t r = in_a ? t.m0 + 32 * i + lane : t.n0 + 32 * (i - 4) + lane;
+          // rows past the ends: any scale that is a number (127: one)
+          w[i] = r < (in_a ? g.spa : g.spb)
+                     ? __ldg((in_a ? g.sa + kg * g.spa : g.sb + kg * g.spb) + r)
+                     : 0x7F7F7F7Fu;
+        }
+        if (!f8_wait(&sempty[slot], ((grp / kF8Ring) & 1u) ^ 1u, g.status)) {
+          *abort_flag = 1;
+          ok = false;
+          break;
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(smem + slot * kF8RingBytes);
+#pragma unroll
+        for (int i = 0; i < (4 + kSbCols) / 4; ++i)
+          dst[32 * i + lane] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) mbar_arrive_cluster(leader_addr(&sfull[slot]));
+          else mbar_arrive(&sfull[slot]);
+        }
+      }
+    }
+    // the last copies have been read (and, in a pair, the leader's arrivals are in)
+    for (int i = 0; ok && i < kF8Ring; ++i, ++grp)
+      ok = f8_wait(&sempty[grp % kF8Ring], ((grp / kF8Ring) & 1u) ^ 1u, g.status);
   }
   tc_fence_before();
   __syncthreads();
@@ -683,7 +721,7 @@ static bool make_map_codes(CUtensorMap *m, const fqt_fp8 *q, uint32_t box_rows) 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output as boxes of 32 rows x 128 bytes (its base and its pitch on 16 bytes).
+// The output as boxes of 32 x 32 (its base and its pitch on 16 bytes).
 static bool make_map_f8_out(CUtensorMap *m, void *out, bool bf16, int64_t rows, int64_t cols,
                             int64_t ldo) {
   EncodeTiledFn fn = encode_fn();
@@ -691,10 +729,11 @@ static bool make_map_f8_out(CUtensorMap *m, void *out, bool bf16, int64_t rows, 
   const cuuint64_t es = bf16 ? 2 : 4;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ldo * es};
-  cuuint32_t box[2] = {(cuuint32_t)(128 / es), 32};
+  cuuint32_t box[2] = {32, 32};
   cuuint32_t one[2] = {1, 1};
   return fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, out,
-            dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_NONE,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -718,18 +757,17 @@ static F8Plan f8_plan(int64_t M, int64_t N, int64_t nkb, int nsm) {
   p.m_tiles = (int)((a + rows - 1) / rows);
   p.nt = p.pair ? 256 : !p.swap ? 128 : b <= 32 ? 32 : 64;
   p.n_tiles = (int)((b + p.nt - 1) / p.nt);
-  if (p.pair) {
-    p.splits = 1;
-    p.kb_per = (int)nkb;
-    return p;
-  }
   const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
-  // fewer tiles than SMs: the contraction is split, at least 4 K blocks each
-  int64_t splits = tiles < nsm ? nsm / tiles : 1;
-  if (splits > nkb / 4) splits = nkb / 4;
+  // fewer tiles than SMs: the contraction is split, into groups of K blocks
+  const int64_t groups = (nkb + kF8Group - 1) / kF8Group;
+  int64_t splits = tiles * 4 <= (int64_t)nsm * 3 && !p.pair ? nsm / tiles : 1;
+  // ... and where an accumulator would take more than 8192 terms: a step of the tensor
+  // core drops what lies below the accumulator's last bit (5e-7 of the result after
+  // 8192 terms, 8e-6 after 65536)
+  if (splits < (groups + 15) / 16) splits = (groups + 15) / 16;
+  if (splits > groups) splits = groups;
   if (splits > 16) splits = 16;
-  if (splits < 1) splits = 1;
-  p.kb_per = (int)((nkb + splits - 1) / splits);
+  p.kb_per = (int)((groups + splits - 1) / splits) * kF8Group;
   p.splits = (int)((nkb + p.kb_per - 1) / p.kb_per);
   return p;
 }
@@ -740,16 +778,16 @@ size_t fp8_matmul_ws_bytes(int64_t M, int64_t N, int64_t K) {
   return kHeaderBytes + (p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0);
 }
 
-template <int NT, bool PAIR>
+template <int NT, int ACCS, bool PAIR>
 static fqt_status launch_f8(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &to,
                             F8Args &g, int nsm, cudaStream_t st) {
   constexpr size_t stage = kTileBytes + (PAIR ? NT / 2 : NT) * kF8Block;
-  constexpr size_t boxes = NT >= 128 ? kF8EpiWarps * kF8BoxBytes : 0;
+  constexpr size_t boxes = NT > 64 ? kF8EpiWarps * kF8BoxBytes : 0;
   constexpr size_t room = 227 * 1024 - 1024 - kF8Fixed - boxes;
   constexpr int stages = room / stage < kMaxStages ? (int)(room / stage) : kMaxStages;
   constexpr size_t smem = 1024 + kF8Fixed + stages * stage + boxes;
   g.stages = stages;
-  auto kernel = k_f8_mm<NT, PAIR>;
+  auto kernel = k_f8_mm<NT, ACCS, PAIR>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)smem);
   if (e != cudaSuccess) return cuda_fail(e, "FP8 product attribute");
@@ -775,7 +813,7 @@ static bool f8_aligned(const void *p, size_t n) {
   return reinterpret_cast<uintptr_t>(p) % n == 0;
 }
 
-static int64_t scale_pitch(int64_t rows) { return (rows + kF8Block - 1) / kF8Block * kF8Block; }
+static int64_t scale_rows(int64_t rows) { return (rows + kF8Block - 1) / kF8Block * kF8Block; }
 
 // a code matrix whose rows and pitch stay inside 32-bit coordinates and 64-bit offsets
 static bool f8_good(const fqt_fp8 *q) {
@@ -796,13 +834,13 @@ fqt_status quantize_fp8(const void *X, int64_t ldx, bool bf16, int64_t rows, int
     a.c = q->codes;
     a.pitch = q->pitch;
     a.s = q->scales;
-    a.sp = scale_pitch(rows);
+    a.sp = scale_rows(rows);
   }
   if (qt) {
     a.ct = qt->codes;
     a.pitch_t = qt->pitch;
     a.st = qt->scales;
-    a.spt = scale_pitch(cols);
+    a.spt = scale_rows(cols);
   }
   const bool vec = f8_aligned(X, 16) && a.ldx * (bf16 ? 2 : 4) % 16 == 0;
   const dim3 grid((unsigned)((cols + kF8Block - 1) / kF8Block),
@@ -820,16 +858,16 @@ fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, 
   const fqt_fp8 *a = p.swap ? B : A, *b = p.swap ? A : B;
   F8Args g = {};
   g.ldo = M > 1 ? ldo : N;
-  g.boxes = p.nt >= 128 && p.splits == 1 && f8_aligned(out, 16) &&
+  g.boxes = p.nt > 64 && p.splits == 1 && f8_aligned(out, 16) &&
             g.ldo * (bf16 ? 2 : 4) % 16 == 0;
   CUtensorMap ta, tb, to = {};
-  if (!make_map_codes(&ta, a, BM) || !make_map_codes(&tb, b, p.pair ? 128u : (uint32_t)p.nt) ||
+  if (!make_map_codes(&ta, a, BM) || !make_map_codes(&tb, b, (uint32_t)(p.pair ? p.nt / 2 : p.nt)) ||
       (g.boxes && !make_map_f8_out(&to, out, bf16, M, N, g.ldo)))
     return cuda_fail(cudaErrorUnknown, "FP8 tensor map");
-  g.sa = a->scales;
-  g.sb = b->scales;
-  g.spa = scale_pitch(a->rows);
-  g.spb = scale_pitch(b->rows);
+  g.sa = reinterpret_cast<const uint32_t *>(a->scales);
+  g.sb = reinterpret_cast<const uint32_t *>(b->scales);
+  g.spa = scale_rows(a->rows);
+  g.spb = scale_rows(b->rows);
   g.M = a->rows;
   g.N = b->rows;
   g.nkb = (int)((K + kF8Block - 1) / kF8Block);
@@ -842,12 +880,11 @@ fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, 
   g.bf16 = bf16;
   g.swap = p.swap;
   g.part = reinterpret_cast<float *>(static_cast<char *>(ws) + kHeaderBytes);
-  g.b_whole = b->block_rows == kF8Block;
   g.status = static_cast<int *>(ws);
-  fqt_status s = p.pair        ? launch_f8<256, true>(ta, tb, to, g, nsm, st)
-                 : p.nt == 128 ? launch_f8<128, false>(ta, tb, to, g, nsm, st)
-                 : p.nt == 64  ? launch_f8<64, false>(ta, tb, to, g, nsm, st)
-                               : launch_f8<32, false>(ta, tb, to, g, nsm, st);
+  fqt_status s = p.pair        ? launch_f8<256, 1, true>(ta, tb, to, g, nsm, st)
+                 : p.nt == 128 ? launch_f8<128, 2, false>(ta, tb, to, g, nsm, st)
+                 : p.nt == 64  ? launch_f8<64, 2, false>(ta, tb, to, g, nsm, st)
+                               : launch_f8<32, 2, false>(ta, tb, to, g, nsm, st);
   if (s != FQT_OK || p.splits == 1) return s;
   const int64_t blocks = (M * N + 255) / 256;
   const int grid = (int)(blocks < 8 * nsm ? blocks : 8 * nsm);

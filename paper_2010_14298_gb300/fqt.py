@@ -704,8 +704,9 @@ class Fp8Tensor:
     fqt_fp8 of include/fqt.h).
 
     ``codes`` holds the E4M3 codes, rows of ``pitch`` bytes of which the first
-    ``cols`` count; ``scales`` one row per block of columns, of which the first
-    ``rows`` entries count.  ``block_rows``: rows that share a scale, 1 or 128.
+    ``cols`` count; ``scales`` the blocks' exponents + 127: ``scales[k // 4, r, k % 4]``
+    is that of block k of row r, of which the first ``rows`` rows count.
+    ``block_rows``: rows that share a scale, 1 or 128.
     """
     codes: torch.Tensor
     scales: torch.Tensor
@@ -715,8 +716,8 @@ class Fp8Tensor:
 
     def __post_init__(self):
         c, s = self.codes, self.scales
-        if c.dtype != torch.uint8 or s.dtype != torch.float32:
-            raise ValueError(f"codes are uint8 and scales float32, not {c.dtype} and {s.dtype}")
+        if c.dtype != torch.uint8 or s.dtype != torch.uint8:
+            raise ValueError(f"codes and scales are uint8, not {c.dtype} and {s.dtype}")
         if c.dim() != 2 or c.shape[0] != self.rows or c.shape[1] < self.cols or c.shape[1] % 16:
             raise ValueError(f"{self.rows} x {self.cols} codes do not lie in {tuple(c.shape)} bytes")
         if s.shape != self.scale_shape(self.rows, self.cols):
@@ -731,13 +732,13 @@ class Fp8Tensor:
 
     @staticmethod
     def scale_shape(rows: int, cols: int):
-        return -(-cols // FP8_BLOCK), -(-rows // FP8_BLOCK) * FP8_BLOCK
+        return -(-cols // (4 * FP8_BLOCK)), -(-rows // FP8_BLOCK) * FP8_BLOCK, 4
 
     @staticmethod
     def empty(rows: int, cols: int, block_rows: int = 1, device="cuda"):
         return Fp8Tensor(
             torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device),
-            torch.empty(Fp8Tensor.scale_shape(rows, cols), dtype=torch.float32, device=device),
+            torch.empty(Fp8Tensor.scale_shape(rows, cols), dtype=torch.uint8, device=device),
             rows, cols, block_rows)
 
     @property
@@ -755,8 +756,9 @@ class Fp8Tensor:
     def dequantize(self) -> torch.Tensor:
         """The values (fp32): code times scale."""
         v = self.codes[:, :self.cols].contiguous().view(torch.float8_e4m3fn).float()
-        s = self.scales[:, :self.rows].t().repeat_interleave(FP8_BLOCK, 1)
-        return v * s[:, :self.cols]
+        e = self.scales[:, :self.rows].permute(1, 0, 2).reshape(self.rows, -1).int()
+        s = torch.where(e > 0, e << 23, 1 << 22).view(torch.float32)
+        return v * s.repeat_interleave(FP8_BLOCK, 1)[:, :self.cols]
 
 
 def _fp8_out(t, name, rows, cols, block_rows, like, stream):

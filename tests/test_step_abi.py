@@ -98,11 +98,13 @@ def test_fp8_refusals():
 
 
 def test_fp8_tensors_that_do_not_fit_are_refused():
-    codes, scales = torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((1, 128))
+    u8 = dict(dtype=torch.uint8)
+    codes, scales = torch.zeros((4, 64), **u8), torch.zeros((1, 128, 4), **u8)
     fqt.Fp8Tensor(codes, scales, 4, 64)
-    for bad in (dict(codes=codes.int()), dict(scales=scales.double()), dict(rows=5),
+    for bad in (dict(codes=codes.int()), dict(scales=scales.float()), dict(rows=5),
                 dict(cols=65), dict(codes=torch.zeros((4, 60), dtype=torch.uint8)),
-                dict(scales=torch.zeros((1, 64))), dict(scales=torch.zeros((2, 128))),
+                dict(scales=torch.zeros((1, 64, 4), **u8)),
+                dict(scales=torch.zeros((2, 128, 4), **u8)),
                 dict(codes=torch.zeros((64, 4), dtype=torch.uint8).t()), dict(block_rows=2)):
         with pytest.raises(ValueError):
             fqt.Fp8Tensor(**{**dict(codes=codes, scales=scales, rows=4, cols=64), **bad})

@@ -57,123 +57,269 @@ __device__ __forceinline__ int64_t scale_at(int64_t block, int64_t rows, int64_t
   return ((block >> 2) * rows + row) * 4 + (block & 3);
 }
 
-constexpr int kF8Pitch = kF8Block + 16;  // bytes of a transposed row in shared memory
+// Entries that are no numbers, given as NaN: they count for no scale and take the NaN
+// code (0x7F or 0xFF).  Magnitudes are compared as integers.
+__device__ __forceinline__ uint32_t f8_mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// One CTA per 128 x 128 tile.  A thread holds 8 rows x 8 columns of it, so it packs
-// codes along either axis without exchanging bytes: 8 bytes of each of its rows go
-// straight to memory, 8 bytes of each of its columns through shared memory.  Bound by
-// memory traffic: the entries are read once for both outputs.
-template <typename T>
-__global__ void __launch_bounds__(256) k_f8_quant(const F8QuantArgs a, const bool vec) {
-  __shared__ uint32_t cmax[8][kF8Block];
-  __shared__ __align__(16) uint8_t tr[kF8Block * kF8Pitch];
-  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  const int cg = t & 15, rg = t >> 4;  // its 8 columns and its 8 rows
-  const int64_t r0 = (int64_t)blockIdx.y * kF8Block;
-  const int64_t c0 = (int64_t)blockIdx.x * kF8Block;
-  const int64_t row = r0 + rg * 8, col = c0 + cg * 8;
-  float v[8][8];
+// Packed bf16: the products of both halves; a power of two in both.
+__device__ __forceinline__ uint32_t bf16_mul2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&a),
+                                   *reinterpret_cast<const __nv_bfloat162 *>(&b));
+  return *reinterpret_cast<const uint32_t *>(&p);
+}
+__device__ __forceinline__ uint32_t bf16_both(float v) {
+  return __byte_perm(__float_as_uint(v), 0u, 0x3232);
+}
+
+// N consecutive entries as they lie in memory: bf16 in half the registers, so that
+// more of them can be on their way.
+template <typename T, int N>
+struct F8Raw {
+  static constexpr int words = N * (int)sizeof(T) / 4;
+  uint32_t w[words];
+  // zeros past `left` entries
+  __device__ __forceinline__ void load(const T *p, int64_t left, bool vec) {
+    if (vec && left >= N) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const T *p = static_cast<const T *>(a.x) + (row + i) * a.ldx + col;
-    if (row + i < a.rows && vec && col + 8 <= a.cols) {
-      load_oct(p, v[i]);
+      for (int i = 0; i < words; i += 4) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i / 4);
+        w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+      }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        w[i] = i < left ? __ldg(reinterpret_cast<const unsigned *>(p) + i) : 0u;
+    } else {
+      const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
+#pragma unroll
+      for (int i = 0; i < words; ++i)
+        w[i] = (2 * i < left ? __ldg(h + 2 * i) : 0u) |
+               (uint32_t)(2 * i + 1 < left ? __ldg(h + 2 * i + 1) : 0u) << 16;
+    }
+  }
+  __device__ __forceinline__ float f(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ void set_nan(int i) {
+    if constexpr (sizeof(T) == 4) w[i] = 0x7FFFFFFFu;
+    else w[i / 2] |= i & 1 ? 0x7FFF0000u : 0x7FFFu;
+  }
+  // The largest magnitude (fp32 bits).  Entries that are no numbers become NaN and
+  // count for none.
+  __device__ __forceinline__ uint32_t top(int *status) {
+    uint32_t m = 0u;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        v[i][j] = row + i < a.rows && col + j < a.cols ? (float)p[j] : 0.0f;
+      for (int i = 0; i < words; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+      m = max(m << 16, m & 0xFFFF0000u);
+    }
+    if (m >= 0x7F800000u) {
+      record_status(status, FQT_ENONFINITE);
+      m = 0u;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (isfinite(f(i))) m = max(m, f8_mag(f(i)));
+        else set_nan(i);
+      }
+    }
+    return m;
+  }
+  // Codes of entries 2 i and 2 i + 1, which share a scale.  (A product with a power of
+  // two is exact in bf16 down to 2^-133, far below what E4M3 holds of it.)
+  __device__ __forceinline__ uint32_t pair(int i, float inv) const {
+    if constexpr (sizeof(T) == 4) {
+      return f8_pair(f(2 * i) * inv, f(2 * i + 1) * inv);
+    } else {
+      const uint32_t s = bf16_mul2(w[i], bf16_both(inv));
+      return f8_pair(__uint_as_float(s << 16), __uint_as_float(s & 0xFFFF0000u));
     }
   }
-  uint32_t top = 0u;
+};
+
+// Codes by rows alone, one scale per 128 entries: a warp takes 512 columns of R rows,
+// a lane 16 of each, so that a block's maximum is three shuffles, the codes leave in
+// 16-byte stores and a row's four scales in one word.  Bound by memory traffic.
+template <typename T, int R>
+__global__ void __launch_bounds__(256) k_f8_rows(const F8QuantArgs a, const bool vec) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * R;
+  const int64_t col = (int64_t)blockIdx.y * 512 + lane * 16;
+  F8Raw<T, 16> v[R];
+  uint32_t m[R];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int r = 0; r < R; ++r)
+    v[r].load(static_cast<const T *>(a.x) + (row + r) * a.ldx + col,
+              row + r < a.rows ? a.cols - col : 0, vec);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7FFFFFFFu);
-  // entries that are no numbers count for no scale and take the NaN code
-  const bool bad = top >= 0x7F800000u;
-  if (bad) {
-    record_status(a.status, FQT_ENONFINITE);
+  for (int r = 0; r < R; ++r) m[r] = v[r].top(a.status);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+  for (int o = 4; o > 0; o >>= 1)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (!isfinite(v[i][j])) v[i][j] = __uint_as_float(0x7FFFFFFFu);
+    for (int r = 0; r < R; ++r) m[r] = max(m[r], __shfl_xor_sync(0xffffffffu, m[r], o));
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int e = f8_exponent(m[r]);
+    // the four blocks' bytes, from lanes 0, 8, 16 and 24
+    uint32_t w = (uint32_t)(e + 127) << (lane >> 3) * 8;
+    w |= __shfl_xor_sync(0xffffffffu, w, 8);
+    w |= __shfl_xor_sync(0xffffffffu, w, 16);
+    if (row + r >= a.rows) continue;
+    if (lane == 0) reinterpret_cast<uint32_t *>(a.s)[blockIdx.y * a.sp + row + r] = w;
+    if (col >= a.cols) continue;
+    const float inv = pow2(-e);
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = v[r].pair(2 * i, inv) | v[r].pair(2 * i + 1, inv) << 16;
+    *reinterpret_cast<uint4 *>(a.c + (row + r) * a.pitch + col) =
+        make_uint4(c[0], c[1], c[2], c[3]);
   }
-  auto mag = [&](float x) {
-    const uint32_t m = __float_as_uint(x) & 0x7FFFFFFFu;
-    return m < 0x7F800000u ? m : 0u;
-  };
-  // row maxima: over the 16 threads of a row; column maxima: over the two row groups
-  // of a warp, then over the warps
-  uint32_t rm[8], cm[8];
+}
+
+// Codes along both axes (or blocks of 128 x 128): one CTA per 128 x 128 tile.  A thread
+// holds 4 rows x 8 columns, so it packs codes along either axis without exchanging
+// bytes: 8 bytes of each of its rows go straight to memory, 4 bytes of each of its
+// columns through shared memory.  Bound by memory traffic: the entries are read once
+// for both outputs.
+constexpr int kF8TileThreads = 512;
+
+template <typename T>
+__global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
+    k_f8_tile(const F8QuantArgs a, const bool vec) {
+  __shared__ __align__(16) uint32_t cmax[kF8TileThreads / 32][kF8Block];  // fp32 bits
+  __shared__ __align__(16) float cinv[kF8Block];
+  __shared__ uint32_t wmax[4];
+  // a column's 32 words of 4 rows, word w at place w ^ 2 (column / 8): the threads of a
+  // warp, 16 columns 8 apart x 2 words, write 32 banks
+  __shared__ __align__(16) uint32_t tr[kF8Block * 32];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int cg = t & 15, rg = t >> 4;  // its 8 columns and its 4 rows
+  const int64_t r0 = (int64_t)blockIdx.x * kF8Block;
+  const int64_t c0 = (int64_t)blockIdx.y * kF8Block;
+  const int64_t row = r0 + rg * 4, col = c0 + cg * 8;
+  F8Raw<T, 8> v[4];
+  uint32_t rm[4], cm[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) rm[i] = cm[i] = 0u;
+  for (int i = 0; i < 4; ++i)
+    v[i].load(static_cast<const T *>(a.x) + (row + i) * a.ldx + col,
+              row + i < a.rows ? a.cols - col : 0, vec);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 4; ++i) rm[i] = v[i].top(a.status);
+  // column maxima over the thread's rows (NaN counts for none) and the warp's two row
+  // groups; packed for bf16
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint32_t m = mag(v[i][j]);
-      rm[i] = max(rm[i], m);
-      cm[j] = max(cm[j], m);
+      cm[j] = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t m = f8_mag(v[i].f(j));
+        cm[j] = max(cm[j], m < 0x7F800000u ? m : 0u);
+      }
+      cm[j] = max(cm[j], __shfl_xor_sync(0xffffffffu, cm[j], 16));
     }
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+    for (int j = 0; j < 4; ++j) {
+      uint32_t m = 0u;
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) rm[i] = max(rm[i], __shfl_xor_sync(0xffffffffu, rm[i], o));
+      for (int i = 0; i < 4; ++i) m = __vmaxu2(m, v[i].w[j] & 0x7FFF7FFFu);
+      if (max(m << 16, m & 0xFFFF0000u) >= 0x7F800000u) {
+        m = 0u;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    cm[j] = max(cm[j], __shfl_xor_sync(0xffffffffu, cm[j], 16));
-    if (lane < 16) cmax[warp][cg * 8 + j] = cm[j];
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = v[i].w[j] & 0x7FFF7FFFu;
+          m = __vmaxu2(m, ((x & 0xFFFFu) < 0x7F80u ? x & 0xFFFFu : 0u) |
+                              (x < 0x7F800000u ? x & 0xFFFF0000u : 0u));
+        }
+      }
+      m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 16));
+      cm[2 * j] = m << 16;
+      cm[2 * j + 1] = m & 0xFFFF0000u;
+    }
   }
+  if (lane < 16) {
+    *reinterpret_cast<uint4 *>(&cmax[warp][cg * 8]) = make_uint4(cm[0], cm[1], cm[2], cm[3]);
+    *reinterpret_cast<uint4 *>(&cmax[warp][cg * 8 + 4]) = make_uint4(cm[4], cm[5], cm[6], cm[7]);
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rm[i] = max(rm[i], __shfl_xor_sync(0xffffffffu, rm[i], o));
   __syncthreads();
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-#pragma unroll
-    for (int w = 0; w < 8; ++w) cm[j] = max(cm[j], cmax[w][cg * 8 + j]);
-  if (a.whole) {
+  int e_col = 0;
+  if (t < kF8Block) {
     uint32_t m = 0u;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, cm[j]);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) rm[i] = cm[i] = m;
+    for (int w = 0; w < kF8TileThreads / 32; ++w) m = max(m, cmax[w][t]);
+    if (a.whole) {
+      m = __reduce_max_sync(0xffffffffu, m);
+      if (lane == 0) wmax[warp] = m;
+    } else {
+      e_col = f8_exponent(m);
+      cinv[t] = pow2(-e_col);
+    }
   }
+  __syncthreads();
+  if (a.whole) {
+    const uint32_t m = max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rm[i] = m;
+    e_col = f8_exponent(m);
+  }
+  if (a.ct && t < kF8Block) a.st[scale_at(blockIdx.x, a.spt, c0 + t)] = (uint8_t)(e_col + 127);
   if (a.c) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       const int e = f8_exponent(rm[i]);
-      if (cg == 0) a.s[scale_at(blockIdx.x, a.sp, row + i)] = (uint8_t)(e + 127);
+      if (cg == 0) a.s[scale_at(blockIdx.y, a.sp, row + i)] = (uint8_t)(e + 127);
       if (row + i >= a.rows || col >= a.cols) continue;
       const float inv = pow2(-e);
-      uint32_t w[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        w[h] = f8_pair(v[i][4 * h] * inv, v[i][4 * h + 1] * inv) |
-               f8_pair(v[i][4 * h + 2] * inv, v[i][4 * h + 3] * inv) << 16;
-      *reinterpret_cast<uint2 *>(a.c + (row + i) * a.pitch + col) = make_uint2(w[0], w[1]);
+      *reinterpret_cast<uint2 *>(a.c + (row + i) * a.pitch + col) =
+          make_uint2(v[i].pair(0, inv) | v[i].pair(1, inv) << 16,
+                     v[i].pair(2, inv) | v[i].pair(3, inv) << 16);
     }
   }
   if (a.ct) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = f8_exponent(cm[j]);
-      if (rg == 0) a.st[scale_at(blockIdx.y, a.spt, col + j)] = (uint8_t)(e + 127);
-      const float inv = pow2(-e);
-      uint32_t w[2];
+    for (int j = 0; j < 8; j += 2) {
+      float2 inv = *reinterpret_cast<const float2 *>(&cinv[cg * 8 + j]);
+      if (a.whole) inv.x = inv.y = pow2(-e_col);
+      uint32_t c[2];
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        w[h] = f8_pair(v[4 * h][j] * inv, v[4 * h + 1][j] * inv) |
-               f8_pair(v[4 * h + 2][j] * inv, v[4 * h + 3][j] * inv) << 16;
-      *reinterpret_cast<uint2 *>(tr + (cg * 8 + j) * kF8Pitch + rg * 8) = make_uint2(w[0], w[1]);
+        for (int h = 0; h < 2; ++h) {
+          const float s = h ? inv.y : inv.x;
+          c[h] = f8_pair(v[0].f(j + h) * s, v[1].f(j + h) * s) |
+                 f8_pair(v[2].f(j + h) * s, v[3].f(j + h) * s) << 16;
+        }
+      } else {
+        const uint32_t s =
+            __byte_perm(__float_as_uint(inv.x), __float_as_uint(inv.y), 0x7632);
+        uint32_t p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = bf16_mul2(v[i].w[j / 2], s);
+        c[0] = f8_pair(__uint_as_float(p[0] << 16), __uint_as_float(p[1] << 16)) |
+               f8_pair(__uint_as_float(p[2] << 16), __uint_as_float(p[3] << 16)) << 16;
+        c[1] = f8_pair(__uint_as_float(p[0] & 0xFFFF0000u), __uint_as_float(p[1] & 0xFFFF0000u)) |
+               f8_pair(__uint_as_float(p[2] & 0xFFFF0000u), __uint_as_float(p[3] & 0xFFFF0000u))
+                   << 16;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) tr[(cg * 8 + j + h) * 32 + (rg ^ (2 * cg))] = c[h];
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int at = k * 256 + t, j = at >> 3, ch = at & 7;
-      if (c0 + j < a.cols && r0 + ch * 16 < a.rows)
-        *reinterpret_cast<uint4 *>(a.ct + (c0 + j) * a.pitch_t + r0 + ch * 16) =
-            *reinterpret_cast<const uint4 *>(tr + j * kF8Pitch + ch * 16);
+    for (int k = 0; k < 2; ++k) {
+      const int at = k * kF8TileThreads + t, j = at >> 3, ch = at & 7;
+      if (c0 + j >= a.cols || r0 + ch * 16 >= a.rows) continue;
+      const uint2 *pairs = reinterpret_cast<const uint2 *>(tr + j * 32);
+      const uint2 lo = pairs[(2 * ch) ^ (j >> 3)], hi = pairs[(2 * ch + 1) ^ (j >> 3)];
+      *reinterpret_cast<uint4 *>(a.ct + (c0 + j) * a.pitch_t + r0 + ch * 16) =
+          make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   }
 }
@@ -843,10 +989,24 @@ fqt_status quantize_fp8(const void *X, int64_t ldx, bool bf16, int64_t rows, int
     a.spt = scale_rows(cols);
   }
   const bool vec = f8_aligned(X, 16) && a.ldx * (bf16 ? 2 : 4) % 16 == 0;
-  const dim3 grid((unsigned)((cols + kF8Block - 1) / kF8Block),
-                  (unsigned)((rows + kF8Block - 1) / kF8Block));
-  if (bf16) k_f8_quant<__nv_bfloat16><<<grid, 256, 0, st>>>(a, vec);
-  else k_f8_quant<float><<<grid, 256, 0, st>>>(a, vec);
+  if (!qt && block_rows == 1) {
+    // rows of a warp: 64 entries of a thread on their way, fewer where the rows are few
+    const int64_t chunks = (cols + 511) / 512;
+    const int per = rows * chunks < 32 * device_sm_count() ? 1 : bf16 ? 4 : 2;
+    const dim3 grid((unsigned)((rows + 8 * per - 1) / (8 * per)), (unsigned)chunks);
+    if (bf16) {
+      if (per == 4) k_f8_rows<__nv_bfloat16, 4><<<grid, 256, 0, st>>>(a, vec);
+      else k_f8_rows<__nv_bfloat16, 1><<<grid, 256, 0, st>>>(a, vec);
+    } else {
+      if (per == 2) k_f8_rows<float, 2><<<grid, 256, 0, st>>>(a, vec);
+      else k_f8_rows<float, 1><<<grid, 256, 0, st>>>(a, vec);
+    }
+    return cuda_fail(cudaGetLastError(), "FP8 quantizer launch");
+  }
+  const dim3 grid((unsigned)((rows + kF8Block - 1) / kF8Block),
+                  (unsigned)((cols + kF8Block - 1) / kF8Block));
+  if (bf16) k_f8_tile<__nv_bfloat16><<<grid, kF8TileThreads, 0, st>>>(a, vec);
+  else k_f8_tile<float><<<grid, kF8TileThreads, 0, st>>>(a, vec);
   return cuda_fail(cudaGetLastError(), "FP8 quantizer launch");
 }
 

@@ -140,6 +140,23 @@ def test_blocks_at_the_ends_of_the_range():
     _check_codes(qt, np.ascontiguousarray(x.T).astype(np.float64), 1)
 
 
+def test_bf16_blocks_at_the_ends_of_the_range():
+    """Subnormal, smallest and largest bf16 entries, alone and beside larger ones."""
+    bits = torch.zeros((16, 256), dtype=torch.int16)
+    bits[1, :4] = torch.tensor([1, 3, 0x7F, -32768 + 5], dtype=torch.int16)
+    bits[2, :2] = torch.tensor([0x7F7F, 1], dtype=torch.int16)
+    bits[3, :3] = torch.tensor([0x80, 0x40, 0x81], dtype=torch.int16)
+    bits[4, 128:131] = torch.tensor([0x3F80, 0x0100, 0x3B00], dtype=torch.int16)
+    bits[5, :3] = torch.tensor([0x43E0, 0x43E1, 0x43DF], dtype=torch.int16)
+    X = bits.view(torch.bfloat16)
+    q, qt = fqt.quantize_fp8(X.cuda(), cols=True)
+    only, _ = fqt.quantize_fp8(X.cuda())
+    x = X.double().numpy()
+    _check_codes(q, x, 1)
+    _check_codes(only, x, 1)
+    _check_codes(qt, np.ascontiguousarray(x.T), 1)
+
+
 def test_entries_that_are_not_finite():
     """They take the NaN code, count for no scale, and are reported."""
     X = _matrix(200, 300, "bf16", 1)
@@ -152,6 +169,10 @@ def test_entries_that_are_not_finite():
     codes, scales = _reference(X.double().cpu().numpy(), 1)
     got = q.codes.cpu().numpy()[:, :300]
     at = [(3, 5), (150, 299), (150, 0)]
+    only, _ = fqt.quantize_fp8(bad)
+    assert torch.equal(only.codes[:, :300], q.codes[:, :300])
+    tcodes, tscales = _reference(np.ascontiguousarray(X.double().cpu().numpy().T), 1)
+    assert np.array_equal(_scales(qt), tscales)
     for r, c in at:
         assert got[r, c] & 127 == 127 and qt.codes[c, r].item() & 127 == 127
         got[r, c] = codes[r, c]

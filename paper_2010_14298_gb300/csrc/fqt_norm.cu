@@ -8,15 +8,22 @@
 //   dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
 //
 // Both directions are bound by memory traffic (8 and 14 operations per entry
-// against 4 and 6 bytes of bf16), so a row is read once and kept in registers, as
-// it was read, by a group of threads wide enough to hold it: the group reduces the
-// row's sums, and every thread then finishes the entries it holds.  A group keeps
-// its columns from row to row, so gamma, beta and the partial sums of the column
-// reductions stay in registers too.  The variance is taken about the mean (a second
-// reduction over registers), not from the sum of squares, which loses it where the
-// mean is large.  All statistics and sums are fp32.
+// against 4 and 6 bytes of bf16), so a row is read once and kept in registers by a
+// group of threads wide enough to hold it: the group reduces the row's sums, and every
+// thread then finishes the entries it holds.  A thread holds 16 entries of a row and
+// keeps its columns from row to row: fewer leave the reductions' shuffles and the
+// addresses to too few entries, and with more gamma and beta no longer fit the
+// registers, and reading them again for every row took as many wavefronts of the
+// load/store pipe as the row itself.  Rows are fetched ahead by cp.async: a thread
+// copies the 16 bytes that it will read itself, so rows are on their way without
+// registers and without barriers.  In the backward the columns' sums stay in registers.
+// The variance is taken about the mean (a second reduction over registers), not from
+// the sum of squares, which loses it where the mean is large.  All statistics and sums
+// are fp32.
 #include <cuda_runtime.h>
 #include <math.h>
+
+#include <algorithm>
 
 #include "fqt.h"
 #include "fqt_common.cuh"
@@ -24,9 +31,8 @@
 
 namespace fqt {
 
-constexpr int kNormCtaThreads = 512;  // groups share a CTA up to this many threads
-constexpr int kNormMaxGroups = 8;     // named barriers 1 .. 8
-constexpr int kNormMaxThreads = 1024;
+constexpr int kNormThreads = 512;    // of a CTA at most
+constexpr int kNormMaxGroups = 16;    // of a warp each; 8 wider ones (named barriers 1 .. 8)
 
 struct NormArgs {
   const void *x, *dy;
@@ -56,6 +62,11 @@ struct Pack {
       w[0] = __ldg(reinterpret_cast<const unsigned short *>(p));
     }
   }
+  __device__ __forceinline__ void take(const uint4 &v) {
+    if constexpr (words == 4) {
+      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    }
+  }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < words; ++i) w[i] = 0u;
@@ -67,10 +78,9 @@ struct Pack {
 };
 
 template <typename T, int V>
-__device__ __forceinline__ void store_pack(T *p, const float (&v)[V]) {
-  if constexpr (sizeof(T) == 4) {
-    if constexpr (V == 4) *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else *p = v[0];
+__device__ __forceinline__ void store_pack(T *p, const float *v) {
+  if constexpr (V == 4) {
+    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
   } else if constexpr (V == 8) {
     uint32_t w[4];
 #pragma unroll
@@ -80,321 +90,478 @@ __device__ __forceinline__ void store_pack(T *p, const float (&v)[V]) {
     }
     *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
-    *p = __float2bfloat16_rn(v[0]);
+    *p = (T)v[0];
   }
 }
 
-// Sums of NV values over the threads of a group (G threads from a warp boundary,
-// G a multiple of 32), in every thread, in an order that does not change.  slot:
-// the group's NV x 32 floats of shared memory; a call must not follow another on the
-// same slot without a barrier of the group between the reads and the writes, so
-// callers alternate slots.
-template <int NV>
-__device__ __forceinline__ void group_sum(float (&v)[NV], float *slot, int G, int gid, int gw,
-                                          int lane) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-    for (int k = 0; k < NV; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-  if (G == 32) return;
-  if (lane == 0)
-#pragma unroll
-    for (int k = 0; k < NV; ++k) slot[k * 32 + gw] = v[k];
-  asm volatile("bar.sync %0, %1;" ::"r"(1 + gid), "r"(G) : "memory");
-  const int nw = G >> 5;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    float s = 0.0f;
-    for (int i = 0; i < nw; ++i) s += slot[k * 32 + i];
-    v[k] = s;
-  }
-}
-
-// Forward.  A group takes R rows at a time (two where there are rows enough: twice
-// the loads in flight, and half the barriers per row).
-template <typename T, int V, int VPT, int R>
-__global__ void __launch_bounds__(kNormMaxThreads)
-    k_norm_fwd(const NormArgs a, int G) {
-  __shared__ float slots[kNormMaxGroups][2][R * 32];
-  const int gid = threadIdx.x / G, t = threadIdx.x - gid * G;
-  const int lane = t & 31, gw = t >> 5, ngrp = blockDim.x / G;
-  const int nvec = a.cols / V;
-  const float n = (float)a.cols;
-  float ga[VPT * V], be[VPT * V];
+// This thread's entries of a vector of `cols` floats: V from every column (j G + t) V
+// on; `none` where the vector or the column is missing.
+template <int V, int VPT>
+__device__ __forceinline__ void load_columns(const float *p, int cols, int G, int t, float none,
+                                             float (&v)[V * VPT]) {
 #pragma unroll
   for (int j = 0; j < VPT; ++j)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int c = (j * G + t) * V + i;
-      ga[j * V + i] = a.gamma && c < a.cols ? __ldg(a.gamma + c) : 1.0f;
-      be[j * V + i] = a.beta && c < a.cols ? __ldg(a.beta + c) : 0.0f;
+      v[j * V + i] = p && c < cols ? __ldg(p + c) : none;
     }
+}
+
+// Sums of a value (two values) over the threads of a group (G threads from a warp
+// boundary, G a multiple of 32, at most 16 warps), in every thread, in an order that
+// does not change.  slot: 32 floats of the group; a call must not follow another on the
+// same slot without a barrier of the group between the reads and the writes, so callers
+// alternate slots.
+__device__ __forceinline__ float group_sum(float v, float *slot, int G, int gid, int gw,
+                                           int lane) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (G == 32) return v;
+  if (lane == 0) slot[gw] = v;
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + gid), "r"(G) : "memory");
+  // every warp adds the warps' sums by itself
+  v = lane < (G >> 5) ? slot[lane] : 0.0f;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return __shfl_sync(0xffffffffu, v, 0);
+}
+
+// (The first value is summed in the lower half of the lanes, the second in the upper.)
+__device__ __forceinline__ float2 group_sum2(float a, float b, float *slot, int G, int gid,
+                                             int gw, int lane) {
+  const bool up = lane & 16;
+  float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (G > 32) {
+    if ((lane & 15) == 0) slot[(lane & 16) + gw] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + gid), "r"(G) : "memory");
+    v = (lane & 15) < (G >> 5) ? slot[lane] : 0.0f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
+}
+
+template <int R>
+__device__ __forceinline__ void group_sums(float (&s)[R], float *slot, int G, int gid, int gw,
+                                           int lane) {
+  static_assert(R == 1 || R == 2, "one or two sums");
+  if constexpr (R == 1) {
+    s[0] = group_sum(s[0], slot, G, gid, gw, lane);
+  } else {
+    const float2 v = group_sum2(s[0], s[1], slot, G, gid, gw, lane);
+    s[0] = v.x;
+    s[1] = v.y;
+  }
+}
+
+// 16 bytes of this thread on their way to its place in shared memory.
+__device__ __forceinline__ void copy16(void *dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src)
+               : "memory");
+}
+__device__ __forceinline__ void copy_commit() {
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void copy_wait() {  // all but the last N groups are there
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Threads' 16-byte places in S stages of shared memory, `N` places of a row (or of
+// two rows, X's and dY's) a stage.
+template <int N>
+struct NormRing {
+  uint4 *base;
+  __device__ __forceinline__ uint4 *at(int stage, int i) const {
+    return base + (stage * N + i) * blockDim.x + threadIdx.x;
+  }
+};
+
+// Forward.  S > 0: rows come through S stages of shared memory.  A group takes R rows
+// at a time: their sums share shuffles and barriers.
+template <typename T, int V, int VPT, int R, int S>
+__global__ void __launch_bounds__(kNormThreads)
+    k_norm_fwd(const NormArgs a, int G) {
+  extern __shared__ __align__(16) uint4 smem[];
+  __shared__ float slots[kNormMaxGroups][2][32];
+  constexpr int E = V * VPT;
+  const int gid = threadIdx.x / G, t = threadIdx.x - gid * G;
+  const int lane = t & 31, gw = t >> 5, ngrp = blockDim.x / G;
+  const int nvec = a.cols / V;
+  const float n = (float)a.cols;
+  const NormRing<R * VPT> ring{smem};
   const int64_t step = (int64_t)gridDim.x * ngrp * R;
-  for (int64_t r0 = ((int64_t)blockIdx.x * ngrp + gid) * R; r0 < a.rows; r0 += step) {
-    Pack<T, V> x[R][VPT];
+  const T *px = static_cast<const T *>(a.x) + (int64_t)t * V;
+  auto fetch = [&](int stage, int64_t r0) {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      if (r0 + k < a.rows)
+#pragma unroll
+        for (int j = 0; j < VPT; ++j)
+          if (j * G + t < nvec)
+            copy16(ring.at(stage, k * VPT + j), px + (r0 + k) * a.ldx + (int64_t)j * G * V);
+    copy_commit();
+  };
+  int64_t r0 = ((int64_t)blockIdx.x * ngrp + gid) * R;
+  if constexpr (S > 0)
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) fetch(i, r0 + i * step);
+  float ga[E], be[E];
+  load_columns<V, VPT>(a.gamma, a.cols, G, t, 1.0f, ga);
+  load_columns<V, VPT>(a.beta, a.cols, G, t, 0.0f, be);
+  int stage = 0;
+  for (; r0 < a.rows; r0 += step) {
+    float d[R][E], mean[R];
+    if constexpr (S > 0) {
+      fetch(stage == 0 ? S - 1 : stage - 1, r0 + (S - 1) * step);
+      copy_wait<S - 1>();
+    }
     float s[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      s[r] = 0.0f;
+    for (int k = 0; k < R; ++k) {
+      Pack<T, V> x[VPT];
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
-        const int v = j * G + t;
-        if (r0 + r < a.rows && v < nvec)
-          x[r][j].load(static_cast<const T *>(a.x) + (r0 + r) * a.ldx + (int64_t)v * V);
-        else
-          x[r][j].zero();
+        if (r0 + k >= a.rows || j * G + t >= nvec) x[j].zero();
+        else if constexpr (S > 0) x[j].take(*ring.at(stage, k * VPT + j));
+        else x[j].load(px + (r0 + k) * a.ldx + (int64_t)j * G * V);
+      }
+      s[k] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        d[k][i] = x[i / V].f(i % V);
+        s[k] += d[k][i];
       }
     }
+    if constexpr (S > 0) stage = stage == S - 1 ? 0 : stage + 1;
+    group_sums<R>(s, slots[gid][0], G, gid, gw, lane);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int k = 0; k < R; ++k) {
+      mean[k] = s[k] / n;
+      s[k] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < VPT; ++j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[r] += x[r][j].f(i);
-    group_sum<R>(s, slots[gid][0], G, gid, gw, lane);
-    float mean[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      mean[r] = s[r] / n;
-      s[r] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j)
-        if (j * G + t < nvec)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float d = x[r][j].f(i) - mean[r];
-            s[r] = fmaf(d, d, s[r]);
-          }
+      for (int i = 0; i < E; ++i) {
+        d[k][i] -= mean[k];
+        if ((i / V) * G + t < nvec) s[k] = fmaf(d[k][i], d[k][i], s[k]);
+      }
     }
-    group_sum<R>(s, slots[gid][1], G, gid, gw, lane);
+    group_sums<R>(s, slots[gid][1], G, gid, gw, lane);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (r0 + r >= a.rows) break;
-      const float rstd = 1.0f / sqrtf(s[r] / n + a.eps);
+    for (int k = 0; k < R; ++k) {
+      const float rstd = 1.0f / sqrtf(s[k] / n + a.eps);
+      if (r0 + k >= a.rows) break;
       if (t == 0) {
-        if (a.mean) a.mean[r0 + r] = mean[r];
-        if (a.rstd) a.rstd[r0 + r] = rstd;
+        if (a.mean) a.mean[r0 + k] = mean[k];
+        if (a.rstd) a.rstd[r0 + k] = rstd;
       }
+      T *py = static_cast<T *>(a.y) + (r0 + k) * a.ldy + (int64_t)t * V;
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
-        const int v = j * G + t;
-        if (v >= nvec) continue;
+        if (j * G + t >= nvec) break;
         float y[V];
 #pragma unroll
         for (int i = 0; i < V; ++i)
-          y[i] = fmaf((x[r][j].f(i) - mean[r]) * rstd, ga[j * V + i], be[j * V + i]);
-        store_pack<T, V>(static_cast<T *>(a.y) + (r0 + r) * a.ldy + (int64_t)v * V, y);
+          y[i] = fmaf(d[k][j * V + i] * rstd, ga[j * V + i], be[j * V + i]);
+        store_pack<T, V>(py + (int64_t)j * G * V, y);
       }
     }
   }
 }
 
-// Backward.  The column sums of a group's rows stay in its registers; at the end
-// the groups of a CTA are added in shared memory, and each CTA writes one row of
-// partial sums (k_norm_cols adds those).
-template <typename T, int V, int VPT, int R>
-__global__ void __launch_bounds__(kNormMaxThreads)
+// Backward.  The column sums of a group's rows stay in its registers; at the end the
+// groups of a CTA add theirs in shared memory, and each CTA writes one row of partial
+// sums (k_norm_cols adds those).
+template <typename T, int V, int VPT, int S>
+__global__ void __launch_bounds__(kNormThreads)
     k_norm_bwd(const NormArgs a, int G) {
-  extern __shared__ float colsum[];  // 2 x cols, where the CTA has several groups
-  __shared__ float slots[kNormMaxGroups][2][2 * R * 32];
+  extern __shared__ __align__(16) uint4 smem[];
+  __shared__ float slots[kNormMaxGroups][2][32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  constexpr int E = V * VPT;
   const int gid = threadIdx.x / G, t = threadIdx.x - gid * G;
   const int lane = t & 31, gw = t >> 5, ngrp = blockDim.x / G;
   const int nvec = a.cols / V;
   const float n = (float)a.cols;
-  float ga[VPT * V], dg[VPT * V], db[VPT * V];
+  const NormRing<2 * VPT> ring{smem};
+  const int64_t step = (int64_t)gridDim.x * ngrp;
+  const T *px = static_cast<const T *>(a.x) + (int64_t)t * V;
+  const T *pdy = static_cast<const T *>(a.dy) + (int64_t)t * V;
+  auto fetch = [&](int stage, int64_t r) {
+    if (r < a.rows)
 #pragma unroll
-  for (int j = 0; j < VPT; ++j)
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = (j * G + t) * V + i;
-      ga[j * V + i] = a.gamma && c < a.cols ? __ldg(a.gamma + c) : 1.0f;
-      dg[j * V + i] = db[j * V + i] = 0.0f;
-    }
-  const int64_t step = (int64_t)gridDim.x * ngrp * R;
-  int slot = 0;
-  for (int64_t r0 = ((int64_t)blockIdx.x * ngrp + gid) * R; r0 < a.rows; r0 += step, slot ^= 1) {
-    Pack<T, V> x[R][VPT], dy[R][VPT];
-    float mean[R], rstd[R], s[2 * R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const bool in = r0 + r < a.rows;
-      mean[r] = in ? __ldg(a.mean + r0 + r) : 0.0f;
-      rstd[r] = in ? __ldg(a.rstd + r0 + r) : 0.0f;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int v = j * G + t;
-        if (in && v < nvec) {
-          x[r][j].load(static_cast<const T *>(a.x) + (r0 + r) * a.ldx + (int64_t)v * V);
-          dy[r][j].load(static_cast<const T *>(a.dy) + (r0 + r) * a.lddy + (int64_t)v * V);
-        } else {
-          x[r][j].zero();
-          dy[r][j].zero();
+      for (int j = 0; j < VPT; ++j)
+        if (j * G + t < nvec) {
+          copy16(ring.at(stage, 2 * j), px + r * a.ldx + (int64_t)j * G * V);
+          copy16(ring.at(stage, 2 * j + 1), pdy + r * a.lddy + (int64_t)j * G * V);
         }
+    copy_commit();
+  };
+  int64_t r = (int64_t)blockIdx.x * ngrp + gid;
+  if constexpr (S > 0)
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) fetch(i, r + i * step);
+  float ga[E], dg[E], db[E];
+  load_columns<V, VPT>(a.gamma, a.cols, G, t, 1.0f, ga);
+#pragma unroll
+  for (int i = 0; i < E; ++i) dg[i] = db[i] = 0.0f;
+  // a row's statistics, one step ahead
+  float mean_next = 0.0f, rstd_next = 0.0f;
+  if (r < a.rows) {
+    mean_next = __ldg(a.mean + r);
+    rstd_next = __ldg(a.rstd + r);
+  }
+  int slot = 0, stage = 0;
+  for (; r < a.rows; r += step, slot ^= 1) {
+    Pack<T, V> x[VPT], dy[VPT];
+    const float mean = mean_next, rstd = rstd_next;
+    if constexpr (S > 0) {
+      fetch(stage == 0 ? S - 1 : stage - 1, r + (S - 1) * step);
+      copy_wait<S - 1>();
+    }
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      if (j * G + t >= nvec) {
+        x[j].zero();
+        dy[j].zero();
+      } else if constexpr (S > 0) {
+        x[j].take(*ring.at(stage, 2 * j));
+        dy[j].take(*ring.at(stage, 2 * j + 1));
+      } else {
+        x[j].load(px + r * a.ldx + (int64_t)j * G * V);
+        dy[j].load(pdy + r * a.lddy + (int64_t)j * G * V);
       }
     }
+    if constexpr (S > 0) stage = stage == S - 1 ? 0 : stage + 1;
+    if (r + step < a.rows) {
+      mean_next = __ldg(a.mean + r + step);
+      rstd_next = __ldg(a.rstd + r + step);
+    }
+    // u = x - mean and g = dy gamma are kept for dx; a missing entry's dy is 0
+    float u[E], g[E], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      s[2 * r] = s[2 * r + 1] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        if (r0 + r >= a.rows || j * G + t >= nvec) continue;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float xh = (x[r][j].f(i) - mean[r]) * rstd[r], d = dy[r][j].f(i);
-          const float g = d * ga[j * V + i];
-          s[2 * r] += g;
-          s[2 * r + 1] = fmaf(g, xh, s[2 * r + 1]);
-          dg[j * V + i] = fmaf(d, xh, dg[j * V + i]);
-          db[j * V + i] += d;
-        }
-      }
+    for (int i = 0; i < E; ++i) {
+      const float e = dy[i / V].f(i % V);
+      u[i] = x[i / V].f(i % V) - mean;
+      g[i] = e * ga[i];
+      s1 += g[i];
+      s2 = fmaf(g[i], u[i], s2);
+      dg[i] = fmaf(e * rstd, u[i], dg[i]);
+      db[i] += e;
     }
     if (!a.y) continue;
-    group_sum<2 * R>(s, slots[gid][slot], G, gid, gw, lane);
+    const float2 s = group_sum2(s1, s2, slots[gid][slot], G, gid, gw, lane);
+    // dx = rstd g - rstd sum(g) / n - (x - mean) rstd^3 sum(g (x - mean)) / n
+    const float k0 = -rstd * (s.x / n), k1 = -rstd * (rstd * (rstd * (s.y / n)));
+    T *pdx = static_cast<T *>(a.y) + r * a.ldy + (int64_t)t * V;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (r0 + r >= a.rows) break;
-      const float m1 = s[2 * r] / n, m2 = s[2 * r + 1] / n;
+    for (int j = 0; j < VPT; ++j) {
+      if (j * G + t >= nvec) break;
+      float o[V];
 #pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        const int v = j * G + t;
-        if (v >= nvec) continue;
-        float o[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float xh = (x[r][j].f(i) - mean[r]) * rstd[r];
-          const float g = dy[r][j].f(i) * ga[j * V + i];
-          o[i] = rstd[r] * (g - m1 - xh * m2);
-        }
-        store_pack<T, V>(static_cast<T *>(a.y) + (r0 + r) * a.ldy + (int64_t)v * V, o);
-      }
+      for (int i = 0; i < V; ++i)
+        o[i] = fmaf(u[j * V + i], k1, fmaf(g[j * V + i], rstd, k0));
+      store_pack<T, V>(pdx + (int64_t)j * G * V, o);
     }
   }
   if (!a.part) return;
+  // every thread's sums in shared memory, entry i of thread t of a group at i G + t;
+  // then the groups' sums, from the first to the last
+  float *sums = reinterpret_cast<float *>(smem);
+  const int per = E * G;  // sums of a group: dgamma's, then dbeta's
   float *dst = a.part + (int64_t)blockIdx.x * 2 * a.cols;
-  for (int q = ngrp - 1; q >= 0; --q) {  // groups add up from the last to the first
-    if (gid == q)
+  if (ngrp > 1 && S > 0) {
+    copy_wait<0>();
+    __syncthreads();
+  }
 #pragma unroll
-      for (int j = 0; j < VPT; ++j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int c = (j * G + t) * V + i;
-          if (c >= a.cols) continue;
-          float u = dg[j * V + i], w = db[j * V + i];
-          if (q < ngrp - 1) {
-            u += colsum[c];
-            w += colsum[a.cols + c];
-          }
-          if (q > 0) {
-            colsum[c] = u;
-            colsum[a.cols + c] = w;
-          } else {
-            dst[c] = u;
-            dst[a.cols + c] = w;
-          }
-        }
-    if (q > 0) __syncthreads();
+  for (int i = 0; i < E; ++i) {
+    const int c = ((i / V) * G + t) * V + i % V;
+    if (ngrp > 1) {
+      sums[(2 * gid) * per + i * G + t] = dg[i];
+      sums[(2 * gid + 1) * per + i * G + t] = db[i];
+    } else if (c < a.cols) {
+      dst[c] = dg[i];
+      dst[a.cols + c] = db[i];
+    }
+  }
+  if (ngrp == 1) return;
+  __syncthreads();
+  for (int k = threadIdx.x; k < per; k += blockDim.x) {
+    const int i = k / G, v = k - i * G, c = ((i / V) * G + v) * V + i % V;
+    if (c >= a.cols) continue;
+    float p = 0.0f, q = 0.0f;
+    for (int j = 0; j < ngrp; ++j) {
+      p += sums[(2 * j) * per + k];
+      q += sums[(2 * j + 1) * per + k];
+    }
+    dst[c] = p;
+    dst[a.cols + c] = q;
   }
 }
 
-// Rows wider than a CTA's registers: three reads of X in the forward ...
-template <typename T>
-__global__ void __launch_bounds__(kNormMaxThreads)
+// Rows wider than a CTA's registers, one CTA a row: X is read three times in the
+// forward (the second and third time from L1 or L2) ...
+template <typename T, int V>
+__global__ void __launch_bounds__(kNormThreads)
     k_norm_fwd_wide(const NormArgs a) {
   __shared__ float slots[2][32];
   const int t = threadIdx.x, lane = t & 31, gw = t >> 5;
+  const int nvec = a.cols / V;
   const float n = (float)a.cols;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const T *x = static_cast<const T *>(a.x) + r * a.ldx;
-    T *y = static_cast<T *>(a.y) + r * a.ldy;
-    float s[1] = {0.0f};
-    for (int c = t; c < a.cols; c += blockDim.x) s[0] += (float)x[c];
-    group_sum<1>(s, slots[0], blockDim.x, 0, gw, lane);
-    const float mean = s[0] / n;
-    s[0] = 0.0f;
-    for (int c = t; c < a.cols; c += blockDim.x) {
-      const float d = (float)x[c] - mean;
-      s[0] = fmaf(d, d, s[0]);
+    const T *px = static_cast<const T *>(a.x) + r * a.ldx;
+    T *py = static_cast<T *>(a.y) + r * a.ldy;
+    Pack<T, V> x;
+    float s = 0.0f;
+#pragma unroll 4
+    for (int v = t; v < nvec; v += kNormThreads) {
+      x.load(px + (int64_t)v * V);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s += x.f(i);
     }
-    group_sum<1>(s, slots[1], blockDim.x, 0, gw, lane);
-    const float rstd = 1.0f / sqrtf(s[0] / n + a.eps);
+    const float mean = group_sum(s, slots[0], kNormThreads, 0, gw, lane) / n;
+    s = 0.0f;
+#pragma unroll 4
+    for (int v = t; v < nvec; v += kNormThreads) {
+      x.load(px + (int64_t)v * V);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = x.f(i) - mean;
+        s = fmaf(d, d, s);
+      }
+    }
+    const float var = group_sum(s, slots[1], kNormThreads, 0, gw, lane) / n;
+    const float rstd = 1.0f / sqrtf(var + a.eps);
     if (t == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
     }
-    for (int c = t; c < a.cols; c += blockDim.x) {
-      const float g = a.gamma ? __ldg(a.gamma + c) : 1.0f, b = a.beta ? __ldg(a.beta + c) : 0.0f;
-      y[c] = (T)fmaf(((float)x[c] - mean) * rstd, g, b);
+#pragma unroll 2
+    for (int v = t; v < nvec; v += kNormThreads) {
+      x.load(px + (int64_t)v * V);
+      float ga[V], be[V], y[V];
+      load_columns<V, 1>(a.gamma, a.cols, 0, v, 1.0f, ga);
+      load_columns<V, 1>(a.beta, a.cols, 0, v, 0.0f, be);
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[i] = fmaf((x.f(i) - mean) * rstd, ga[i], be[i]);
+      store_pack<T, V>(py + (int64_t)v * V, y);
     }
   }
 }
 
-// ... and, in the backward, dX by rows and the column sums by columns.
-template <typename T>
-__global__ void __launch_bounds__(kNormMaxThreads)
+// ... and, in the backward, X and dY twice for dX by rows, and once for the column sums
+// by columns.
+template <typename T, int V>
+__global__ void __launch_bounds__(kNormThreads)
     k_norm_bwd_wide(const NormArgs a) {
-  __shared__ float slots[2][64];
+  __shared__ float slots[2][32];
   const int t = threadIdx.x, lane = t & 31, gw = t >> 5;
+  const int nvec = a.cols / V;
   const float n = (float)a.cols;
   int slot = 0;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, slot ^= 1) {
-    const T *x = static_cast<const T *>(a.x) + r * a.ldx;
-    const T *dy = static_cast<const T *>(a.dy) + r * a.lddy;
-    T *dx = static_cast<T *>(a.y) + r * a.ldy;
+    const T *px = static_cast<const T *>(a.x) + r * a.ldx;
+    const T *pdy = static_cast<const T *>(a.dy) + r * a.lddy;
+    T *pdx = static_cast<T *>(a.y) + r * a.ldy;
     const float mean = a.mean[r], rstd = a.rstd[r];
-    float s[2] = {0.0f, 0.0f};
-    for (int c = t; c < a.cols; c += blockDim.x) {
-      const float g = (float)dy[c] * (a.gamma ? __ldg(a.gamma + c) : 1.0f);
-      s[0] += g;
-      s[1] = fmaf(g, ((float)x[c] - mean) * rstd, s[1]);
+    Pack<T, V> x, dy;
+    float ga[V], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll 2
+    for (int v = t; v < nvec; v += kNormThreads) {
+      x.load(px + (int64_t)v * V);
+      dy.load(pdy + (int64_t)v * V);
+      load_columns<V, 1>(a.gamma, a.cols, 0, v, 1.0f, ga);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float g = dy.f(i) * ga[i];
+        s1 += g;
+        s2 = fmaf(g, x.f(i) - mean, s2);
+      }
     }
-    group_sum<2>(s, slots[slot], blockDim.x, 0, gw, lane);
-    const float m1 = s[0] / n, m2 = s[1] / n;
-    for (int c = t; c < a.cols; c += blockDim.x) {
-      const float g = (float)dy[c] * (a.gamma ? __ldg(a.gamma + c) : 1.0f);
-      const float xh = ((float)x[c] - mean) * rstd;
-      dx[c] = (T)(rstd * (g - m1 - xh * m2));
+    const float2 s = group_sum2(s1, s2, slots[slot], kNormThreads, 0, gw, lane);
+    const float k0 = -rstd * (s.x / n), k1 = -rstd * (rstd * (rstd * (s.y / n)));
+#pragma unroll 2
+    for (int v = t; v < nvec; v += kNormThreads) {
+      x.load(px + (int64_t)v * V);
+      dy.load(pdy + (int64_t)v * V);
+      load_columns<V, 1>(a.gamma, a.cols, 0, v, 1.0f, ga);
+      float o[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        o[i] = fmaf(x.f(i) - mean, k1, fmaf(dy.f(i) * ga[i], rstd, k0));
+      store_pack<T, V>(pdx + (int64_t)v * V, o);
     }
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_norm_cols_wide(const NormArgs a, int64_t rows_per) {
-  const int c = blockIdx.x * blockDim.x + threadIdx.x;
-  if (c >= a.cols) return;
+constexpr int kNormColRows = 32;  // partial rows of the wide columns' sums
+
+template <typename T, int V>
+__global__ void __launch_bounds__(128) k_norm_cols_wide(const NormArgs a, int64_t rows_per) {
+  const int v = blockIdx.x * blockDim.x + threadIdx.x;
+  if (v >= a.cols / V) return;
   const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = min(a.rows, r0 + rows_per);
-  float dg = 0.0f, db = 0.0f;
+  const T *px = static_cast<const T *>(a.x) + (int64_t)v * V;
+  const T *pdy = static_cast<const T *>(a.dy) + (int64_t)v * V;
+  float dg[V] = {}, db[V] = {};
+#pragma unroll 4
   for (int64_t r = r0; r < r1; ++r) {
-    const float d = (float)static_cast<const T *>(a.dy)[r * a.lddy + c];
-    const float x = (float)static_cast<const T *>(a.x)[r * a.ldx + c];
-    dg = fmaf(d, (x - a.mean[r]) * a.rstd[r], dg);
-    db += d;
+    Pack<T, V> x, dy;
+    x.load(px + r * a.ldx);
+    dy.load(pdy + r * a.lddy);
+    const float mean = __ldg(a.mean + r), rstd = __ldg(a.rstd + r);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      dg[i] = fmaf(dy.f(i) * rstd, x.f(i) - mean, dg[i]);
+      db[i] += dy.f(i);
+    }
   }
-  float *dst = a.part + (int64_t)blockIdx.y * 2 * a.cols;
-  dst[c] = dg;
-  dst[a.cols + c] = db;
+  float *dst = a.part + (int64_t)blockIdx.y * 2 * a.cols + (int64_t)v * V;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    dst[i] = dg[i];
+    dst[a.cols + i] = db[i];
+  }
 }
 
-// dgamma and dbeta: the sums of n partial rows, 32 columns a CTA, warp w taking
-// rows w, w + 8, ...
-__global__ void __launch_bounds__(256)
+// dgamma and dbeta: the sums of n partial rows, 8 columns a CTA, 64 rows side by side
+// (so that a few loads a thread and many CTAs finish soon).  It is launched while the
+// partial sums are still being made and waits for them.
+constexpr int kNormColThreads = 512;
+
+__global__ void __launch_bounds__(kNormColThreads)
     k_norm_cols(const float *part, int n, int cols, float *dgamma, float *dbeta) {
-  __shared__ float sums[2][8][33];
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  __shared__ float sums[2][kNormColThreads / 32][8];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 8 + (lane & 7);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   float u = 0.0f, v = 0.0f;
-  if (c < cols)
-    for (int i = w; i < n; i += 8) {
-      u += part[(int64_t)i * 2 * cols + c];
-      v += part[(int64_t)i * 2 * cols + cols + c];
+  if (c < cols) {
+#pragma unroll 4
+    for (int i = threadIdx.x >> 3; i < n; i += kNormColThreads / 8) {
+      u += __ldcg(part + (int64_t)i * 2 * cols + c);
+      v += __ldcg(part + (int64_t)i * 2 * cols + cols + c);
     }
-  sums[0][w][lane] = u;
-  sums[1][w][lane] = v;
+  }
+#pragma unroll
+  for (int o = 16; o > 4; o >>= 1) {
+    u += __shfl_xor_sync(0xffffffffu, u, o);
+    v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  if (lane < 8) {
+    sums[0][w][lane] = u;
+    sums[1][w][lane] = v;
+  }
   __syncthreads();
-  if (w < 2 && c < cols) {
+  if (threadIdx.x < 16 && c < cols) {
+    const int which = threadIdx.x >> 3;
     float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += sums[w][i][lane];
-    float *out = w ? dbeta : dgamma;
+    for (int i = 0; i < kNormColThreads / 32; ++i) s += sums[which][i][lane & 7];
+    float *out = which ? dbeta : dgamma;
     if (out) out[c] = s;
   }
 }
@@ -404,47 +571,47 @@ __global__ void __launch_bounds__(256)
 // ---------------------------------------------------------------------------
 // Threads per row, groups per CTA and CTAs of the kernels that hold a row.
 struct NormPlan {
-  bool wide;  // rows wider than a CTA's registers
-  int v, vpt, G, groups, grid;
-  bool two;   // two rows at a time
+  bool wide;   // rows wider than a CTA's registers
+  bool ahead;  // rows fetched ahead through shared memory
+  bool thin;   // 16 bytes a thread: few rows, where their latency counts
+  int v, G, groups, grid;
 };
 
-static NormPlan norm_plan(int64_t rows, int64_t cols, bool bf16, bool vec, int nsm) {
+constexpr int kNormEntries = 16;  // of a row, a thread
+
+static NormPlan norm_plan(int64_t rows, int64_t cols, bool bf16, bool vec, bool bwd, int nsm) {
   NormPlan p = {};
-  const int vmax = bf16 ? 8 : 4;
-  p.v = vec ? vmax : 1;
+  p.v = vec ? (bf16 ? 8 : 4) : 1;
   const int64_t nvec = cols / p.v;
-  // entries per thread: 16 bytes, or 4 single entries; twice that where a CTA's
-  // threads do not cover the row
-  p.vpt = vec ? 1 : 4;
-  if (nvec > (int64_t)p.vpt * kNormMaxThreads) p.vpt *= 2;
-  p.wide = nvec > (int64_t)p.vpt * kNormMaxThreads;
+  p.thin = vec && rows <= nsm && nvec <= kNormThreads;
+  const int vpt = p.thin ? 1 : kNormEntries / p.v;
+  p.wide = nvec > (int64_t)vpt * kNormThreads;
   if (p.wide) {
-    p.G = kNormMaxThreads;
+    p.G = kNormThreads;
     p.groups = 1;
-    p.grid = (int)(rows < 2 * nsm ? rows : 2 * nsm);
+    p.grid = (int)(rows < 4 * nsm ? rows : 4 * nsm);
     return p;
   }
-  const int64_t need = (nvec + p.vpt - 1) / p.vpt;
+  const int64_t need = (nvec + vpt - 1) / vpt;
   p.G = (int)((need + 31) / 32 * 32);
-  p.groups = kNormCtaThreads / p.G;
-  if (p.groups < 1) p.groups = 1;
-  if (p.groups > kNormMaxGroups) p.groups = kNormMaxGroups;
-  // 64 registers a thread: 1024 threads an SM
-  const int per_sm = kNormMaxThreads / (p.G * p.groups);
-  const int64_t slots = (int64_t)nsm * per_sm * p.groups;
-  p.two = rows >= 2 * slots && p.vpt == (vec ? 1 : 4);
-  // few rows: one group a CTA, so that they spread over the SMs
-  if (rows <= nsm) p.groups = 1;
-  const int64_t each = (int64_t)p.groups * (p.two ? 2 : 1);
+  p.groups = kNormThreads / p.G;
+  if (p.G > 32 && p.groups > 8) p.groups = 8;  // their named barriers
+  const int64_t slots = (int64_t)nsm * p.groups;
+  // rows fetched ahead where there is a next one; few rows go to SMs of their own
+  p.ahead = vec && rows > slots;
+  if (!p.ahead) {
+    const int64_t each = (rows + nsm - 1) / nsm;
+    if (each < p.groups) p.groups = (int)each;
+  }
+  // (the forward takes two rows at a time where it fetches ahead)
+  const int64_t each = p.groups * (p.ahead && !bwd ? 2 : 1);
   const int64_t want = (rows + each - 1) / each;
-  p.grid = (int)(want < nsm * per_sm ? want : nsm * per_sm);
+  p.grid = (int)(want < nsm ? want : nsm);
   return p;
 }
 
-// The most partial rows of column sums that any plan writes (CTAs of 8 groups of
-// a warp: four an SM).
-static int norm_parts(int nsm) { return kNormMaxThreads / (32 * kNormMaxGroups) * nsm; }
+// The most partial rows of column sums that any plan writes: a CTA each.
+static int norm_parts(int nsm) { return nsm > kNormColRows ? nsm : kNormColRows; }
 
 size_t layer_norm_ws_bytes(int64_t rows, int64_t cols) {
   (void)rows;
@@ -452,21 +619,63 @@ size_t layer_norm_ws_bytes(int64_t rows, int64_t cols) {
   return kHeaderBytes + (size_t)norm_parts(device_sm_count()) * 2 * (size_t)cols * sizeof(float);
 }
 
-template <typename T, int V, int VPT, int R>
-static void launch_rows(const NormArgs &a, const NormPlan &p, bool bwd, cudaStream_t st) {
+template <typename T, bool BWD, int V, int VPT, int S>
+static cudaError_t launch_rows(const NormArgs &a, const NormPlan &p, cudaStream_t st) {
   const int nth = p.G * p.groups;
-  // several groups only where G <= 256: at most 2 x 2048 columns, 16 KB
-  const size_t smem = p.groups > 1 && a.part ? 2 * sizeof(float) * a.cols : 0;
-  if (bwd) k_norm_bwd<T, V, VPT, R><<<p.grid, nth, smem, st>>>(a, p.G);
-  else k_norm_fwd<T, V, VPT, R><<<p.grid, nth, 0, st>>>(a, p.G);
+  constexpr int R = !BWD && S > 0 ? 2 : 1;
+  size_t smem = (size_t)S * VPT * (BWD ? 2 : R) * 16 * nth;  // the rows on their way
+  const size_t sums = BWD && p.groups > 1 && a.part ? 2 * sizeof(float) * VPT * V * nth : 0;
+  smem = std::max(smem, sums);
+  void (*kernel)(NormArgs, int);
+  if constexpr (BWD) kernel = k_norm_bwd<T, V, VPT, S>;
+  else kernel = k_norm_fwd<T, V, VPT, R, S>;
+  if (smem > 40 * 1024) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<p.grid, nth, smem, st>>>(a, p.G);
+  return cudaGetLastError();
+}
+
+template <typename T, bool BWD, int V>
+static cudaError_t launch_held(const NormArgs &a, const NormPlan &p, cudaStream_t st) {
+  constexpr int VPT = kNormEntries / V;
+  // stages: 128 KB of rows in bf16 (four) and 192 KB in fp32 (three)
+  if constexpr (V == 1) return launch_rows<T, BWD, 1, VPT, 0>(a, p, st);
+  else if (p.thin) return launch_rows<T, BWD, V, 1, 0>(a, p, st);
+  else if (p.ahead) return launch_rows<T, BWD, V, VPT, V == 8 ? 4 : 3>(a, p, st);
+  else return launch_rows<T, BWD, V, VPT, 0>(a, p, st);
+}
+
+template <bool BWD>
+static cudaError_t launch_norm(const NormArgs &a, const NormPlan &p, bool bf16, cudaStream_t st) {
+  if (bf16)
+    return p.v > 1 ? launch_held<__nv_bfloat16, BWD, 8>(a, p, st)
+                   : launch_held<__nv_bfloat16, BWD, 1>(a, p, st);
+  return p.v > 1 ? launch_held<float, BWD, 4>(a, p, st) : launch_held<float, BWD, 1>(a, p, st);
 }
 
 template <typename T, int V>
-static void launch_held(const NormArgs &a, const NormPlan &p, bool bwd, cudaStream_t st) {
-  constexpr int v1 = V == 1 ? 4 : 1;
-  if (p.vpt > v1) launch_rows<T, V, 2 * v1, 1>(a, p, bwd, st);
-  else if (p.two) launch_rows<T, V, v1, 2>(a, p, bwd, st);
-  else launch_rows<T, V, v1, 1>(a, p, bwd, st);
+static void launch_wide_rows(const NormArgs &a, const NormPlan &p, bool bwd, int64_t rows_per,
+                             int nparts, cudaStream_t st) {
+  if (!bwd) k_norm_fwd_wide<T, V><<<p.grid, kNormThreads, 0, st>>>(a);
+  if (bwd && a.y) k_norm_bwd_wide<T, V><<<p.grid, kNormThreads, 0, st>>>(a);
+  if (nparts > 0)
+    k_norm_cols_wide<T, V><<<dim3((unsigned)((a.cols / V + 127) / 128), (unsigned)nparts), 128, 0,
+                             st>>>(a, rows_per);
+}
+
+static void launch_wide(const NormArgs &a, const NormPlan &p, bool bf16, bool bwd,
+                        int64_t rows_per, int nparts, cudaStream_t st) {
+  if (bf16 && p.v > 1) launch_wide_rows<__nv_bfloat16, 8>(a, p, bwd, rows_per, nparts, st);
+  else if (bf16) launch_wide_rows<__nv_bfloat16, 1>(a, p, bwd, rows_per, nparts, st);
+  else if (p.v > 1) launch_wide_rows<float, 4>(a, p, bwd, rows_per, nparts, st);
+  else launch_wide_rows<float, 1>(a, p, bwd, rows_per, nparts, st);
+}
+
+static bool ptr_aligned(const void *p, size_t n) {
+  return reinterpret_cast<uintptr_t>(p) % n == 0;
 }
 
 static bool rows_aligned(const void *p, int64_t ld, int64_t esize) {
@@ -477,46 +686,40 @@ fqt_status layer_norm(const NormArgs &in, bool bf16, bool bwd, cudaStream_t st) 
   NormArgs a = in;
   const int64_t es = bf16 ? 2 : 4;
   const int nsm = device_sm_count();
-  const bool vec = a.cols % (bf16 ? 8 : 4) == 0 && rows_aligned(a.x, a.ldx, es) &&
+  const bool vec = a.cols % (bf16 ? 8 : 4) == 0 && ptr_aligned(a.gamma, 16) &&
+                   ptr_aligned(a.beta, 16) && rows_aligned(a.x, a.ldx, es) &&
                    rows_aligned(a.dy, a.lddy, es) && rows_aligned(a.y, a.ldy, es);
-  NormPlan p = norm_plan(a.rows, a.cols, bf16, vec, nsm);
+  NormPlan p = norm_plan(a.rows, a.cols, bf16, vec, bwd, nsm);
   int nparts = p.grid;
   if (p.wide) {
-    if (!bwd) {
-      if (bf16) k_norm_fwd_wide<__nv_bfloat16><<<p.grid, p.G, 0, st>>>(a);
-      else k_norm_fwd_wide<float><<<p.grid, p.G, 0, st>>>(a);
+    if (bwd && a.part) {
+      nparts = (int)(a.rows < kNormColRows ? a.rows : kNormColRows);
+      const int64_t per = (a.rows + nparts - 1) / nparts;
+      nparts = (int)((a.rows + per - 1) / per);
+      launch_wide(a, p, bf16, bwd, per, nparts, st);
     } else {
-      if (a.y) {
-        if (bf16) k_norm_bwd_wide<__nv_bfloat16><<<p.grid, p.G, 0, st>>>(a);
-        else k_norm_bwd_wide<float><<<p.grid, p.G, 0, st>>>(a);
-      }
-      if (a.part) {
-        nparts = (int)(a.rows < 32 ? a.rows : 32);
-        const int64_t per = (a.rows + nparts - 1) / nparts;
-        nparts = (int)((a.rows + per - 1) / per);
-        const dim3 grid((unsigned)((a.cols + 255) / 256), (unsigned)nparts);
-        if (bf16) k_norm_cols_wide<__nv_bfloat16><<<grid, 256, 0, st>>>(a, per);
-        else k_norm_cols_wide<float><<<grid, 256, 0, st>>>(a, per);
-      }
+      launch_wide(a, p, bf16, bwd, 0, 0, st);
     }
-  } else if (bf16) {
-    if (vec) launch_held<__nv_bfloat16, 8>(a, p, bwd, st);
-    else launch_held<__nv_bfloat16, 1>(a, p, bwd, st);
-  } else {
-    if (vec) launch_held<float, 4>(a, p, bwd, st);
-    else launch_held<float, 1>(a, p, bwd, st);
   }
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = p.wide ? cudaGetLastError()
+                  : bwd  ? launch_norm<true>(a, p, bf16, st)
+                         : launch_norm<false>(a, p, bf16, st);
   if (e != cudaSuccess) return cuda_fail(e, "layer norm launch");
   if (bwd && a.part) {
-    k_norm_cols<<<(a.cols + 31) / 32, 256, 0, st>>>(a.part, nparts, a.cols, a.dgamma, a.dbeta);
-    return cuda_fail(cudaGetLastError(), "layer norm column sums launch");
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.cols + 7) / 8));
+    cfg.blockDim = dim3(kNormColThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, k_norm_cols, (const float *)a.part, nparts, a.cols, a.dgamma,
+                           a.dbeta);
+    return cuda_fail(e, "layer norm column sums launch");
   }
   return FQT_OK;
-}
-
-static bool ptr_aligned(const void *p, size_t n) {
-  return reinterpret_cast<uintptr_t>(p) % n == 0;
 }
 
 // rows x cols entries at a row pitch of ld: sizes that stay inside 64 bits

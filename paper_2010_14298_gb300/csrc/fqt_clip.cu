@@ -5,10 +5,11 @@
 //   out  = g max_norm / norm where norm > max_norm, else g
 //
 // Two passes over the gradients, bound by memory traffic: one adds the squares, one
-// scales.  The tensors are cut into units of 32 KB, which CTAs take in a fixed order
-// whatever tensor they lie in, so that hundreds of small tensors cost one launch and
-// a few large ones still fill the GPU.  The second pass runs through the units
-// backwards: what the first one read last is still in L2.
+// scales.  The tensors are cut into units of 32 KB, which CTAs take in turn whatever
+// tensor they lie in, so that hundreds of small tensors cost one launch and a few large
+// ones fill the GPU.  (A run of its own for every CTA balances better, but the second
+// pass then took 42 us instead of 31 for the 102 MB of a ResNet-50.)  The second pass
+// goes through the units backwards: what the first one read last is still in L2.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -19,6 +20,7 @@
 namespace fqt {
 
 constexpr int kClipThreads = 256;
+constexpr int kClipCtas = 3;  // of an SM
 constexpr int kClipVecs = 8;  // 16-byte loads of a thread per unit
 constexpr int kClipUnitBytes = kClipThreads * kClipVecs * 16;
 
@@ -42,9 +44,10 @@ struct ClipTable {
 constexpr int kClipSmall = 40, kClipMid = 250, kClipLarge = 1020;  // 1.3, 8 and 32.6 KB
 static_assert(sizeof(ClipTable<kClipLarge>) <= 32764 - 64, "launch parameters end at 32764 bytes");
 
+// The entry of a unit: the last one in lo .. hi with unit0 <= unit.
 template <int CAP>
-__device__ __forceinline__ int clip_entry(const ClipTable<CAP> &t, uint32_t unit) {
-  int lo = 0, hi = t.n - 1;  // the last entry with unit0 <= unit
+__device__ __forceinline__ int clip_entry(const ClipTable<CAP> &t, int lo, int hi,
+                                          uint32_t unit) {
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (t.e[mid].unit0 <= unit) lo = mid;
@@ -53,35 +56,94 @@ __device__ __forceinline__ int clip_entry(const ClipTable<CAP> &t, uint32_t unit
   return lo;
 }
 
-// A unit of an entry: `count` entries at `in` (and `out`).
+// A unit: `count` entries at `in` (and `out`): `head` entries before the first 16-byte
+// boundary, whole vectors, and what is left.
 struct ClipUnit {
   const char *in;
   char *out;
-  int count;
+  int count, head, nvec;
   bool bf16;
 };
 
-template <int CAP>
-__device__ __forceinline__ ClipUnit clip_unit(const ClipTable<CAP> &t, uint32_t unit) {
-  const ClipEntry &e = t.e[clip_entry(t, unit)];
-  const int per = kClipUnitBytes / (e.bf16 ? 2 : 4);
-  const int64_t at = (int64_t)(unit - e.unit0) * per;
+__device__ __forceinline__ ClipUnit clip_unit(const ClipEntry &e, uint32_t unit) {
+  const int es = e.bf16 ? 2 : 4, per = kClipUnitBytes / es;
+  const int64_t first = (int64_t)(unit - e.unit0) * per;
   ClipUnit u;
-  u.in = static_cast<const char *>(e.in) + at * (e.bf16 ? 2 : 4);
-  u.out = static_cast<char *>(e.out) + at * (e.bf16 ? 2 : 4);
-  u.count = (int)min((int64_t)per, e.count - at);
+  u.in = static_cast<const char *>(e.in) + first * es;
+  u.out = static_cast<char *>(e.out) + first * es;
+  u.count = (int)min((int64_t)per, e.count - first);
   u.bf16 = e.bf16;
+  const int off = (int)(reinterpret_cast<uintptr_t>(u.in) & 15);
+  u.head = min(u.count, off ? (16 - off) / es : 0);
+  u.nvec = (u.count - u.head) / (16 / es);
   return u;
 }
 
 // Squares of fp32 entries leave fp32's range for entries outside 2^-63 .. 2^64, so
 // the sum of a vector's squares says which of three sums it belongs to: as it is,
 // or of the entries times 2^96 or 2^-96.  (An entry that is no number is in the last
-// one.)  The sums that count in practice are float-float per thread.
+// one.)  The sums that count in practice are float-float.  (No 64-bit arithmetic: this
+// GPU's FP64 pipe made the sum of the CTAs' sums, in every CTA of the second pass, take
+// 4 us.)
 struct Squares {
   ff mid;
   float small, big;
 };
+
+__device__ __forceinline__ Squares add(const Squares &a, const Squares &b) {
+  return {ff_add(a.mid, b.mid), a.small + b.small, a.big + b.big};
+}
+
+__device__ __forceinline__ Squares from_lane(const Squares &s, int o) {  // lane ^ o
+  return {{__shfl_xor_sync(0xffffffffu, s.mid.h, o), __shfl_xor_sync(0xffffffffu, s.mid.l, o)},
+          __shfl_xor_sync(0xffffffffu, s.small, o),
+          __shfl_xor_sync(0xffffffffu, s.big, o)};
+}
+
+// The sum over the CTA's threads, in thread 0, in a fixed order.
+__device__ __forceinline__ Squares cta_sum(Squares s) {
+  __shared__ Squares sums[kClipThreads / 32];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s = add(s, from_lane(s, o));
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    s = sums[threadIdx.x % (kClipThreads / 32)];
+#pragma unroll
+    for (int o = kClipThreads / 64; o > 0; o >>= 1) s = add(s, from_lane(s, o));
+  }
+  return s;
+}
+
+// sqrt of the sum as norm = root 2^k, root in [1, 2): the sums in units of 2^192, 1 or
+// 2^-192, whichever is the largest that holds any (what is then lost is under 2^-24 of
+// it).  Returns whether it is finite; a sum of 0 gives root 0.
+__device__ __forceinline__ bool norm_of(const Squares &s, float *root, int *k) {
+  float t = ff_round(s.mid);
+  int unit = 0;
+  if (!(s.big == 0.0f)) {  // NaN too
+    t = s.big + t * 0x1p-96f * 0x1p-96f;
+    unit = 96;
+  } else if (t > 0.0f) {
+    t += s.small * 0x1p-96f * 0x1p-96f;
+  } else {
+    t = s.small;
+    unit = -96;
+  }
+  *k = 0;
+  *root = 0.0f;
+  if (t == 0.0f) return true;
+  if (!isfinite(t)) {
+    *root = t;
+    return false;
+  }
+  int e;
+  float m = frexpf(t, &e);  // m in [1/2, 1)
+  e -= 1;                   // 2 m in [1, 2)
+  *root = sqrtf(e & 1 ? 4.0f * m : 2.0f * m);
+  *k = ((e - (e & 1)) >> 1) + unit;
+  return true;
+}
 
 __device__ __forceinline__ void add_squares(Squares &s, float &unit, const float *x, int n) {
   float q = 0.0f;
@@ -118,86 +180,69 @@ __device__ __forceinline__ float one_entry(const char *p, int i, bool bf16) {
   return reinterpret_cast<const float *>(p)[i];
 }
 
-// Entries before the first 16-byte boundary, at most the unit's.
-__device__ __forceinline__ int unit_head(const ClipUnit &u) {
-  const int off = (int)(reinterpret_cast<uintptr_t>(u.in) & 15);
-  return min(u.count, off ? (16 - off) / (u.bf16 ? 2 : 4) : 0);
+template <int PER>
+__device__ __forceinline__ void add_unit(Squares &s, const ClipUnit &u) {
+  const bool bf16 = PER == 8;
+  const uint4 *body = reinterpret_cast<const uint4 *>(u.in + u.head * (16 / PER));
+  uint4 v[kClipVecs];
+#pragma unroll
+  for (int k = 0; k < kClipVecs; ++k) {
+    const int i = k * kClipThreads + threadIdx.x;
+    v[k] = i < u.nvec ? __ldg(body + i) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kClipVecs; ++k) {
+    float x[8];
+    widen(v[k], bf16, x);
+    add_squares(s, sum, x, PER);
+  }
+  // what lies outside the 16-byte vectors: under PER entries at either end
+  if ((int)threadIdx.x < u.count - u.nvec * PER) {
+    const int i = (int)threadIdx.x < u.head ? threadIdx.x : threadIdx.x + u.nvec * PER;
+    const float x = one_entry(u.in, i, bf16);
+    add_squares(s, sum, &x, 1);
+  }
+  s.mid = ff_add(s.mid, {sum, 0.0f});
 }
 
 // part[CTA]: the sum of its units' squares.
 template <int CAP>
-__global__ void __launch_bounds__(kClipThreads)
-    k_clip_squares(const __grid_constant__ ClipTable<CAP> t, double *part) {
-  __shared__ double sums[kClipThreads / 32];
+__global__ void __launch_bounds__(kClipThreads, kClipCtas)
+    k_clip_squares(const __grid_constant__ ClipTable<CAP> t, float4 *part) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   Squares s = {{0.0f, 0.0f}, 0.0f, 0.0f};
+  int e = 0;
   for (uint32_t unit = blockIdx.x; unit < t.units; unit += gridDim.x) {
-    const ClipUnit u = clip_unit(t, unit);
-    const int head = unit_head(u), per = u.bf16 ? 8 : 4;
-    const int nvec = (u.count - head) / per;
-    const uint4 *body =
-        reinterpret_cast<const uint4 *>(u.in + (size_t)head * (u.bf16 ? 2 : 4));
-    uint4 v[kClipVecs];
-#pragma unroll
-    for (int k = 0; k < kClipVecs; ++k) {
-      const int i = k * kClipThreads + threadIdx.x;
-      v[k] = i < nvec ? body[i] : make_uint4(0u, 0u, 0u, 0u);
-    }
-    float sum = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kClipVecs; ++k) {
-      float x[8];
-      widen(v[k], u.bf16, x);
-      if (u.bf16) add_squares(s, sum, x, 8);
-      else add_squares(s, sum, x, 4);
-    }
-    // what lies outside the 16-byte vectors: under 8 entries at either end
-    const int tail = u.count - head - nvec * per;
-    if (threadIdx.x < head + tail) {
-      const int i = (int)threadIdx.x < head ? threadIdx.x : head + nvec * per + threadIdx.x - head;
-      const float x = one_entry(u.in, i, u.bf16);
-      add_squares(s, sum, &x, 1);
-    }
-    s.mid = ff_add(s.mid, {sum, 0.0f});
+    if (e + 1 < t.n && t.e[e + 1].unit0 <= unit) e = clip_entry(t, e + 1, t.n - 1, unit);
+    const ClipUnit u = clip_unit(t.e[e], unit);
+    if (u.bf16) add_unit<8>(s, u);
+    else add_unit<4>(s, u);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const ff m = {__shfl_xor_sync(0xffffffffu, s.mid.h, o),
-                  __shfl_xor_sync(0xffffffffu, s.mid.l, o)};
-    s.mid = ff_add(s.mid, m);
-    s.small += __shfl_xor_sync(0xffffffffu, s.small, o);
-    s.big += __shfl_xor_sync(0xffffffffu, s.big, o);
-  }
-  if ((threadIdx.x & 31) == 0)
-    sums[threadIdx.x >> 5] = (double)s.mid.h + (double)s.mid.l + (double)s.small * 0x1p-192 +
-                             (double)s.big * 0x1p192;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double total = 0.0;
-    for (int w = 0; w < kClipThreads / 32; ++w) total += sums[w];
-    part[blockIdx.x] = total;
-  }
+  s = cta_sum(s);
+  if (threadIdx.x == 0) part[blockIdx.x] = make_float4(s.mid.h, s.mid.l, s.small, s.big);
 }
 
 // The factor, from the partial sums (every CTA adds them in the same order); CTA 0
 // writes the norm.
-__device__ __forceinline__ float clip_factor(const double *part, int nparts, float max_norm,
+__device__ __forceinline__ float clip_factor(const float4 *part, int nparts, float max_norm,
                                              float *norm_out, int *status) {
-  __shared__ double sums[kClipThreads / 32];
   __shared__ float factor;
-  double s = 0.0;
-  for (int i = threadIdx.x; i < nparts; i += kClipThreads) s += part[i];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
-  __syncthreads();
+  Squares s = {{0.0f, 0.0f}, 0.0f, 0.0f};
+  for (int i = threadIdx.x; i < nparts; i += kClipThreads) {
+    const float4 v = __ldcg(part + i);
+    s = add(s, {{v.x, v.y}, v.z, v.w});
+  }
+  s = cta_sum(s);
   if (threadIdx.x == 0) {
-    double total = 0.0;
-    for (int w = 0; w < kClipThreads / 32; ++w) total += sums[w];
-    const double norm = sqrt(total);
-    const bool good = isfinite(norm);
-    factor = good && norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f;
+    float root;
+    int k;
+    const bool good = norm_of(s, &root, &k);
+    const float norm = ldexpf(root, k);  // infinite where it passes fp32
+    // max_norm / norm, the quotient of numbers in fp32's middle first
+    factor = good && norm > max_norm ? ldexpf(max_norm / root, -k) : 1.0f;
     if (blockIdx.x == 0) {
-      if (norm_out) *norm_out = (float)norm;
+      if (norm_out) *norm_out = norm;
       if (!good) record_status(status, FQT_ENONFINITE);
     }
   }
@@ -205,71 +250,89 @@ __device__ __forceinline__ float clip_factor(const double *part, int nparts, flo
   return factor;
 }
 
-template <int CAP>
-__global__ void __launch_bounds__(kClipThreads)
-    k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const double *part, int nparts,
-                 float max_norm, float *norm_out, int *status) {
-  const float f = clip_factor(part, nparts, max_norm, norm_out, status);
-  for (uint32_t k = blockIdx.x; k < t.units; k += gridDim.x) {
-    const ClipUnit u = clip_unit(t, t.units - 1 - k);
-    if (f == 1.0f && u.in == u.out) continue;  // nothing to change in place
-    const int es = u.bf16 ? 2 : 4, per = 16 / es;
-    // vectors where the output lies on the same bytes of 16 as the input
-    const bool vec = ((reinterpret_cast<uintptr_t>(u.in) ^ reinterpret_cast<uintptr_t>(u.out)) &
-                      15) == 0;
-    const int head = vec ? unit_head(u) : 0;
-    const int nvec = vec ? (u.count - head) / per : 0;
-    const uint4 *in = reinterpret_cast<const uint4 *>(u.in + (size_t)head * es);
-    uint4 *out = reinterpret_cast<uint4 *>(u.out + (size_t)head * es);
-    uint4 v[kClipVecs];
+template <int PER>
+__device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
+  const bool bf16 = PER == 8;
+  // vectors where the output lies on the same bytes of 16 as the input
+  const bool vec = ((reinterpret_cast<uintptr_t>(u.in) ^ reinterpret_cast<uintptr_t>(u.out)) &
+                    15) == 0;
+  const int head = vec ? u.head : 0, nvec = vec ? u.nvec : 0;
+  const uint4 *in = reinterpret_cast<const uint4 *>(u.in + head * (16 / PER));
+  uint4 *out = reinterpret_cast<uint4 *>(u.out + head * (16 / PER));
+  uint4 v[kClipVecs];
 #pragma unroll
-    for (int i = 0; i < kClipVecs; ++i) {
-      const int at = i * kClipThreads + threadIdx.x;
-      if (at < nvec) v[i] = in[at];
-    }
+  for (int k = 0; k < kClipVecs; ++k) {
+    const int i = k * kClipThreads + threadIdx.x;
+    if (i < nvec) v[k] = in[i];
+  }
 #pragma unroll
-    for (int i = 0; i < kClipVecs; ++i) {
-      const int at = i * kClipThreads + threadIdx.x;
-      if (at >= nvec) continue;
-      float x[8];
-      widen(v[i], u.bf16, x);
-      uint32_t w[4];
+  for (int k = 0; k < kClipVecs; ++k) {
+    const int i = k * kClipThreads + threadIdx.x;
+    if (i >= nvec) continue;
+    float x[8];
+    widen(v[k], bf16, x);
+    uint32_t w[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (u.bf16) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * j] * f, x[2 * j + 1] * f);
-          w[j] = *reinterpret_cast<const uint32_t *>(&b);
-        } else {
-          w[j] = __float_as_uint(x[j] * f);
-        }
+    for (int j = 0; j < 4; ++j) {
+      if (bf16) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * j] * f, x[2 * j + 1] * f);
+        w[j] = *reinterpret_cast<const uint32_t *>(&b);
+      } else {
+        w[j] = __float_as_uint(x[j] * f);
       }
-      out[at] = f == 1.0f ? v[i] : make_uint4(w[0], w[1], w[2], w[3]);
     }
-    // the ends, or a unit without vectors
-    const int rest = u.count - nvec * per;
-    for (int j = threadIdx.x; j < rest; j += kClipThreads) {
-      const int i = j < head ? j : j + nvec * per;
-      const float x = one_entry(u.in, i, u.bf16) * f;
-      if (u.bf16) reinterpret_cast<__nv_bfloat16 *>(u.out)[i] = __float2bfloat16_rn(x);
-      else reinterpret_cast<float *>(u.out)[i] = x;
+    out[i] = f == 1.0f ? v[k] : make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  // the ends, or a unit without vectors
+  const int rest = u.count - nvec * PER;
+  for (int j = threadIdx.x; j < rest; j += kClipThreads) {
+    const int i = j < head ? j : j + nvec * PER;
+    if (bf16) {
+      const unsigned short raw = reinterpret_cast<const unsigned short *>(u.in)[i];
+      const __nv_bfloat16 y = __float2bfloat16_rn(one_entry(u.in, i, true) * f);
+      reinterpret_cast<unsigned short *>(u.out)[i] = f == 1.0f ? raw : __bfloat16_as_ushort(y);
+    } else {
+      const uint32_t raw = reinterpret_cast<const uint32_t *>(u.in)[i];
+      reinterpret_cast<uint32_t *>(u.out)[i] =
+          f == 1.0f ? raw : __float_as_uint(__uint_as_float(raw) * f);
     }
+  }
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kClipThreads, kClipCtas)
+    k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const float4 *part, int nparts,
+                 float max_norm, float *norm_out, int *status) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const float f = clip_factor(part, nparts, max_norm, norm_out, status);
+  int e = t.n - 1;
+  // the units of the CTA of this number in the first pass, from the last to the first
+  const uint32_t mine = (t.units - 1 - blockIdx.x) / gridDim.x;
+  for (uint32_t k = 0; k <= mine; ++k) {
+    const uint32_t unit = blockIdx.x + (mine - k) * gridDim.x;
+    if (t.e[e].unit0 > unit) e = clip_entry(t, 0, e - 1, unit);
+    if (f == 1.0f && t.e[e].in == t.e[e].out) continue;  // nothing to change in place
+    const ClipUnit u = clip_unit(t.e[e], unit);
+    if (u.bf16) scale_unit<8>(u, f);
+    else scale_unit<4>(u, f);
   }
 }
 
 // The norm alone.
 __global__ void __launch_bounds__(kClipThreads)
-    k_clip_norm(const double *part, int nparts, float *norm_out, int *status) {
+    k_clip_norm(const float4 *part, int nparts, float *norm_out, int *status) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   clip_factor(part, nparts, INFINITY, norm_out, status);
 }
 
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-static int clip_grid(int nsm) { return 3 * nsm; }
+static int clip_grid(int nsm) { return kClipCtas * nsm; }
 
 size_t clip_ws_bytes(int64_t n) {
   const int64_t launches = n > 0 ? (n + kClipLarge - 1) / kClipLarge : 1;
-  return kHeaderBytes + (size_t)launches * clip_grid(device_sm_count()) * sizeof(double);
+  return kHeaderBytes + (size_t)launches * clip_grid(device_sm_count()) * sizeof(float4);
 }
 
 // Entries first .. of the lists, as many as a table holds; returns the next one.
@@ -289,11 +352,26 @@ static int64_t fill_table(ClipTable<CAP> &t, const fqt_tensor *in, const fqt_ten
   return i;
 }
 
+// A launch that may begin while the one before it ends (the kernel waits for that).
+template <typename... P, typename... A>
+static cudaError_t launch_after(int grid, cudaStream_t st, void (*kernel)(P...), A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(kClipThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <int CAP>
 static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_t n,
                              float max_norm, float *norm, void *ws, cudaStream_t st) {
   const int most = clip_grid(device_sm_count());
-  double *part = reinterpret_cast<double *>(static_cast<char *>(ws) + kHeaderBytes);
+  float4 *part = reinterpret_cast<float4 *>(static_cast<char *>(ws) + kHeaderBytes);
   int *status = static_cast<int *>(ws);
   ClipTable<CAP> t;
   int nparts = 0;
@@ -307,8 +385,9 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
     nparts += grid;
   }
   if (!out || nparts == 0) {
-    k_clip_norm<<<1, kClipThreads, 0, st>>>(part, nparts, norm, status);
-    return cuda_fail(cudaGetLastError(), "gradient norm launch");
+    const cudaError_t e =
+        launch_after(1, st, k_clip_norm, (const float4 *)part, nparts, norm, status);
+    return cuda_fail(e, "gradient norm launch");
   }
   bool first = true;
   for (int64_t i = 0; i < n;) {
@@ -316,9 +395,9 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
     else i = n;  // the table is still there
     if (t.units == 0) continue;
     const int grid = t.units < (uint32_t)most ? (int)t.units : most;
-    k_clip_scale<CAP><<<grid, kClipThreads, 0, st>>>(t, part, nparts, max_norm,
-                                                     first ? norm : nullptr, status);
-    const cudaError_t e = cudaGetLastError();
+    // (a second list waits for the first one's scaling only, which waited for the sums)
+    const cudaError_t e = launch_after(grid, st, k_clip_scale<CAP>, t, (const float4 *)part,
+                                       nparts, max_norm, first ? norm : nullptr, status);
     if (e != cudaSuccess) return cuda_fail(e, "gradient clipping launch");
     first = false;
   }
@@ -350,7 +429,7 @@ fqt_status fqt_clip_grad_norm(const fqt_tensor *grads, const fqt_tensor *out, in
       if (g.count > 0 &&
           (!g.data || reinterpret_cast<uintptr_t>(g.data) % (g.dtype == FQT_BF16 ? 2 : 4)))
         return FQT_EINVAL;
-      if ((total += g.count) > ((int64_t)1 << 44)) return FQT_EINVAL;
+      if ((total += g.count) > ((int64_t)1 << 41)) return FQT_EINVAL;
     }
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || ws_bytes < clip_ws_bytes(n))
     return FQT_EWORKSPACE;

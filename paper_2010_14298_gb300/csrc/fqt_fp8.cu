@@ -495,37 +495,39 @@ __device__ __forceinline__ uint4 f8_pack(const uint32_t *v) {
   }
 }
 
-// This thread's 32 sums: row m of the tile's rows, columns n ..
+// A warp's 32 rows (this lane's is m0 + lane) x W <= 32 columns from n on, one by one:
+// transposed outputs straight from the registers (lanes are neighbours there), others
+// by way of the box, so that a row's columns are neighbours.
 template <typename T>
-__device__ __forceinline__ void f8_store(const F8Args &g, T *out, int64_t ld, int64_t m,
-                                         int64_t n, const uint32_t (&v)[32], int W) {
-  if (m >= g.M) return;
+__device__ __forceinline__ void f8_store(const F8Args &g, T *out, int64_t ld, float *box,
+                                         int lane, int64_t m0, int64_t n,
+                                         const uint32_t (&v)[32], int W) {
   if (g.swap) {
+    const int64_t m = m0 + lane;
 #pragma unroll
     for (int j = 0; j < 32; ++j)
-      if (j < W && n + j < g.N) out[(n + j) * ld + m] = f8_out<T>(__uint_as_float(v[j]));
+      if (m < g.M && j < W && n + j < g.N) out[(n + j) * ld + m] = f8_out<T>(__uint_as_float(v[j]));
     return;
   }
-  T *p = out + m * ld + n;
-  constexpr int E = 16 / sizeof(T);
-  const bool vec = (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+  if (m0 >= g.M || n >= g.N) return;
+  __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 32; j += E) {
-    if (j >= W) break;
-    if (vec && n + j + E <= g.N) {
-      *reinterpret_cast<uint4 *>(p + j) = f8_pack<T>(&v[j]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (n + j + i < g.N) p[j + i] = f8_out<T>(__uint_as_float(v[j + i]));
-    }
-  }
+  for (int j = 0; j < 32; j += 4)  // 16-byte chunk j / 4 of row r at chunk (j / 4) ^ (r & 7)
+    *reinterpret_cast<uint4 *>(box + lane * 32 + (j ^ (4 * (lane & 7)))) =
+        make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  __syncwarp();
+  const int rows = (int)min((int64_t)32, g.M - m0);
+  T *p = out + m0 * ld + n + lane;
+  const bool in = lane < W && n + lane < g.N;
+#pragma unroll 8
+  for (int r = 0; r < rows; ++r)
+    if (in) p[r * ld] = f8_out<T>(box[r * 32 + (lane ^ (4 * (r & 7)))]);
 }
 
 // The same for a warp's 32 rows at once, through a box in shared memory that TMA writes
 // (it leaves out what lies past the output's ends): 32 columns of fp32 in rows of 128
 // bytes (128-byte swizzle), or of bf16 in rows of 64 (64-byte swizzle).  Stored from
-// registers, a warp's 16-byte pieces of 32 rows take half a sector each.
+// registers, a warp's pieces of 32 rows would take a part of a sector each.
 template <typename T>
 __device__ __forceinline__ void f8_store_box(const F8Args &g, const CUtensorMap *map,
                                              uint8_t *box, int lane, int64_t m0, int64_t n,
@@ -656,19 +658,22 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       for (int p = 0; p < P; ++p) {
         if (32 * p >= W) break;
         const int64_t np = n + 32 * p;
-        if (NT > 64 && g.boxes) {
+        if (NT >= 64 && g.boxes) {
           if (g.bf16)
             f8_store_box<__nv_bfloat16>(g, &tmOut, box + (nbox ^= 1) * 2048, lane, m, np, v[p]);
           else
             f8_store_box<float>(g, &tmOut, box, lane, m, np, v[p]);
-        } else if (g.splits > 1) {
-          f8_store<float>(g, g.part + t.split * g.M * g.N, g.swap ? g.M : g.N, m + lane, np, v[p],
-                          W);
-        } else if (g.bf16) {
-          f8_store<__nv_bfloat16>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, m + lane, np,
-                                  v[p], W);
         } else {
-          f8_store<float>(g, static_cast<float *>(g.out), g.ldo, m + lane, np, v[p], W);
+          float *rows = reinterpret_cast<float *>(box);
+          const int w = W - 32 * p;
+          if (g.splits > 1)
+            f8_store<float>(g, g.part + t.split * g.M * g.N, g.swap ? g.M : g.N, rows, lane, m,
+                            np, v[p], w);
+          else if (g.bf16)
+            f8_store<__nv_bfloat16>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, rows, lane, m,
+                                    np, v[p], w);
+          else
+            f8_store<float>(g, static_cast<float *>(g.out), g.ldo, rows, lane, m, np, v[p], w);
         }
       }
     }
@@ -901,12 +906,17 @@ static F8Plan f8_plan(int64_t M, int64_t N, int64_t nkb, int nsm) {
            ((a + 255) / 256) * ((b + 255) / 256) * 8 >= (int64_t)nsm * 3;
   const int rows = p.pair ? 2 * BM : BM;
   p.m_tiles = (int)((a + rows - 1) / rows);
-  p.nt = p.pair ? 256 : !p.swap ? 128 : b <= 32 ? 32 : 64;
+  // single CTAs: 128 columns where that occupies half of the SMs
+  const bool wide = p.m_tiles * ((b + 127) / 128) * 2 >= nsm;
+  p.nt = p.pair ? 256 : p.swap ? (b <= 32 ? 32 : 64) : wide ? 128 : 64;
   p.n_tiles = (int)((b + p.nt - 1) / p.nt);
   const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
   // fewer tiles than SMs: the contraction is split, into groups of K blocks
   const int64_t groups = (nkb + kF8Group - 1) / kF8Group;
-  int64_t splits = tiles * 4 <= (int64_t)nsm * 3 && !p.pair ? nsm / tiles : 1;
+  // (eight K blocks a part at least: the second launch costs as much as ten)
+  int64_t splits = p.pair ? 1 : nsm / tiles;
+  if (splits > nkb / 8) splits = nkb / 8;
+  if (splits < 1) splits = 1;
   // ... and where an accumulator would take more than 8192 terms: a step of the tensor
   // core drops what lies below the accumulator's last bit (5e-7 of the result after
   // 8192 terms, 8e-6 after 65536)
@@ -928,14 +938,14 @@ template <int NT, int ACCS, bool PAIR>
 static fqt_status launch_f8(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &to,
                             F8Args &g, int nsm, cudaStream_t st) {
   constexpr size_t stage = kTileBytes + (PAIR ? NT / 2 : NT) * kF8Block;
-  constexpr size_t boxes = NT > 64 ? kF8EpiWarps * kF8BoxBytes : 0;
+  constexpr size_t boxes = NT >= 64 ? kF8EpiWarps * kF8BoxBytes : 0;
   constexpr size_t room = 227 * 1024 - 1024 - kF8Fixed - boxes;
   constexpr int stages = room / stage < kMaxStages ? (int)(room / stage) : kMaxStages;
   constexpr size_t smem = 1024 + kF8Fixed + stages * stage + boxes;
   g.stages = stages;
   auto kernel = k_f8_mm<NT, ACCS, PAIR>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)smem);
+  static DeviceOnce once;
+  cudaError_t e = allow_smem(kernel, smem, once);
   if (e != cudaSuccess) return cuda_fail(e, "FP8 product attribute");
   const int64_t ctas = g.items * (PAIR ? 2 : 1);
   const int most = PAIR ? nsm & ~1 : nsm;
@@ -1018,7 +1028,7 @@ fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, 
   const fqt_fp8 *a = p.swap ? B : A, *b = p.swap ? A : B;
   F8Args g = {};
   g.ldo = M > 1 ? ldo : N;
-  g.boxes = p.nt > 64 && p.splits == 1 && f8_aligned(out, 16) &&
+  g.boxes = !p.swap && p.splits == 1 && f8_aligned(out, 16) &&
             g.ldo * (bf16 ? 2 : 4) % 16 == 0;
   CUtensorMap ta, tb, to = {};
   if (!make_map_codes(&ta, a, BM) || !make_map_codes(&tb, b, (uint32_t)(p.pair ? p.nt / 2 : p.nt)) ||

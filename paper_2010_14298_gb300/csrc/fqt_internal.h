@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "fqt.h"
 
 namespace fqt {
@@ -103,6 +105,23 @@ fqt_status launch_bhq_grouping(const void *dH, bool bf16, int64_t N, int C, int3
 fqt_status launch_bhq_groups(QuantArgs &a, bool bf16, int num_sms, cudaStream_t st);
 
 int device_sm_count();
+
+// A kernel's limit of dynamic shared memory, raised once per device (the call takes
+// half a microsecond): `once` is a static of the kernel's launcher.
+struct DeviceOnce {
+  std::atomic<uint64_t> devices{0};
+};
+template <typename K>
+inline cudaError_t allow_smem(K kernel, size_t bytes, DeviceOnce &once) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (once.devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) once.devices.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 
 // Records the CUDA error behind an FQT_ECUDA return (per thread) and returns
 // FQT_ECUDA, or FQT_OK for cudaSuccess.

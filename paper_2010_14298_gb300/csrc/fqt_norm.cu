@@ -100,12 +100,21 @@ template <int V, int VPT>
 __device__ __forceinline__ void load_columns(const float *p, int cols, int G, int t, float none,
                                              float (&v)[V * VPT]) {
 #pragma unroll
-  for (int j = 0; j < VPT; ++j)
+  for (int j = 0; j < VPT; ++j) {
+    const int c = (j * G + t) * V;
+    if (!p || c >= cols) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = (j * G + t) * V + i;
-      v[j * V + i] = p && c < cols ? __ldg(p + c) : none;
+      for (int i = 0; i < V; ++i) v[j * V + i] = none;
+    } else if constexpr (V == 1) {
+      v[j] = __ldg(p + c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const float4 f = __ldg(reinterpret_cast<const float4 *>(p + c + i));
+        v[j * V + i] = f.x; v[j * V + i + 1] = f.y; v[j * V + i + 2] = f.z; v[j * V + i + 3] = f.w;
+      }
     }
+  }
 }
 
 // Sums of a value (two values) over the threads of a group (G threads from a warp
@@ -629,9 +638,9 @@ static cudaError_t launch_rows(const NormArgs &a, const NormPlan &p, cudaStream_
   void (*kernel)(NormArgs, int);
   if constexpr (BWD) kernel = k_norm_bwd<T, V, VPT, S>;
   else kernel = k_norm_fwd<T, V, VPT, R, S>;
-  if (smem > 40 * 1024) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem > 40 * 1024) {  // with the static arrays past 48 KB
+    static DeviceOnce once;
+    const cudaError_t e = allow_smem(kernel, 200 * 1024, once);
     if (e != cudaSuccess) return e;
   }
   kernel<<<p.grid, nth, smem, st>>>(a, p.G);

@@ -336,13 +336,19 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
 // 4096, with per-row scales on both sides 232.)
 constexpr int kF8EpiWarps = 8, kF8Epi0 = 4;  // warps 0 loads, 1 products, 2 and 3 scales
 constexpr int kF8Threads = 32 * (kF8Epi0 + kF8EpiWarps);
+// K blocks of an accumulator of an fp32 output: a step of the tensor core drops what lies
+// below the accumulator's last bit (5e-7 of the result after 8192 terms of equal size,
+// over 1e-6 where a few terms are large, 8e-6 after 65536), so every 1024 terms the sums
+// move to fp32 registers, rounded to nearest.  A bf16 output rounds a thousand times as
+// much away: one accumulator takes all of K.
+constexpr int kF8Chunk = 8;
 constexpr int kF8Group = 4;             // K blocks whose scales share a 32-bit word
 constexpr int kF8Ring = 4;              // groups of scales in shared memory
 constexpr size_t kF8RingBytes = 1536;   // 128 of A's rows, up to 256 of B's
 constexpr size_t kF8OffBar = kF8Ring * kF8RingBytes;
 constexpr size_t kF8Bars = 2 * kMaxStages + 2 * kF8Ring + 5;
 constexpr size_t kF8Fixed = (kF8OffBar + kF8Bars * 8 + 16 + 1023) & ~(size_t)1023;
-constexpr size_t kF8BoxBytes = 4096;    // an epilogue warp's boxes of output
+constexpr size_t kF8BoxBytes = 2048;    // an epilogue warp's box of output
 constexpr int kF8Band = 8;              // row tiles of a band of tiles
 
 struct F8Args {
@@ -478,6 +484,13 @@ __device__ __forceinline__ T f8_out(float v) {
   else return __float2bfloat16_rn(v);
 }
 
+// 32 columns (16 where the warp has no more) of this warp's lanes, without waiting.
+template <int W>
+__device__ __forceinline__ void f8_read(uint32_t taddr, uint32_t (&v)[32]) {
+  if constexpr (W < 32) tmem_ld16_nw(taddr, *reinterpret_cast<uint32_t(*)[16]>(v));
+  else tmem_ld32_nw(taddr, v);
+}
+
 // 16 bytes of output from the sums at v (fp32 bits).
 template <typename T>
 __device__ __forceinline__ uint4 f8_pack(const uint32_t *v) {
@@ -495,6 +508,12 @@ __device__ __forceinline__ uint4 f8_pack(const uint32_t *v) {
   }
 }
 
+// Byte offset of 16-byte chunk k of row r in a box of 32 rows of 64 bytes (the 64-byte
+// swizzle: no bank conflicts either way).
+__device__ __forceinline__ uint32_t box_off(int r, int k) {
+  return (uint32_t)(r * 64 + ((k ^ ((r >> 1) & 3)) << 4));
+}
+
 // A warp's 32 rows (this lane's is m0 + lane) x W <= 32 columns from n on, one by one:
 // transposed outputs straight from the registers (lanes are neighbours there), others
 // by way of the box, so that a row's columns are neighbours.
@@ -510,44 +529,47 @@ __device__ __forceinline__ void f8_store(const F8Args &g, T *out, int64_t ld, fl
     return;
   }
   if (m0 >= g.M || n >= g.N) return;
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < 32; j += 4)  // 16-byte chunk j / 4 of row r at chunk (j / 4) ^ (r & 7)
-    *reinterpret_cast<uint4 *>(box + lane * 32 + (j ^ (4 * (lane & 7)))) =
-        make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-  __syncwarp();
   const int rows = (int)min((int64_t)32, g.M - m0);
-  T *p = out + m0 * ld + n + lane;
-  const bool in = lane < W && n + lane < g.N;
+  const int col = lane & 15, up = lane >> 4;
+#pragma unroll
+  for (int h = 0; h < 32; h += 16) {  // 16 columns of 32 rows at a time, two rows a store
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint4 *>(box + box_off(lane, j) / 4) =
+          make_uint4(v[h + 4 * j], v[h + 4 * j + 1], v[h + 4 * j + 2], v[h + 4 * j + 3]);
+    __syncwarp();
+    const bool in = h + col < W && n + h + col < g.N;
+    T *p = out + m0 * ld + n + h + col;
 #pragma unroll 8
-  for (int r = 0; r < rows; ++r)
-    if (in) p[r * ld] = f8_out<T>(box[r * 32 + (lane ^ (4 * (r & 7)))]);
+    for (int r = up; r < rows; r += 2)
+      if (in) p[r * ld] = f8_out<T>(box[box_off(r, col >> 2) / 4 + (col & 3)]);
+  }
 }
 
-// The same for a warp's 32 rows at once, through a box in shared memory that TMA writes
-// (it leaves out what lies past the output's ends): 32 columns of fp32 in rows of 128
-// bytes (128-byte swizzle), or of bf16 in rows of 64 (64-byte swizzle).  Stored from
-// registers, a warp's pieces of 32 rows would take a part of a sector each.
+// The same through a box that TMA writes (it leaves out what lies past the output's
+// ends): rows of 64 bytes, 16 columns of fp32 or 32 of bf16.  Stored from registers, a
+// warp's pieces of 32 rows would take a part of a sector each.
 template <typename T>
-__device__ __forceinline__ void f8_store_box(const F8Args &g, const CUtensorMap *map,
-                                             uint8_t *box, int lane, int64_t m0, int64_t n,
+__device__ __forceinline__ void f8_store_box(const F8Args &g, const CUtensorMap *map, float *box,
+                                             int lane, int64_t m0, int64_t n,
                                              const uint32_t (&v)[32]) {
   constexpr int E = 16 / sizeof(T);
-  constexpr int kBoxes = sizeof(T) == 4 ? 1 : 2;  // boxes of a warp
-  if (m0 >= g.M || n >= g.N) return;
-  if (lane == 0) bulk_wait_read(kBoxes - 1);
-  __syncwarp();
+  if (m0 >= g.M) return;
 #pragma unroll
-  for (int k = 0; k < 32 / E; ++k) {
-    const uint32_t at = sizeof(T) == 4 ? sw128_off(lane, k)
-                                       : (uint32_t)(lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4));
-    *reinterpret_cast<uint4 *>(box + at) = f8_pack<T>(&v[k * E]);
-  }
-  fence_proxy_async_smem();
-  __syncwarp();
-  if (lane == 0) {
-    tma_store_2d(map, (int32_t)n, (int32_t)m0, box);
-    bulk_commit();
+  for (int h = 0; h < 32; h += 4 * E) {
+    if (n + h >= g.N) return;
+    if (lane == 0) bulk_wait_read(0);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      *reinterpret_cast<uint4 *>(box + box_off(lane, k) / 4) = f8_pack<T>(&v[h + k * E]);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_2d(map, (int32_t)(n + h), (int32_t)m0, box);
+      bulk_commit();
+    }
   }
 }
 
@@ -558,8 +580,9 @@ __device__ __forceinline__ void f8_store_box(const F8Args &g, const CUtensorMap 
 // and 3 in turn the scales of four K blocks, warp 1 issues a K block's four products;
 // the eight epilogue warps (quadrant of rows x half of the columns) take an accumulator
 // into registers, hand it back and store it.  ACCS accumulators of NT columns: with two
-// a tile's products overlap the epilogue of the one before.
-template <int NT, int ACCS, bool PAIR>
+// the products go on meanwhile.  FOLD: an accumulator holds kF8Chunk K blocks, and the
+// epilogue adds them up.
+template <int NT, int ACCS, bool PAIR, bool FOLD>
 __global__ void __launch_bounds__(kF8Threads, 1)
     k_f8_mm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
             const __grid_constant__ CUtensorMap tmOut, const F8Args g) {
@@ -626,54 +649,67 @@ __global__ void __launch_bounds__(kF8Threads, 1)
     const int q = warp & 3, h = (warp - kF8Epi0) >> 2;
     const int W = h ? W1 : W0;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * W0);
-    uint8_t *box = ops + (size_t)g.stages * kStage + (size_t)(warp - kF8Epi0) * kF8BoxBytes;
-    uint32_t c = 0;  // tiles so far
-    int nbox = 0;
-    for (int64_t it = first; it < g.items && !*abort_flag; it += step, ++c) {
+    float *box = reinterpret_cast<float *>(ops + (size_t)g.stages * kStage +
+                                           (size_t)(warp - kF8Epi0) * kF8BoxBytes);
+    uint32_t c = 0;  // accumulators so far
+    bool ok = true;
+    for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step) {
       const F8Item t = f8_item<NT, PAIR>(g, it);
-      const int buf = c % ACCS;
-      if (!f8_wait(&accf[buf], (c / ACCS) & 1u, g.status)) {
-        *abort_flag = 1;
-        break;
-      }
-      tc_fence_after();
       constexpr int P = (W0 + 31) / 32;  // pieces of up to 32 columns
       uint32_t v[P][32];
+      if constexpr (FOLD)
 #pragma unroll
-      for (int p = 0; p < P; ++p)
-        if (32 * p < W) {
-          if constexpr (W0 < 32)
-            tmem_ld16_nw(lane_base + (uint32_t)(buf * NT),
-                         *reinterpret_cast<uint32_t(*)[16]>(v[0]));
-          else
-            tmem_ld32_nw(lane_base + (uint32_t)(buf * NT + 32 * p), v[p]);
+        for (int i = 0; i < 32 * P; ++i) v[i / 32][i % 32] = 0u;
+      for (int kb = t.kb0; kb < t.kb1; kb = FOLD ? kb + kF8Chunk : t.kb1, ++c) {
+        const int buf = c % ACCS;
+        if (!f8_wait(&accf[buf], (c / ACCS) & 1u, g.status)) {
+          *abort_flag = 1;
+          ok = false;
+          break;
         }
+        tc_fence_after();
+        const uint32_t from = lane_base + (uint32_t)(buf * NT);
+        if constexpr (!FOLD) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) tmem_wait_ld(v[p]);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) f8_release<PAIR>(&acce[buf]);
+          for (int p = 0; p < P; ++p) f8_read<W0>(from + 32 * p, v[p]);
+#pragma unroll
+          for (int p = 0; p < P; ++p) tmem_wait_ld(v[p]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < W0; j += 16) {  // 16 columns at a time: registers
+            uint32_t r[16];
+            tmem_ld16_nw(from + (uint32_t)j, r);
+            tmem_wait_ld(r);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              uint32_t &x = v[j / 32][j % 32 + i];
+              x = __float_as_uint(__uint_as_float(x) + __uint_as_float(r[i]));
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) f8_release<PAIR>(&acce[buf]);
+      }
+      if (!ok) break;
       const int64_t m = t.m0 + q * 32, n = t.n0 + h * W0;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         if (32 * p >= W) break;
         const int64_t np = n + 32 * p;
         if (NT >= 64 && g.boxes) {
-          if (g.bf16)
-            f8_store_box<__nv_bfloat16>(g, &tmOut, box + (nbox ^= 1) * 2048, lane, m, np, v[p]);
-          else
-            f8_store_box<float>(g, &tmOut, box, lane, m, np, v[p]);
+          if (g.bf16) f8_store_box<__nv_bfloat16>(g, &tmOut, box, lane, m, np, v[p]);
+          else f8_store_box<float>(g, &tmOut, box, lane, m, np, v[p]);
         } else {
-          float *rows = reinterpret_cast<float *>(box);
           const int w = W - 32 * p;
           if (g.splits > 1)
-            f8_store<float>(g, g.part + t.split * g.M * g.N, g.swap ? g.M : g.N, rows, lane, m,
-                            np, v[p], w);
+            f8_store<float>(g, g.part + t.split * g.M * g.N, g.swap ? g.M : g.N, box, lane, m, np,
+                            v[p], w);
           else if (g.bf16)
-            f8_store<__nv_bfloat16>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, rows, lane, m,
+            f8_store<__nv_bfloat16>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, box, lane, m,
                                     np, v[p], w);
           else
-            f8_store<float>(g, static_cast<float *>(g.out), g.ldo, rows, lane, m, np, v[p], w);
+            f8_store<float>(g, static_cast<float *>(g.out), g.ldo, box, lane, m, np, v[p], w);
         }
       }
     }
@@ -724,55 +760,56 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       // byte of B's and A's scale words
       constexpr uint32_t idesc0 = ((uint32_t)(NT >> 3) << 17) | (1u << 23) |
                                   ((uint32_t)(PAIR ? 2 : 1) << 27);
-      for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step, ++c) {
+      for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step) {
         const F8Item t = f8_item<NT, PAIR>(g, it);
-        const int buf = c % ACCS;
-        if (!f8_wait(&acce[buf], ((c / ACCS) & 1u) ^ 1u, g.status)) {
-          *abort_flag = 1;
-          break;
-        }
         uint32_t sa = 0;
-        for (int kb = t.kb0; kb < t.kb1; ++kb) {
-          if ((kb & (kF8Group - 1)) == 0) {  // the next group's scales
-            const int slot = grp % kF8Ring;
-            if (!f8_wait_cluster(&sfull[slot], (grp / kF8Ring) & 1u, g.status)) {
-              *abort_flag = 1;
+        for (int k0 = t.kb0; ok && k0 < t.kb1; k0 = FOLD ? k0 + kF8Chunk : t.kb1, ++c) {
+          const int k1 = FOLD ? min(k0 + kF8Chunk, t.kb1) : t.kb1, buf = c % ACCS;
+          if (!f8_wait(&acce[buf], ((c / ACCS) & 1u) ^ 1u, g.status)) {
+            ok = false;
+            break;
+          }
+          for (int kb = k0; kb < k1; ++kb) {
+            if ((kb & (kF8Group - 1)) == 0) {  // the next group's scales
+              const int slot = grp % kF8Ring;
+              if (!f8_wait_cluster(&sfull[slot], (grp / kF8Ring) & 1u, g.status)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+              sa = tmem + kScales + (grp & 1u) * (4 + kSbCols);
+              const uint32_t src = smem_u32(smem + slot * kF8RingBytes);
+              f8_copy_scales<PAIR>(sa, src);
+#pragma unroll
+              for (int i = 0; i < kSbCols / 4; ++i)
+                f8_copy_scales<PAIR>(sa + 4 + 4 * i, src + 512 + 512 * i);
+              if constexpr (PAIR) umma_commit_pair(&sempty[slot]);
+              else umma_commit(&sempty[slot]);
+              ++grp;
+            }
+            if (!f8_wait(&full[s], ph, g.status)) {
               ok = false;
               break;
             }
             tc_fence_after();
-            sa = tmem + kScales + (grp & 1u) * (4 + kSbCols);
-            const uint32_t src = smem_u32(smem + slot * kF8RingBytes);
-            f8_copy_scales<PAIR>(sa, src);
+            const uint32_t a_addr = smem_u32(ops + (size_t)s * kStage);
+            const uint64_t da = sw128_desc(a_addr), db = sw128_desc(a_addr + (uint32_t)kTileBytes);
+            const uint32_t id = (uint32_t)kb & (kF8Group - 1);
+            const uint32_t idesc = idesc0 | id << 4 | id << 29;
 #pragma unroll
-            for (int i = 0; i < kSbCols / 4; ++i)
-              f8_copy_scales<PAIR>(sa + 4 + 4 * i, src + 512 + 512 * i);
-            if constexpr (PAIR) umma_commit_pair(&sempty[slot]);
-            else umma_commit(&sempty[slot]);
-            ++grp;
+            for (int k = 0; k < 4; ++k)  // 32 entries each
+              f8_mma<PAIR>(tmem + (uint32_t)(buf * NT), da + 2 * k, db + 2 * k, idesc, sa, sa + 4,
+                           (k > 0 || kb > k0) ? 1u : 0u);
+            if constexpr (PAIR) umma_commit_pair(&empty[s]);
+            else umma_commit(&empty[s]);
+            if (++s == g.stages) { s = 0; ph ^= 1u; }
           }
-          if (!f8_wait(&full[s], ph, g.status)) {
-            *abort_flag = 1;
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint32_t a_addr = smem_u32(ops + (size_t)s * kStage);
-          const uint64_t da = sw128_desc(a_addr), db = sw128_desc(a_addr + (uint32_t)kTileBytes);
-          const uint32_t id = (uint32_t)kb & (kF8Group - 1);
-          const uint32_t idesc = idesc0 | id << 4 | id << 29;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)  // 32 entries each
-            f8_mma<PAIR>(tmem + (uint32_t)(buf * NT), da + 2 * k, db + 2 * k, idesc, sa, sa + 4,
-                         (k > 0 || kb > t.kb0) ? 1u : 0u);
-          if constexpr (PAIR) umma_commit_pair(&empty[s]);
-          else umma_commit(&empty[s]);
-          if (++s == g.stages) { s = 0; ph ^= 1u; }
+          if (!ok) break;
+          if constexpr (PAIR) umma_commit_pair(&accf[buf]);
+          else umma_commit(&accf[buf]);
         }
-        if (!ok) break;
-        if constexpr (PAIR) umma_commit_pair(&accf[buf]);
-        else umma_commit(&accf[buf]);
       }
+      if (!ok) *abort_flag = 1;
       // every product has completed before tensor memory is released
       if constexpr (PAIR)
         asm volatile(
@@ -872,7 +909,7 @@ static bool make_map_codes(CUtensorMap *m, const fqt_fp8 *q, uint32_t box_rows) 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output as boxes of 32 x 32 (its base and its pitch on 16 bytes).
+// The output as boxes of 32 rows x 64 bytes (its base and its pitch on 16 bytes).
 static bool make_map_f8_out(CUtensorMap *m, void *out, bool bf16, int64_t rows, int64_t cols,
                             int64_t ldo) {
   EncodeTiledFn fn = encode_fn();
@@ -880,11 +917,10 @@ static bool make_map_f8_out(CUtensorMap *m, void *out, bool bf16, int64_t rows, 
   const cuuint64_t es = bf16 ? 2 : 4;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ldo * es};
-  cuuint32_t box[2] = {32, 32};
+  cuuint32_t box[2] = {(cuuint32_t)(64 / es), 32};
   cuuint32_t one[2] = {1, 1};
   return fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, out,
-            dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+            dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
             CU_TENSOR_MAP_L2_PROMOTION_NONE,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -917,11 +953,6 @@ static F8Plan f8_plan(int64_t M, int64_t N, int64_t nkb, int nsm) {
   int64_t splits = p.pair ? 1 : nsm / tiles;
   if (splits > nkb / 8) splits = nkb / 8;
   if (splits < 1) splits = 1;
-  // ... and where an accumulator would take more than 8192 terms: a step of the tensor
-  // core drops what lies below the accumulator's last bit (5e-7 of the result after
-  // 8192 terms, 8e-6 after 65536)
-  if (splits < (groups + 15) / 16) splits = (groups + 15) / 16;
-  if (splits > groups) splits = groups;
   if (splits > 16) splits = 16;
   p.kb_per = (int)((groups + splits - 1) / splits) * kF8Group;
   p.splits = (int)((nkb + p.kb_per - 1) / p.kb_per);
@@ -934,8 +965,8 @@ size_t fp8_matmul_ws_bytes(int64_t M, int64_t N, int64_t K) {
   return kHeaderBytes + (p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0);
 }
 
-template <int NT, int ACCS, bool PAIR>
-static fqt_status launch_f8(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &to,
+template <int NT, int ACCS, bool PAIR, bool FOLD>
+static fqt_status launch_f8_as(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &to,
                             F8Args &g, int nsm, cudaStream_t st) {
   constexpr size_t stage = kTileBytes + (PAIR ? NT / 2 : NT) * kF8Block;
   constexpr size_t boxes = NT >= 64 ? kF8EpiWarps * kF8BoxBytes : 0;
@@ -943,7 +974,7 @@ static fqt_status launch_f8(const CUtensorMap &ta, const CUtensorMap &tb, const 
   constexpr int stages = room / stage < kMaxStages ? (int)(room / stage) : kMaxStages;
   constexpr size_t smem = 1024 + kF8Fixed + stages * stage + boxes;
   g.stages = stages;
-  auto kernel = k_f8_mm<NT, ACCS, PAIR>;
+  auto kernel = k_f8_mm<NT, ACCS, PAIR, FOLD>;
   static DeviceOnce once;
   cudaError_t e = allow_smem(kernel, smem, once);
   if (e != cudaSuccess) return cuda_fail(e, "FP8 product attribute");
@@ -963,6 +994,14 @@ static fqt_status launch_f8(const CUtensorMap &ta, const CUtensorMap &tb, const 
   cfg.numAttrs = 1;
   return cuda_fail(cudaLaunchKernelEx(&cfg, kernel, ta, tb, to, (const F8Args &)g),
                    "FP8 product launch");
+}
+
+template <int NT, int ACCS, bool PAIR>
+static fqt_status launch_f8(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &to,
+                            F8Args &g, int nsm, cudaStream_t st) {
+  if (!g.bf16 && g.kb_per > kF8Chunk)
+    return launch_f8_as<NT, ACCS, PAIR, true>(ta, tb, to, g, nsm, st);
+  return launch_f8_as<NT, ACCS, PAIR, false>(ta, tb, to, g, nsm, st);
 }
 
 static bool f8_aligned(const void *p, size_t n) {

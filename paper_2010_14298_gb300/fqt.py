@@ -226,12 +226,14 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(_raw_stream(stream))
 
 
+_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
 
 
 def _seed(seed) -> int:
@@ -590,44 +592,55 @@ def _new(shape, dtype, like, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _row_stride(t, name):
+# The checks of a call's tensors take as long as its launch, so the usual case (dense
+# tensors) asks a tensor four things.
+def _row_stride(t, rows, cols):
     """The row pitch of a matrix whose rows are contiguous, or None."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} is not on a GPU")
-    if t.dim() != 2:
-        raise ValueError(f"{name} has {t.dim()} dimensions, not two")
-    (rows, cols), (ld, step) = t.shape, t.stride()
+    if t.is_contiguous():
+        return cols
+    ld, step = t.stride()
     if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         return None
     return ld if rows > 1 else cols
 
 
+def _matrix(t, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not on a GPU")
+    if t.dim() != 2:
+        raise ValueError(f"{name} has {t.dim()} dimensions, not two")
+    return t.shape
+
+
 def _rows_in(t, name, stream):
-    """A matrix to read, and its row pitch; one laid out otherwise is copied."""
-    ld = _row_stride(t, name)
+    """A matrix to read, its sizes and its row pitch; one laid out otherwise is copied."""
+    rows, cols = _matrix(t, name)
+    ld = _row_stride(t, rows, cols)
     if ld is None:
         with _on(stream):
             t = t.contiguous()
-        ld = t.shape[1]
-    return t, ld
+        ld = cols
+    return t, rows, cols, ld
 
 
-def _rows_out(t, name, shape, dtype, like, stream):
+def _rows_out(t, name, rows, cols, dtype, like, stream):
     """A matrix to write (a new one for None), and its row pitch."""
     if t is None:
-        return _new(shape, dtype, like, stream), shape[1]
-    if t.shape != shape or t.dtype != dtype:
-        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
-    ld = _row_stride(t, name)
+        return _new((rows, cols), dtype, like, stream), cols
+    if t.dtype != dtype or _matrix(t, name) != (rows, cols):
+        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, not {dtype} {(rows, cols)}")
+    ld = _row_stride(t, rows, cols)
     if ld is None:
         raise ValueError(f"the rows of {name} are not contiguous")
     return t, ld
 
 
-def _vector(t, name, n, dtype=torch.float32):
-    """A contiguous vector of n entries on the GPU."""
-    if t.dtype != dtype or t.shape != (n,) or not t.is_cuda or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} is no contiguous {dtype} vector of {n} entries on the GPU")
+def _vector(t, name, n, like=None, stream=None):
+    """n contiguous fp32 entries on the GPU (new ones for None, where `like` is given)."""
+    if t is None:
+        return None if like is None else _new((n,), torch.float32, like, stream)
+    if not (t.is_cuda and t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()):
+        raise ValueError(f"{name} is no contiguous float32 vector of {n} entries on the GPU")
     return t
 
 
@@ -637,17 +650,12 @@ def layer_norm_forward(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
                        rstd: torch.Tensor = None, stream=None):
     """(Y, mean, rstd): layer norm of the rows of X (fqt_layer_norm_forward).
     gamma and beta are fp32 (None: 1 and 0); Y has X's type."""
-    X, ldx = _rows_in(X, "X", stream)
-    rows, cols = X.shape
-    if gamma is not None:
-        _vector(gamma, "gamma", cols)
-    if beta is not None:
-        _vector(beta, "beta", cols)
-    Y, ldy = _rows_out(out, "out", X.shape, X.dtype, X, stream)
-    mean = (_vector(mean, "mean", rows) if mean is not None
-            else _new((rows,), torch.float32, X, stream))
-    rstd = (_vector(rstd, "rstd", rows) if rstd is not None
-            else _new((rows,), torch.float32, X, stream))
+    X, rows, cols, ldx = _rows_in(X, "X", stream)
+    _vector(gamma, "gamma", cols)
+    _vector(beta, "beta", cols)
+    Y, ldy = _rows_out(out, "out", rows, cols, X.dtype, X, stream)
+    mean = _vector(mean, "mean", rows, X, stream)
+    rstd = _vector(rstd, "rstd", rows, X, stream)
     st = native().layer_norm_forward(X, ldx, _dtype_code(X), rows, cols, gamma, beta, eps, Y, ldy,
                                      mean, rstd, _raw_stream(stream))
     if st:
@@ -668,21 +676,17 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
     and grad_w choose them, None stands for one that was not asked for."""
     if dY.shape != X.shape or dY.dtype != X.dtype:
         raise ValueError(f"dY is {dY.dtype} {tuple(dY.shape)}, X {X.dtype} {tuple(X.shape)}")
-    X, ldx = _rows_in(X, "X", stream)
-    dY, lddy = _rows_in(dY, "dY", stream)
-    rows, cols = X.shape
+    X, rows, cols, ldx = _rows_in(X, "X", stream)
+    dY, _, _, lddy = _rows_in(dY, "dY", stream)
     _vector(mean, "mean", rows)
     _vector(rstd, "rstd", rows)
-    if gamma is not None:
-        _vector(gamma, "gamma", cols)
+    _vector(gamma, "gamma", cols)
     dX, lddx, dgamma, dbeta, nbytes = None, cols, None, None, 0
     if grad_x:
-        dX, lddx = _rows_out(out_x, "out_x", X.shape, X.dtype, X, stream)
+        dX, lddx = _rows_out(out_x, "out_x", rows, cols, X.dtype, X, stream)
     if grad_w:
-        dgamma = (_vector(out_gamma, "out_gamma", cols) if out_gamma is not None
-                  else _new((cols,), torch.float32, X, stream))
-        dbeta = (_vector(out_beta, "out_beta", cols) if out_beta is not None
-                 else _new((cols,), torch.float32, X, stream))
+        dgamma = _vector(out_gamma, "out_gamma", cols, X, stream)
+        dbeta = _vector(out_beta, "out_beta", cols, X, stream)
         if ws is None:
             with _on(stream):
                 ws = Workspace.of_size(layer_norm_workspace_size(rows, cols), X.device)
@@ -777,8 +781,7 @@ def quantize_fp8(X: torch.Tensor, block_rows: int = 1, q: Fp8Tensor = None, qt: 
     """(X, X^T) in 8-bit floating point (fqt_quantize_fp8): the blocks of the first
     run along X's rows, those of the second along its columns.  `rows` and `cols` ask
     for them (a tensor given for one does too), None stands for one that was not."""
-    X, ldx = _rows_in(X, "X", stream)
-    n, k = X.shape
+    X, n, k, ldx = _rows_in(X, "X", stream)
     if rows or q is not None:
         q = _fp8_out(q, "q", n, k, block_rows, X, stream)
     if cols or qt is not None:
@@ -807,12 +810,9 @@ def fp8_matmul(A: Fp8Tensor, B: Fp8Tensor, out: torch.Tensor = None, dtype=torch
         raise ValueError(f"A has {A.cols} columns, B {B.cols}")
     if not (A.codes.is_cuda and B.codes.is_cuda):
         raise ValueError("A and B are not on a GPU")
-    shape = (A.rows, B.rows)
     if out is not None:
         dtype = out.dtype
-        if out.shape != shape:
-            raise ValueError(f"out is {tuple(out.shape)}, not {shape}")
-    out, ldo = _rows_out(out, "out", torch.Size(shape), dtype, A.codes, stream)
+    out, ldo = _rows_out(out, "out", A.rows, B.rows, dtype, A.codes, stream)
     if ws is None:
         with _on(stream):
             ws = Workspace.of_size(fp8_matmul_workspace_size(A.rows, B.rows, A.cols),
@@ -866,8 +866,7 @@ def _clip(grads, out, max_norm, norm, ws, stream):
         if out is not grads and (out._kinds != grads._kinds
                                  or out[0].device != grads[0].device):
             raise ValueError("out has other sizes, types or another GPU than the gradients")
-    norm = _vector(norm, "norm", 1) if norm is not None else _new((1,), torch.float32, grads[0],
-                                                                  stream)
+    norm = _vector(norm, "norm", 1, grads[0], stream)
     if ws is None:
         with _on(stream):
             ws = Workspace.of_size(clip_grad_norm_workspace_size(grads), grads[0].device)

@@ -180,15 +180,45 @@ __device__ __forceinline__ float one_entry(const char *p, int i, bool bf16) {
   return reinterpret_cast<const float *>(p)[i];
 }
 
-template <int PER>
+// Cache policies: entries that the second pass reads again are to stay in L2, what it
+// reads and writes is not (49.3 -> 47.5 us for a ResNet-50, 12.1 -> 10.9 for an FFN in
+// bf16).  Only where the output lies apart: in place there may be no second reading, and
+// the entries would stay for nobody.
+__device__ __forceinline__ uint64_t keep_policy() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint64_t pass_policy() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint4 load_as(const uint4 *p, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p), "l"(policy)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_as(uint4 *p, const uint4 &v, uint64_t policy) {
+  asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x),
+               "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy)
+               : "memory");
+}
+
+template <int PER, bool APART>
 __device__ __forceinline__ void add_unit(Squares &s, const ClipUnit &u) {
   const bool bf16 = PER == 8;
+  const uint64_t policy = keep_policy();
   const uint4 *body = reinterpret_cast<const uint4 *>(u.in + u.head * (16 / PER));
   uint4 v[kClipVecs];
 #pragma unroll
   for (int k = 0; k < kClipVecs; ++k) {
     const int i = k * kClipThreads + threadIdx.x;
-    v[k] = i < u.nvec ? __ldg(body + i) : make_uint4(0u, 0u, 0u, 0u);
+    v[k] = make_uint4(0u, 0u, 0u, 0u);
+    if (i < u.nvec) v[k] = APART ? load_as(body + i, policy) : __ldg(body + i);
   }
   float sum = 0.0f;
 #pragma unroll
@@ -207,7 +237,7 @@ __device__ __forceinline__ void add_unit(Squares &s, const ClipUnit &u) {
 }
 
 // part[CTA]: the sum of its units' squares.
-template <int CAP>
+template <int CAP, bool APART>
 __global__ void __launch_bounds__(kClipThreads, kClipCtas)
     k_clip_squares(const __grid_constant__ ClipTable<CAP> t, float4 *part) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -216,8 +246,8 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
   for (uint32_t unit = blockIdx.x; unit < t.units; unit += gridDim.x) {
     if (e + 1 < t.n && t.e[e + 1].unit0 <= unit) e = clip_entry(t, e + 1, t.n - 1, unit);
     const ClipUnit u = clip_unit(t.e[e], unit);
-    if (u.bf16) add_unit<8>(s, u);
-    else add_unit<4>(s, u);
+    if (u.bf16) add_unit<8, APART>(s, u);
+    else add_unit<4, APART>(s, u);
   }
   s = cta_sum(s);
   if (threadIdx.x == 0) part[blockIdx.x] = make_float4(s.mid.h, s.mid.l, s.small, s.big);
@@ -250,7 +280,7 @@ __device__ __forceinline__ float clip_factor(const float4 *part, int nparts, flo
   return factor;
 }
 
-template <int PER>
+template <int PER, bool APART>
 __device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
   const bool bf16 = PER == 8;
   // vectors where the output lies on the same bytes of 16 as the input
@@ -259,11 +289,12 @@ __device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
   const int head = vec ? u.head : 0, nvec = vec ? u.nvec : 0;
   const uint4 *in = reinterpret_cast<const uint4 *>(u.in + head * (16 / PER));
   uint4 *out = reinterpret_cast<uint4 *>(u.out + head * (16 / PER));
+  const uint64_t policy = pass_policy();
   uint4 v[kClipVecs];
 #pragma unroll
   for (int k = 0; k < kClipVecs; ++k) {
     const int i = k * kClipThreads + threadIdx.x;
-    if (i < nvec) v[k] = in[i];
+    if (i < nvec) v[k] = APART ? load_as(in + i, policy) : in[i];
   }
 #pragma unroll
   for (int k = 0; k < kClipVecs; ++k) {
@@ -281,7 +312,9 @@ __device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
         w[j] = __float_as_uint(x[j] * f);
       }
     }
-    out[i] = f == 1.0f ? v[k] : make_uint4(w[0], w[1], w[2], w[3]);
+    const uint4 y = f == 1.0f ? v[k] : make_uint4(w[0], w[1], w[2], w[3]);
+    if constexpr (APART) store_as(out + i, y, policy);
+    else out[i] = y;
   }
   // the ends, or a unit without vectors
   const int rest = u.count - nvec * PER;
@@ -299,7 +332,7 @@ __device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
   }
 }
 
-template <int CAP>
+template <int CAP, bool APART>
 __global__ void __launch_bounds__(kClipThreads, kClipCtas)
     k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const float4 *part, int nparts,
                  float max_norm, float *norm_out, int *status) {
@@ -313,8 +346,8 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
     if (t.e[e].unit0 > unit) e = clip_entry(t, 0, e - 1, unit);
     if (f == 1.0f && t.e[e].in == t.e[e].out) continue;  // nothing to change in place
     const ClipUnit u = clip_unit(t.e[e], unit);
-    if (u.bf16) scale_unit<8>(u, f);
-    else scale_unit<4>(u, f);
+    if (u.bf16) scale_unit<8, APART>(u, f);
+    else scale_unit<4, APART>(u, f);
   }
 }
 
@@ -367,7 +400,7 @@ static cudaError_t launch_after(int grid, cudaStream_t st, void (*kernel)(P...),
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <int CAP>
+template <int CAP, bool APART>
 static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_t n,
                              float max_norm, float *norm, void *ws, cudaStream_t st) {
   const int most = clip_grid(device_sm_count());
@@ -379,7 +412,7 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
     i = fill_table(t, in, out, i, n);
     if (t.units == 0) continue;
     const int grid = t.units < (uint32_t)most ? (int)t.units : most;
-    k_clip_squares<CAP><<<grid, kClipThreads, 0, st>>>(t, part + nparts);
+    k_clip_squares<CAP, APART><<<grid, kClipThreads, 0, st>>>(t, part + nparts);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, "gradient norm launch");
     nparts += grid;
@@ -396,12 +429,20 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
     if (t.units == 0) continue;
     const int grid = t.units < (uint32_t)most ? (int)t.units : most;
     // (a second list waits for the first one's scaling only, which waited for the sums)
-    const cudaError_t e = launch_after(grid, st, k_clip_scale<CAP>, t, (const float4 *)part,
+    const cudaError_t e = launch_after(grid, st, k_clip_scale<CAP, APART>, t, (const float4 *)part,
                                        nparts, max_norm, first ? norm : nullptr, status);
     if (e != cudaSuccess) return cuda_fail(e, "gradient clipping launch");
     first = false;
   }
   return FQT_OK;
+}
+
+template <bool APART>
+static fqt_status clip_as(const fqt_tensor *in, const fqt_tensor *out, int64_t n, float max_norm,
+                          float *norm, void *ws, cudaStream_t st) {
+  if (n <= kClipSmall) return clip_lists<kClipSmall, APART>(in, out, n, max_norm, norm, ws, st);
+  if (n <= kClipMid) return clip_lists<kClipMid, APART>(in, out, n, max_norm, norm, ws, st);
+  return clip_lists<kClipLarge, APART>(in, out, n, max_norm, norm, ws, st);
 }
 
 }  // namespace fqt
@@ -434,9 +475,10 @@ fqt_status fqt_clip_grad_norm(const fqt_tensor *grads, const fqt_tensor *out, in
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || ws_bytes < clip_ws_bytes(n))
     return FQT_EWORKSPACE;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (n <= kClipSmall) return clip_lists<kClipSmall>(grads, out, n, max_norm, norm, workspace, st);
-  if (n <= kClipMid) return clip_lists<kClipMid>(grads, out, n, max_norm, norm, workspace, st);
-  return clip_lists<kClipLarge>(grads, out, n, max_norm, norm, workspace, st);
+  bool apart = false;
+  for (int64_t i = 0; out && i < n; ++i) apart |= out[i].data != grads[i].data;
+  return apart ? clip_as<true>(grads, out, n, max_norm, norm, workspace, st)
+               : clip_as<false>(grads, out, n, max_norm, norm, workspace, st);
 }
 
 }  // extern "C"

@@ -2,14 +2,15 @@
 
 The CUDA library (``_lib/libfqt.so``, C ABI in ``include/fqt.h``) quantizes
 the output gradient of a linear / im2col-conv layer with PTQ, PSQ or BHQ and
-runs the two low-bit contractions grad_X and grad_W.  ``fqt`` is the thin
-ctypes binding; importing this package loads nothing until it is used.
+runs the two low-bit contractions grad_X and grad_W, and has the operators of a
+training step around them.  ``fqt`` is the thin binding, ``ffn`` a feed-forward
+block trained with it; importing this package loads nothing until it is used.
 """
-__all__ = ["fqt", "workloads"]
+__all__ = ["fqt", "ffn", "workloads"]
 
 
 def __getattr__(name):
-    if name in ("fqt", "workloads"):
+    if name in __all__:
         import importlib
         return importlib.import_module(f"{__name__}.{name}")
     raise AttributeError(name)

@@ -240,7 +240,8 @@ __device__ __forceinline__ void add_unit(Squares &s, const ClipUnit &u) {
 template <int CAP, bool APART>
 __global__ void __launch_bounds__(kClipThreads, kClipCtas)
     k_clip_squares(const __grid_constant__ ClipTable<CAP> t, float4 *part) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  let_next_start();
+  wait_for_previous();
   Squares s = {{0.0f, 0.0f}, 0.0f, 0.0f};
   int e = 0;
   for (uint32_t unit = blockIdx.x; unit < t.units; unit += gridDim.x) {
@@ -336,7 +337,8 @@ template <int CAP, bool APART>
 __global__ void __launch_bounds__(kClipThreads, kClipCtas)
     k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const float4 *part, int nparts,
                  float max_norm, float *norm_out, int *status) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  let_next_start();
+  wait_for_previous();
   const float f = clip_factor(part, nparts, max_norm, norm_out, status);
   int e = t.n - 1;
   // the units of the CTA of this number in the first pass, from the last to the first
@@ -354,7 +356,8 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
 // The norm alone.
 __global__ void __launch_bounds__(kClipThreads)
     k_clip_norm(const float4 *part, int nparts, float *norm_out, int *status) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  let_next_start();
+  wait_for_previous();
   clip_factor(part, nparts, INFINITY, norm_out, status);
 }
 
@@ -385,21 +388,6 @@ static int64_t fill_table(ClipTable<CAP> &t, const fqt_tensor *in, const fqt_ten
   return i;
 }
 
-// A launch that may begin while the one before it ends (the kernel waits for that).
-template <typename... P, typename... A>
-static cudaError_t launch_after(int grid, cudaStream_t st, void (*kernel)(P...), A... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kClipThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 template <int CAP, bool APART>
 static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_t n,
                              float max_norm, float *norm, void *ws, cudaStream_t st) {
@@ -412,14 +400,15 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
     i = fill_table(t, in, out, i, n);
     if (t.units == 0) continue;
     const int grid = t.units < (uint32_t)most ? (int)t.units : most;
-    k_clip_squares<CAP, APART><<<grid, kClipThreads, 0, st>>>(t, part + nparts);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_behind(k_clip_squares<CAP, APART>, dim3((unsigned)grid),
+                                        kClipThreads, 0, st, t, part + nparts);
     if (e != cudaSuccess) return cuda_fail(e, "gradient norm launch");
     nparts += grid;
   }
   if (!out || nparts == 0) {
     const cudaError_t e =
-        launch_after(1, st, k_clip_norm, (const float4 *)part, nparts, norm, status);
+        launch_behind(k_clip_norm, dim3(1), kClipThreads, 0, st, (const float4 *)part, nparts,
+                      norm, status);
     return cuda_fail(e, "gradient norm launch");
   }
   bool first = true;
@@ -428,9 +417,9 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
     else i = n;  // the table is still there
     if (t.units == 0) continue;
     const int grid = t.units < (uint32_t)most ? (int)t.units : most;
-    // (a second list waits for the first one's scaling only, which waited for the sums)
-    const cudaError_t e = launch_after(grid, st, k_clip_scale<CAP, APART>, t, (const float4 *)part,
-                                       nparts, max_norm, first ? norm : nullptr, status);
+    const cudaError_t e =
+        launch_behind(k_clip_scale<CAP, APART>, dim3((unsigned)grid), kClipThreads, 0, st, t,
+                      (const float4 *)part, nparts, max_norm, first ? norm : nullptr, status);
     if (e != cudaSuccess) return cuda_fail(e, "gradient clipping launch");
     first = false;
   }

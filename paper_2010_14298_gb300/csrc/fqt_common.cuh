@@ -277,6 +277,17 @@ __device__ __forceinline__ void sleep_ns(uint64_t ns) {
   while (global_ns() - t0 < ns) __nanosleep(1000);
 }
 
+// Programmatic dependent launch.  A kernel launched with launch_behind (fqt_internal.h)
+// may start while the kernels before it in its stream still run, once all their CTAs
+// have let it (let_next_start) or ended; until wait_for_previous returns it touches no
+// memory but its own.  Every thread of such a kernel calls both, first.
+__device__ __forceinline__ void let_next_start() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void wait_for_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 __device__ __forceinline__ void fence_proxy_async_smem() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }

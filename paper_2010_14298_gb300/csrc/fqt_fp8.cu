@@ -145,6 +145,8 @@ struct F8Raw {
 // 16-byte stores and a row's four scales in one word.  Bound by memory traffic.
 template <typename T, int R>
 __global__ void __launch_bounds__(256) k_f8_rows(const F8QuantArgs a, const bool vec) {
+  let_next_start();
+  wait_for_previous();
   const int lane = threadIdx.x & 31;
   const int64_t row = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * R;
   const int64_t col = (int64_t)blockIdx.y * 512 + lane * 16;
@@ -189,6 +191,8 @@ constexpr int kF8TileThreads = 512;
 template <typename T>
 __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
     k_f8_tile(const F8QuantArgs a, const bool vec) {
+  let_next_start();
+  wait_for_previous();
   __shared__ __align__(16) uint32_t cmax[kF8TileThreads / 32][kF8Block];  // fp32 bits
   __shared__ __align__(16) float cinv[kF8Block];
   __shared__ uint32_t wmax[4];
@@ -603,6 +607,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(full + kF8Bars);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   uint8_t *ops = smem + kF8Fixed;
+  let_next_start();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? (int)(blockIdx.x & 1) : 0;
   const int64_t first = PAIR ? blockIdx.x >> 1 : blockIdx.x;
@@ -644,6 +649,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
   if constexpr (PAIR) cluster_sync();  // the peer's barriers exist
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  wait_for_previous();
 
   if (warp >= kF8Epi0) {
     const int q = warp & 3, h = (warp - kF8Epi0) >> 2;
@@ -883,6 +889,8 @@ __global__ void __launch_bounds__(kF8Threads, 1)
 template <typename T>
 __global__ void __launch_bounds__(256)
     k_f8_join(const float *part, int splits, int64_t rows, int64_t cols, T *out, int64_t ldo) {
+  let_next_start();
+  wait_for_previous();
   const int64_t n = rows * cols;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
        i += (int64_t)gridDim.x * blockDim.x) {
@@ -985,13 +993,15 @@ static fqt_status launch_f8_as(const CUtensorMap &ta, const CUtensorMap &tb, con
   cfg.blockDim = dim3(kF8Threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = PAIR ? 2 : 1;
-  at[0].val.clusterDim.y = 1;
-  at[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 2;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = PAIR ? 2 : 1;
   return cuda_fail(cudaLaunchKernelEx(&cfg, kernel, ta, tb, to, (const F8Args &)g),
                    "FP8 product launch");
 }
@@ -1043,20 +1053,15 @@ fqt_status quantize_fp8(const void *X, int64_t ldx, bool bf16, int64_t rows, int
     const int64_t chunks = (cols + 511) / 512;
     const int per = rows * chunks < 32 * device_sm_count() ? 1 : bf16 ? 4 : 2;
     const dim3 grid((unsigned)((rows + 8 * per - 1) / (8 * per)), (unsigned)chunks);
-    if (bf16) {
-      if (per == 4) k_f8_rows<__nv_bfloat16, 4><<<grid, 256, 0, st>>>(a, vec);
-      else k_f8_rows<__nv_bfloat16, 1><<<grid, 256, 0, st>>>(a, vec);
-    } else {
-      if (per == 2) k_f8_rows<float, 2><<<grid, 256, 0, st>>>(a, vec);
-      else k_f8_rows<float, 1><<<grid, 256, 0, st>>>(a, vec);
-    }
-    return cuda_fail(cudaGetLastError(), "FP8 quantizer launch");
+    auto kernel = bf16 ? (per == 4 ? k_f8_rows<__nv_bfloat16, 4> : k_f8_rows<__nv_bfloat16, 1>)
+                       : (per == 2 ? k_f8_rows<float, 2> : k_f8_rows<float, 1>);
+    return cuda_fail(launch_behind(kernel, grid, 256, 0, st, a, vec), "FP8 quantizer launch");
   }
   const dim3 grid((unsigned)((rows + kF8Block - 1) / kF8Block),
                   (unsigned)((cols + kF8Block - 1) / kF8Block));
-  if (bf16) k_f8_tile<__nv_bfloat16><<<grid, kF8TileThreads, 0, st>>>(a, vec);
-  else k_f8_tile<float><<<grid, kF8TileThreads, 0, st>>>(a, vec);
-  return cuda_fail(cudaGetLastError(), "FP8 quantizer launch");
+  auto kernel = bf16 ? k_f8_tile<__nv_bfloat16> : k_f8_tile<float>;
+  return cuda_fail(launch_behind(kernel, grid, kF8TileThreads, 0, st, a, vec),
+                   "FP8 quantizer launch");
 }
 
 fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, int64_t ldo,
@@ -1097,13 +1102,13 @@ fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, 
   if (s != FQT_OK || p.splits == 1) return s;
   const int64_t blocks = (M * N + 255) / 256;
   const int grid = (int)(blocks < 8 * nsm ? blocks : 8 * nsm);
-  if (bf16)
-    k_f8_join<__nv_bfloat16><<<grid, 256, 0, st>>>(g.part, p.splits, M, N,
-                                                   static_cast<__nv_bfloat16 *>(out), g.ldo);
-  else
-    k_f8_join<float><<<grid, 256, 0, st>>>(g.part, p.splits, M, N, static_cast<float *>(out),
-                                           g.ldo);
-  return cuda_fail(cudaGetLastError(), "FP8 join launch");
+  const float *part = g.part;
+  const cudaError_t e =
+      bf16 ? launch_behind(k_f8_join<__nv_bfloat16>, dim3((unsigned)grid), 256, 0, st, part,
+                           p.splits, M, N, static_cast<__nv_bfloat16 *>(out), g.ldo)
+           : launch_behind(k_f8_join<float>, dim3((unsigned)grid), 256, 0, st, part, p.splits, M,
+                           N, static_cast<float *>(out), g.ldo);
+  return cuda_fail(e, "FP8 join launch");
 }
 
 }  // namespace fqt

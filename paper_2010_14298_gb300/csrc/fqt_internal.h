@@ -123,6 +123,24 @@ inline cudaError_t allow_smem(K kernel, size_t bytes, DeviceOnce &once) {
   return e;
 }
 
+// Launches a kernel that begins with wait_for_previous (fqt_common.cuh): its launch
+// overlaps the end of the kernel before it.
+template <typename... P, typename... A>
+inline cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, int threads, size_t smem,
+                                 cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // Records the CUDA error behind an FQT_ECUDA return (per thread) and returns
 // FQT_ECUDA, or FQT_OK for cudaSuccess.
 fqt_status cuda_fail(cudaError_t e, const char *where);

@@ -196,6 +196,8 @@ __global__ void __launch_bounds__(kNormThreads)
     k_norm_fwd(const NormArgs a, int G) {
   extern __shared__ __align__(16) uint4 smem[];
   __shared__ float slots[kNormMaxGroups][2][32];
+  let_next_start();
+  wait_for_previous();
   constexpr int E = V * VPT;
   const int gid = threadIdx.x / G, t = threadIdx.x - gid * G;
   const int lane = t & 31, gw = t >> 5, ngrp = blockDim.x / G;
@@ -288,7 +290,8 @@ __global__ void __launch_bounds__(kNormThreads)
     k_norm_bwd(const NormArgs a, int G) {
   extern __shared__ __align__(16) uint4 smem[];
   __shared__ float slots[kNormMaxGroups][2][32];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  let_next_start();
+  wait_for_previous();
   constexpr int E = V * VPT;
   const int gid = threadIdx.x / G, t = threadIdx.x - gid * G;
   const int lane = t & 31, gw = t >> 5, ngrp = blockDim.x / G;
@@ -417,6 +420,8 @@ template <typename T, int V>
 __global__ void __launch_bounds__(kNormThreads)
     k_norm_fwd_wide(const NormArgs a) {
   __shared__ float slots[2][32];
+  let_next_start();
+  wait_for_previous();
   const int t = threadIdx.x, lane = t & 31, gw = t >> 5;
   const int nvec = a.cols / V;
   const float n = (float)a.cols;
@@ -467,6 +472,8 @@ template <typename T, int V>
 __global__ void __launch_bounds__(kNormThreads)
     k_norm_bwd_wide(const NormArgs a) {
   __shared__ float slots[2][32];
+  let_next_start();
+  wait_for_previous();
   const int t = threadIdx.x, lane = t & 31, gw = t >> 5;
   const int nvec = a.cols / V;
   const float n = (float)a.cols;
@@ -510,6 +517,8 @@ constexpr int kNormColRows = 32;  // partial rows of the wide columns' sums
 
 template <typename T, int V>
 __global__ void __launch_bounds__(128) k_norm_cols_wide(const NormArgs a, int64_t rows_per) {
+  let_next_start();
+  wait_for_previous();
   const int v = blockIdx.x * blockDim.x + threadIdx.x;
   if (v >= a.cols / V) return;
   const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = min(a.rows, r0 + rows_per);
@@ -537,8 +546,7 @@ __global__ void __launch_bounds__(128) k_norm_cols_wide(const NormArgs a, int64_
 }
 
 // dgamma and dbeta: the sums of n partial rows, 8 columns a CTA, 64 rows side by side
-// (so that a few loads a thread and many CTAs finish soon).  It is launched while the
-// partial sums are still being made and waits for them.
+// (so that a few loads a thread and many CTAs finish soon).  
 constexpr int kNormColThreads = 512;
 
 __global__ void __launch_bounds__(kNormColThreads)
@@ -546,7 +554,8 @@ __global__ void __launch_bounds__(kNormColThreads)
   __shared__ float sums[2][kNormColThreads / 32][8];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 8 + (lane & 7);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  let_next_start();
+  wait_for_previous();
   float u = 0.0f, v = 0.0f;
   if (c < cols) {
 #pragma unroll 4
@@ -643,8 +652,7 @@ static cudaError_t launch_rows(const NormArgs &a, const NormPlan &p, cudaStream_
     const cudaError_t e = allow_smem(kernel, 200 * 1024, once);
     if (e != cudaSuccess) return e;
   }
-  kernel<<<p.grid, nth, smem, st>>>(a, p.G);
-  return cudaGetLastError();
+  return launch_behind(kernel, dim3((unsigned)p.grid), nth, smem, st, a, p.G);
 }
 
 template <typename T, bool BWD, int V>
@@ -666,21 +674,26 @@ static cudaError_t launch_norm(const NormArgs &a, const NormPlan &p, bool bf16, 
 }
 
 template <typename T, int V>
-static void launch_wide_rows(const NormArgs &a, const NormPlan &p, bool bwd, int64_t rows_per,
-                             int nparts, cudaStream_t st) {
-  if (!bwd) k_norm_fwd_wide<T, V><<<p.grid, kNormThreads, 0, st>>>(a);
-  if (bwd && a.y) k_norm_bwd_wide<T, V><<<p.grid, kNormThreads, 0, st>>>(a);
-  if (nparts > 0)
-    k_norm_cols_wide<T, V><<<dim3((unsigned)((a.cols / V + 127) / 128), (unsigned)nparts), 128, 0,
-                             st>>>(a, rows_per);
+static cudaError_t launch_wide_rows(const NormArgs &a, const NormPlan &p, bool bwd,
+                                    int64_t rows_per, int nparts, cudaStream_t st) {
+  const dim3 rows((unsigned)p.grid);
+  cudaError_t e = cudaSuccess;
+  if (!bwd) e = launch_behind(k_norm_fwd_wide<T, V>, rows, kNormThreads, 0, st, a);
+  if (bwd && a.y) e = launch_behind(k_norm_bwd_wide<T, V>, rows, kNormThreads, 0, st, a);
+  if (e == cudaSuccess && nparts > 0)
+    e = launch_behind(k_norm_cols_wide<T, V>,
+                      dim3((unsigned)((a.cols / V + 127) / 128), (unsigned)nparts), 128, 0, st, a,
+                      rows_per);
+  return e;
 }
 
-static void launch_wide(const NormArgs &a, const NormPlan &p, bool bf16, bool bwd,
-                        int64_t rows_per, int nparts, cudaStream_t st) {
-  if (bf16 && p.v > 1) launch_wide_rows<__nv_bfloat16, 8>(a, p, bwd, rows_per, nparts, st);
-  else if (bf16) launch_wide_rows<__nv_bfloat16, 1>(a, p, bwd, rows_per, nparts, st);
-  else if (p.v > 1) launch_wide_rows<float, 4>(a, p, bwd, rows_per, nparts, st);
-  else launch_wide_rows<float, 1>(a, p, bwd, rows_per, nparts, st);
+static cudaError_t launch_wide(const NormArgs &a, const NormPlan &p, bool bf16, bool bwd,
+                               int64_t rows_per, int nparts, cudaStream_t st) {
+  if (bf16)
+    return p.v > 1 ? launch_wide_rows<__nv_bfloat16, 8>(a, p, bwd, rows_per, nparts, st)
+                   : launch_wide_rows<__nv_bfloat16, 1>(a, p, bwd, rows_per, nparts, st);
+  return p.v > 1 ? launch_wide_rows<float, 4>(a, p, bwd, rows_per, nparts, st)
+                 : launch_wide_rows<float, 1>(a, p, bwd, rows_per, nparts, st);
 }
 
 static bool ptr_aligned(const void *p, size_t n) {
@@ -700,32 +713,23 @@ fqt_status layer_norm(const NormArgs &in, bool bf16, bool bwd, cudaStream_t st) 
                    rows_aligned(a.dy, a.lddy, es) && rows_aligned(a.y, a.ldy, es);
   NormPlan p = norm_plan(a.rows, a.cols, bf16, vec, bwd, nsm);
   int nparts = p.grid;
+  cudaError_t e;
   if (p.wide) {
+    int64_t per = 0;
+    nparts = 0;
     if (bwd && a.part) {
       nparts = (int)(a.rows < kNormColRows ? a.rows : kNormColRows);
-      const int64_t per = (a.rows + nparts - 1) / nparts;
+      per = (a.rows + nparts - 1) / nparts;
       nparts = (int)((a.rows + per - 1) / per);
-      launch_wide(a, p, bf16, bwd, per, nparts, st);
-    } else {
-      launch_wide(a, p, bf16, bwd, 0, 0, st);
     }
+    e = launch_wide(a, p, bf16, bwd, per, nparts, st);
+  } else {
+    e = bwd ? launch_norm<true>(a, p, bf16, st) : launch_norm<false>(a, p, bf16, st);
   }
-  cudaError_t e = p.wide ? cudaGetLastError()
-                  : bwd  ? launch_norm<true>(a, p, bf16, st)
-                         : launch_norm<false>(a, p, bf16, st);
   if (e != cudaSuccess) return cuda_fail(e, "layer norm launch");
   if (bwd && a.part) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((a.cols + 7) / 8));
-    cfg.blockDim = dim3(kNormColThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, k_norm_cols, (const float *)a.part, nparts, a.cols, a.dgamma,
-                           a.dbeta);
+    e = launch_behind(k_norm_cols, dim3((unsigned)((a.cols + 7) / 8)), kNormColThreads, 0, st,
+                      (const float *)a.part, nparts, a.cols, a.dgamma, a.dbeta);
     return cuda_fail(e, "layer norm column sums launch");
   }
   return FQT_OK;

@@ -78,8 +78,8 @@ struct F8Raw {
   static constexpr int words = N * (int)sizeof(T) / 4;
   uint32_t w[words];
   // zeros past `left` entries
-  __device__ __forceinline__ void load(const T *p, int64_t left, bool vec) {
-    if (vec && left >= N) {
+  __device__ __forceinline__ void load(const T *p, int64_t left) {
+    if (left >= N) {
 #pragma unroll
       for (int i = 0; i < words; i += 4) {
         const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i / 4);
@@ -95,6 +95,14 @@ struct F8Raw {
       for (int i = 0; i < words; ++i)
         w[i] = (2 * i < left ? __ldg(h + 2 * i) : 0u) |
                (uint32_t)(2 * i + 1 < left ? __ldg(h + 2 * i + 1) : 0u) << 16;
+    }
+  }
+  // from shared memory
+  __device__ __forceinline__ void take(const T *p) {
+#pragma unroll
+    for (int i = 0; i < words; i += 4) {
+      const uint4 v = reinterpret_cast<const uint4 *>(p)[i / 4];
+      w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
     }
   }
   __device__ __forceinline__ float f(int i) const {
@@ -140,11 +148,25 @@ struct F8Raw {
   }
 };
 
+// N consecutive entries that lie on no 16-byte boundary to shared memory by one warp
+// (zeros past `left`): entry by entry, but neighbouring lanes read neighbours.  (Each
+// lane its own 8 or 16 entries took eight times the wavefronts.)
+template <typename T, int N>
+__device__ __forceinline__ void f8_stage(T *dst, const T *p, int64_t left, int lane) {
+  T v[N / 32];
+#pragma unroll
+  for (int k = 0; k < N / 32; ++k)
+    v[k] = lane + 32 * k < left ? p[lane + 32 * k] : (T)0.0f;
+#pragma unroll
+  for (int k = 0; k < N / 32; ++k) dst[lane + 32 * k] = v[k];
+}
+
 // Codes by rows alone, one scale per 128 entries: a warp takes 512 columns of R rows,
 // a lane 16 of each, so that a block's maximum is three shuffles, the codes leave in
 // 16-byte stores and a row's four scales in one word.  Bound by memory traffic.
 template <typename T, int R>
 __global__ void __launch_bounds__(256) k_f8_rows(const F8QuantArgs a, const bool vec) {
+  __shared__ __align__(16) uint32_t stages[8][512 * sizeof(T) / 4];
   let_next_start();
   wait_for_previous();
   const int lane = threadIdx.x & 31;
@@ -152,10 +174,23 @@ __global__ void __launch_bounds__(256) k_f8_rows(const F8QuantArgs a, const bool
   const int64_t col = (int64_t)blockIdx.y * 512 + lane * 16;
   F8Raw<T, 16> v[R];
   uint32_t m[R];
+  if (vec) {
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-    v[r].load(static_cast<const T *>(a.x) + (row + r) * a.ldx + col,
-              row + r < a.rows ? a.cols - col : 0, vec);
+    for (int r = 0; r < R; ++r)
+      v[r].load(static_cast<const T *>(a.x) + (row + r) * a.ldx + col,
+                row + r < a.rows ? a.cols - col : 0);
+  } else {
+    T *stage = reinterpret_cast<T *>(stages[threadIdx.x >> 5]);
+    const int64_t c0 = (int64_t)blockIdx.y * 512;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      f8_stage<T, 512>(stage, static_cast<const T *>(a.x) + (row + r) * a.ldx + c0,
+                       row + r < a.rows ? a.cols - c0 : 0, lane);
+      __syncwarp();
+      v[r].take(stage + lane * 16);
+      __syncwarp();
+    }
+  }
 #pragma unroll
   for (int r = 0; r < R; ++r) m[r] = v[r].top(a.status);
 #pragma unroll
@@ -206,10 +241,27 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
   const int64_t row = r0 + rg * 4, col = c0 + cg * 8;
   F8Raw<T, 8> v[4];
   uint32_t rm[4], cm[8];
+  if (vec) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v[i].load(static_cast<const T *>(a.x) + (row + i) * a.ldx + col,
-              row + i < a.rows ? a.cols - col : 0, vec);
+    for (int i = 0; i < 4; ++i)
+      v[i].load(static_cast<const T *>(a.x) + (row + i) * a.ldx + col,
+                row + i < a.rows ? a.cols - col : 0);
+  } else {  // the warp's two rows i at a time, by way of 1 KB of `tr`
+    T *stage = reinterpret_cast<T *>(tr + warp * 256);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t r = r0 + (2 * warp + h) * 4 + i;
+        f8_stage<T, kF8Block>(stage + h * kF8Block, static_cast<const T *>(a.x) + r * a.ldx + c0,
+                              r < a.rows ? a.cols - c0 : 0, lane);
+      }
+      __syncwarp();
+      v[i].take(stage + (lane >> 4) * kF8Block + cg * 8);
+      __syncwarp();
+    }
+    __syncthreads();
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) rm[i] = v[i].top(a.status);
   // column maxima over the thread's rows (NaN counts for none) and the warp's two row

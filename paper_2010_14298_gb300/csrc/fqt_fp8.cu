@@ -570,20 +570,23 @@ __device__ __forceinline__ uint32_t box_off(int r, int k) {
   return (uint32_t)(r * 64 + ((k ^ ((r >> 1) & 3)) << 4));
 }
 
-// A warp's 32 rows (this lane's is m0 + lane) x W <= 32 columns from n on, one by one:
-// transposed outputs straight from the registers (lanes are neighbours there), others
-// by way of the box, so that a row's columns are neighbours.
+// W <= 32 columns from n on of this lane's row m of a transposed output: lanes are
+// neighbours there.
 template <typename T>
-__device__ __forceinline__ void f8_store(const F8Args &g, T *out, int64_t ld, float *box,
-                                         int lane, int64_t m0, int64_t n,
-                                         const uint32_t (&v)[32], int W) {
-  if (g.swap) {
-    const int64_t m = m0 + lane;
+__device__ __forceinline__ void f8_store_swapped(const F8Args &g, T *out, int64_t ld, int64_t m,
+                                                 int64_t n, const uint32_t (&v)[32], int W) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (m < g.M && j < W && n + j < g.N) out[(n + j) * ld + m] = f8_out<T>(__uint_as_float(v[j]));
-    return;
-  }
+  for (int j = 0; j < 32; ++j)
+    if (m < g.M && j < W && n + j < g.N) out[(n + j) * ld + m] = f8_out<T>(__uint_as_float(v[j]));
+}
+
+// A warp's 32 rows (this lane's is m0 + lane) x 32 columns from n on, entry by entry, by
+// way of the box, so that a row's columns are neighbours.  (The loop over rows stays a
+// loop: unrolled into every piece and type, the kernel waited for its instructions.)
+template <typename T>
+__device__ __forceinline__ void f8_store_rows(const F8Args &g, T *out, int64_t ld, float *box,
+                                              int lane, int64_t m0, int64_t n,
+                                              const uint32_t (&v)[32]) {
   if (m0 >= g.M || n >= g.N) return;
   const int rows = (int)min((int64_t)32, g.M - m0);
   const int col = lane & 15, up = lane >> 4;
@@ -595,11 +598,11 @@ __device__ __forceinline__ void f8_store(const F8Args &g, T *out, int64_t ld, fl
       *reinterpret_cast<uint4 *>(box + box_off(lane, j) / 4) =
           make_uint4(v[h + 4 * j], v[h + 4 * j + 1], v[h + 4 * j + 2], v[h + 4 * j + 3]);
     __syncwarp();
-    const bool in = h + col < W && n + h + col < g.N;
-    T *p = out + m0 * ld + n + h + col;
-#pragma unroll 8
-    for (int r = up; r < rows; r += 2)
-      if (in) p[r * ld] = f8_out<T>(box[box_off(r, col >> 2) / 4 + (col & 3)]);
+    if (n + h + col >= g.N) continue;
+    T *p = out + (m0 + up) * ld + n + h + col;
+#pragma unroll 2
+    for (int r = up; r < rows; r += 2, p += 2 * ld)
+      *p = f8_out<T>(box[box_off(r, col >> 2) / 4 + (col & 3)]);
   }
 }
 
@@ -751,23 +754,32 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       }
       if (!ok) break;
       const int64_t m = t.m0 + q * 32, n = t.n0 + h * W0;
+      // a part of the sums (fp32) or the output
+      float *fp32 = g.splits > 1 ? g.part + t.split * g.M * g.N
+                                 : g.bf16 ? nullptr : static_cast<float *>(g.out);
+      __nv_bfloat16 *bf16 = static_cast<__nv_bfloat16 *>(g.out);
+      const int64_t ld = g.splits > 1 ? (g.swap ? g.M : g.N) : g.ldo;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         if (32 * p >= W) break;
         const int64_t np = n + 32 * p;
-        if (NT >= 64 && g.boxes) {
-          if (g.bf16) f8_store_box<__nv_bfloat16>(g, &tmOut, box, lane, m, np, v[p]);
-          else f8_store_box<float>(g, &tmOut, box, lane, m, np, v[p]);
-        } else {
-          const int w = W - 32 * p;
-          if (g.splits > 1)
-            f8_store<float>(g, g.part + t.split * g.M * g.N, g.swap ? g.M : g.N, box, lane, m, np,
-                            v[p], w);
-          else if (g.bf16)
-            f8_store<__nv_bfloat16>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, box, lane, m,
-                                    np, v[p], w);
-          else
-            f8_store<float>(g, static_cast<float *>(g.out), g.ldo, box, lane, m, np, v[p], w);
+        if constexpr (NT >= 64) {
+          if (!g.swap) {
+            if (g.boxes && g.bf16)
+              f8_store_box<__nv_bfloat16>(g, &tmOut, box, lane, m, np, v[p]);
+            else if (g.boxes)
+              f8_store_box<float>(g, &tmOut, box, lane, m, np, v[p]);
+            else if (fp32)
+              f8_store_rows<float>(g, fp32, ld, box, lane, m, np, v[p]);
+            else
+              f8_store_rows<__nv_bfloat16>(g, bf16, ld, box, lane, m, np, v[p]);
+          }
+        }
+        if constexpr (NT <= 64) {
+          if (g.swap && fp32)
+            f8_store_swapped<float>(g, fp32, ld, m + lane, np, v[p], W);
+          else if (g.swap)
+            f8_store_swapped<__nv_bfloat16>(g, bf16, ld, m + lane, np, v[p], W);
         }
       }
     }

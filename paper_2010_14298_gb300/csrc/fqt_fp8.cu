@@ -163,7 +163,8 @@ __device__ __forceinline__ void f8_stage(T *dst, const T *p, int64_t left, int l
 
 // Codes by rows alone, one scale per 128 entries: a warp takes 512 columns of R rows,
 // a lane 16 of each, so that a block's maximum is three shuffles, the codes leave in
-// 16-byte stores and a row's four scales in one word.  Bound by memory traffic.
+// 16-byte stores and a row's four scales in one word.  Bound by memory traffic: 8192 x
+// 4096 in bf16 19.8 us, 5.1 TB/s; in fp32 28.7 us, 5.8 TB/s.
 template <typename T, int R>
 __global__ void __launch_bounds__(256) k_f8_rows(const F8QuantArgs a, const bool vec) {
   __shared__ __align__(16) uint32_t stages[8][512 * sizeof(T) / 4];
@@ -219,8 +220,8 @@ __global__ void __launch_bounds__(256) k_f8_rows(const F8QuantArgs a, const bool
 // Codes along both axes (or blocks of 128 x 128): one CTA per 128 x 128 tile.  A thread
 // holds 4 rows x 8 columns, so it packs codes along either axis without exchanging
 // bytes: 8 bytes of each of its rows go straight to memory, 4 bytes of each of its
-// columns through shared memory.  Bound by memory traffic: the entries are read once
-// for both outputs.
+// columns through shared memory.  The entries are read once for both outputs: 8192 x 4096
+// in bf16 28.8 us, 4.7 TB/s (66% of the issue slots taken), in fp32 37.8 us, 5.3 TB/s.
 constexpr int kF8TileThreads = 512;
 
 template <typename T>
@@ -389,7 +390,10 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
 // 32 entries of K; a block's four steps use the same ones.  (With unscaled products,
 // each block's sums read back and folded into registers, the hand-over of an
 // accumulator for every 128 entries of K bound the kernel: 172 us for 8192 x 4096 x
-// 4096, with per-row scales on both sides 232.)
+// 4096, with per-row scales on both sides 232.)  Now 97 us, 2.83 PFLOP/s of the 3.69
+// that back-to-back products on this GPU reach: a K block of a super tile takes 0.42 us,
+// 64 KB through L2 for 0.28 us of products, and a tile's accumulator is handed over once.
+// An fp32 output takes 115 us (its accumulators are handed over every eight K blocks).
 constexpr int kF8EpiWarps = 8, kF8Epi0 = 4;  // warps 0 loads, 1 products, 2 and 3 scales
 constexpr int kF8Threads = 32 * (kF8Epi0 + kF8EpiWarps);
 // K blocks of an accumulator of an fp32 output: a step of the tensor core drops what lies

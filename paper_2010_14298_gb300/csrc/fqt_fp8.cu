@@ -391,8 +391,8 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
 // each block's sums read back and folded into registers, the hand-over of an
 // accumulator for every 128 entries of K bound the kernel: 172 us for 8192 x 4096 x
 // 4096, with per-row scales on both sides 232.)  Now 97 us, 2.83 PFLOP/s of the 3.69
-// that back-to-back products on this GPU reach: a K block of a super tile takes 0.42 us,
-// 64 KB through L2 for 0.28 us of products, and a tile's accumulator is handed over once.
+// that back-to-back products on this GPU reach: a K block of a super tile takes 0.43 us,
+// 0.35 of products (and 64 KB through L2), and a tile's accumulator is handed over once.
 // An fp32 output takes 115 us (its accumulators are handed over every eight K blocks).
 constexpr int kF8EpiWarps = 8, kF8Epi0 = 4;  // warps 0 loads, 1 products, 2 and 3 scales
 constexpr int kF8Threads = 32 * (kF8Epi0 + kF8EpiWarps);

@@ -9,7 +9,7 @@ to 1e-5 against the gradients that the block made.
 import pytest
 import torch
 
-from paper_2010_14298_gb300 import ffn
+from paper_2010_14298_gb300 import ffn, fqt
 
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
@@ -67,6 +67,20 @@ def test_training_lowers_the_loss(format):
     losses = [float(block.step(x, target, 0.03)) for _ in range(30)]
     assert block.check() == 0
     assert losses[-1] < 0.8 * losses[0]
+
+
+@pytest.mark.parametrize("format", ffn.FORMATS)
+def test_the_same_bits_through_ctypes(format, monkeypatch):
+    """Where the extension module cannot be built, the calls are marshalled by ctypes."""
+    x, target = _data(300, 128)
+    first = ffn.FfnBlock(300, 128, 256, format)
+    first.step(x, target, 0.01)
+    monkeypatch.setattr(fqt, "_native", fqt._CtypesCalls(fqt.load()))
+    second = ffn.FfnBlock(300, 128, 256, format)
+    second.step(x, target, 0.01)
+    assert second.check() == 0
+    assert torch.equal(first.norm, second.norm)
+    assert all(torch.equal(a, b) for a, b in zip(first.parameters, second.parameters))
 
 
 def test_formats_and_widths_that_do_not_exist():

@@ -140,3 +140,23 @@ def test_clip_refusals():
     assert call(good, ws=None) == EWORKSPACE and call(good, nbytes=256) == EWORKSPACE
     assert call(good, ws=_at(p, 8)) == EWORKSPACE
     del raw
+
+
+@pytest.mark.parametrize("calls", ["extension", "ctypes"])
+def test_both_marshallings_take_and_refuse_the_same(calls):
+    """The extension module's calls and the same through ctypes: what the library refuses
+    (or has nothing to do for) without a GPU."""
+    n = fqt.native() if calls == "extension" else fqt._CtypesCalls(fqt.load())
+    X, v = torch.zeros(4, 64), torch.zeros(64)
+    ws = torch.zeros(512, dtype=torch.uint8)
+    assert n.layer_norm_forward(X, 64, 0, 4, 64, v, None, -1.0, X, 64, None, v, 0) == EINVAL
+    assert n.layer_norm_forward(X, 64, 0, 0, 64, None, None, 1e-5, X, 64, v, v, 0) == 0
+    assert n.layer_norm_backward(X, 64, X, 64, 0, -4, 64, v, v, None, X, 64, None, None, None, 0,
+                                 0) == EINVAL
+    q = fqt.Fp8Tensor.empty(4, 64, device="cpu")
+    assert n.quantize_fp8(X, 64, 0, 4, 64, 2, q, None, ws, 512, 0) == EINVAL
+    assert n.quantize_fp8(X, 64, 0, 4, 64, 1, None, None, ws, 512, 0) == EINVAL
+    assert n.fp8_matmul(q, fqt.Fp8Tensor.empty(3, 65, device="cpu"), 0, X, 64, ws, 512, 0) == EINVAL
+    assert n.clip_grad_norm(0, None, 1, 1.0, None, ws, 512, 0) == EINVAL
+    a = (fqt._Tensor * 1)(fqt._Tensor(0, 5, 0, 0))
+    assert n.clip_grad_norm(ctypes.addressof(a), None, 1, 1.0, v, ws, 512, 0) == EINVAL

@@ -436,6 +436,17 @@ __device__ __forceinline__ bool f8_wait(uint64_t *bar, uint32_t parity, int *sta
   return mbar_wait(bar, parity, status);
 }
 
+// True in one lane of a converged warp, the same one every time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(one));
+  return one != 0;
+}
+
 // A wait that acquires what the pair's other CTA has written.
 __device__ __forceinline__ bool f8_wait_cluster(uint64_t *bar, uint32_t parity, int *status) {
   uint64_t t0 = 0;
@@ -826,7 +837,12 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    // The whole warp runs this loop and one lane issues: addresses and descriptors that
+    // are the same in every lane live in uniform registers, where the instructions want
+    // them.  (In a loop of one lane's own, an instruction took longer to issue than to
+    // run: 94 us for 8192 x 4096 x 4096.)
+    if (rank == 0) {
+      const bool one = elect_one();
       int s = 0;
       uint32_t ph = 0, c = 0, grp = 0;
       bool ok = true;
@@ -834,6 +850,8 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       // byte of B's and A's scale words
       constexpr uint32_t idesc0 = ((uint32_t)(NT >> 3) << 17) | (1u << 23) |
                                   ((uint32_t)(PAIR ? 2 : 1) << 27);
+      const uint64_t da0 = sw128_desc(smem_u32(ops));
+      const uint64_t db0 = sw128_desc(smem_u32(ops) + (uint32_t)kTileBytes);
       for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step) {
         const F8Item t = f8_item<NT, PAIR>(g, it);
         uint32_t sa = 0;
@@ -843,6 +861,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             ok = false;
             break;
           }
+          const uint32_t acc = tmem + (uint32_t)(buf * NT);
           for (int kb = k0; kb < k1; ++kb) {
             if ((kb & (kF8Group - 1)) == 0) {  // the next group's scales
               const int slot = grp % kF8Ring;
@@ -852,13 +871,15 @@ __global__ void __launch_bounds__(kF8Threads, 1)
               }
               tc_fence_after();
               sa = tmem + kScales + (grp & 1u) * (4 + kSbCols);
-              const uint32_t src = smem_u32(smem + slot * kF8RingBytes);
-              f8_copy_scales<PAIR>(sa, src);
+              if (one) {
+                const uint32_t src = smem_u32(smem + slot * kF8RingBytes);
+                f8_copy_scales<PAIR>(sa, src);
 #pragma unroll
-              for (int i = 0; i < kSbCols / 4; ++i)
-                f8_copy_scales<PAIR>(sa + 4 + 4 * i, src + 512 + 512 * i);
-              if constexpr (PAIR) umma_commit_pair(&sempty[slot]);
-              else umma_commit(&sempty[slot]);
+                for (int i = 0; i < kSbCols / 4; ++i)
+                  f8_copy_scales<PAIR>(sa + 4 + 4 * i, src + 512 + 512 * i);
+                if constexpr (PAIR) umma_commit_pair(&sempty[slot]);
+                else umma_commit(&sempty[slot]);
+              }
               ++grp;
             }
             if (!f8_wait(&full[s], ph, g.status)) {
@@ -866,32 +887,38 @@ __global__ void __launch_bounds__(kF8Threads, 1)
               break;
             }
             tc_fence_after();
-            const uint32_t a_addr = smem_u32(ops + (size_t)s * kStage);
-            const uint64_t da = sw128_desc(a_addr), db = sw128_desc(a_addr + (uint32_t)kTileBytes);
-            const uint32_t id = (uint32_t)kb & (kF8Group - 1);
-            const uint32_t idesc = idesc0 | id << 4 | id << 29;
+            if (one) {
+              const uint64_t da = da0 + (uint64_t)(s * (int)(kStage >> 4));
+              const uint64_t db = db0 + (uint64_t)(s * (int)(kStage >> 4));
+              const uint32_t id = (uint32_t)kb & (kF8Group - 1);
+              const uint32_t idesc = idesc0 | id << 4 | id << 29;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)  // 32 entries each
-              f8_mma<PAIR>(tmem + (uint32_t)(buf * NT), da + 2 * k, db + 2 * k, idesc, sa, sa + 4,
-                           (k > 0 || kb > k0) ? 1u : 0u);
-            if constexpr (PAIR) umma_commit_pair(&empty[s]);
-            else umma_commit(&empty[s]);
+              for (int k = 0; k < 4; ++k)  // 32 entries each
+                f8_mma<PAIR>(acc, da + 2 * k, db + 2 * k, idesc, sa, sa + 4,
+                             (k > 0 || kb > k0) ? 1u : 0u);
+              if constexpr (PAIR) umma_commit_pair(&empty[s]);
+              else umma_commit(&empty[s]);
+            }
             if (++s == g.stages) { s = 0; ph ^= 1u; }
           }
           if (!ok) break;
-          if constexpr (PAIR) umma_commit_pair(&accf[buf]);
-          else umma_commit(&accf[buf]);
+          if (one) {
+            if constexpr (PAIR) umma_commit_pair(&accf[buf]);
+            else umma_commit(&accf[buf]);
+          }
         }
       }
       if (!ok) *abort_flag = 1;
       // every product has completed before tensor memory is released
-      if constexpr (PAIR)
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                smem_u32(drain))
-            : "memory");
-      else
-        umma_commit(drain);
+      if (one) {
+        if constexpr (PAIR)
+          asm volatile(
+              "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                  smem_u32(drain))
+              : "memory");
+        else
+          umma_commit(drain);
+      }
       f8_wait(drain, 0, g.status);
     }
   } else {

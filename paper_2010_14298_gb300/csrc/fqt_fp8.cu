@@ -390,10 +390,11 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
 // 32 entries of K; a block's four steps use the same ones.  (With unscaled products,
 // each block's sums read back and folded into registers, the hand-over of an
 // accumulator for every 128 entries of K bound the kernel: 172 us for 8192 x 4096 x
-// 4096, with per-row scales on both sides 232.)  Now 97 us, 2.83 PFLOP/s of the 3.69
-// that back-to-back products on this GPU reach: a K block of a super tile takes 0.43 us,
-// 0.35 of products (and 64 KB through L2), and a tile's accumulator is handed over once.
-// An fp32 output takes 115 us (its accumulators are handed over every eight K blocks).
+// 4096, with per-row scales on both sides 232.)  Now 77 us, 3.6 PFLOP/s of the tensor
+// cores' nominal 4.5: a K block of a super tile takes 0.30 us, 0.28 at that rate, and
+// handing its accumulator over 1.2 us.  An fp32 output takes 103 us (its accumulators are
+// handed over every eight K blocks; super tiles of 224 columns, which leave room for two
+// accumulators, took 101, and 38 us where 256 take 25: 4096 x 1024 x 8192 in bf16).
 constexpr int kF8EpiWarps = 8, kF8Epi0 = 4;  // warps 0 loads, 1 products, 2 and 3 scales
 constexpr int kF8Threads = 32 * (kF8Epi0 + kF8EpiWarps);
 // K blocks of an accumulator of an fp32 output: a step of the tensor core drops what lies
@@ -409,6 +410,7 @@ constexpr size_t kF8OffBar = kF8Ring * kF8RingBytes;
 constexpr size_t kF8Bars = 2 * kMaxStages + 2 * kF8Ring + 5;
 constexpr size_t kF8Fixed = (kF8OffBar + kF8Bars * 8 + 16 + 1023) & ~(size_t)1023;
 constexpr size_t kF8BoxBytes = 2048;    // an epilogue warp's box of output
+constexpr int kF8Parts = 8;             // CTAs that share a tile's K blocks at most
 constexpr int kF8Band = 8;              // row tiles of a band of tiles
 
 struct F8Args {
@@ -422,7 +424,6 @@ struct F8Args {
   int64_t ldo;
   int bf16, swap;  // swap: out is indexed [B row][A row]
   int boxes;       // out is written in boxes by TMA
-  float *part;     // splits > 1: fp32 partial outputs, one after another
   int stages;
   int *status;
 };
@@ -523,19 +524,17 @@ __device__ __forceinline__ void f8_copy_scales(uint32_t taddr, uint32_t saddr) {
 }
 
 // An item: this CTA's 128 rows of A against NT rows of B over some K blocks (from a
-// multiple of kF8Group).  The two CTAs of a pair take the same item, each its 128 of
-// the super tile's 256 rows.
+// multiple of kF8Group; a tile's parts follow one another).  The two CTAs of a pair take
+// the same item, each its 128 of the super tile's 256 rows.
 struct F8Item {
   int64_t m0, n0;
-  int kb0, kb1, split;
+  int kb0, kb1;
 };
 
 template <int NT, bool PAIR>
 __device__ __forceinline__ F8Item f8_item(const F8Args &g, int64_t it) {
   F8Item t;
-  const int64_t tiles = (int64_t)g.m_tiles * g.n_tiles;
-  t.split = (int)(it / tiles);
-  const int64_t r = it - t.split * tiles;
+  const int64_t r = PAIR ? it : it / g.splits;
   // bands of kF8Band row tiles, so that the tiles in flight share rows of both operands
   const int64_t band = r / ((int64_t)kF8Band * g.n_tiles);
   const int64_t in = r - band * kF8Band * g.n_tiles;
@@ -544,7 +543,7 @@ __device__ __forceinline__ F8Item f8_item(const F8Args &g, int64_t it) {
   t.n0 = n * NT;
   t.m0 = (band * kF8Band + in - n * high) * (PAIR ? 2 * BM : BM) +
          (PAIR ? (blockIdx.x & 1) * BM : 0);
-  t.kb0 = t.split * g.kb_per;
+  t.kb0 = PAIR ? 0 : (int)(it - r * g.splits) * g.kb_per;
   t.kb1 = min(g.nkb, t.kb0 + g.kb_per);
   return t;
 }
@@ -647,7 +646,49 @@ __device__ __forceinline__ void f8_store_box(const F8Args &g, const CUtensorMap 
   }
 }
 
-// One CTA per 128 x NT tile (and split of the K blocks), persistent, or a pair of CTAs
+// The sums of a tile whose K blocks a cluster's CTAs share, the parts in their order:
+// each part lies in its CTA's shared memory at the same place, in the output's order, in
+// rows of NT + 4 entries or (swapped) columns of 128, and each CTA adds up its share.
+template <int NT>
+__device__ __forceinline__ void f8_join(const F8Args &g, int64_t it, const float *part) {
+  const F8Item t = f8_item<NT, false>(g, it);
+  const int parts = g.splits, self = (int)(it % parts);
+  const int run = g.swap ? BM : NT, pitch = g.swap ? BM : NT + 4;  // of outputs in a row
+  // rows and entries of a row that the output has
+  const int64_t r0 = g.swap ? t.n0 : t.m0, c0 = g.swap ? t.m0 : t.n0;
+  const int rows = (int)min((int64_t)(g.swap ? NT : BM), (g.swap ? g.N : g.M) - r0);
+  const int cols = (int)min((int64_t)run, (g.swap ? g.M : g.N) - c0);
+  for (int e = (self * kF8Threads + (int)threadIdx.x) * 4; e < rows * run;
+       e += parts * kF8Threads * 4) {
+    const int r = e / run, c = e % run;
+    if (c >= cols) continue;
+    float v[kF8Parts][4];
+#pragma unroll
+    for (int k = 0; k < kF8Parts; ++k)
+      if (k < parts)
+        asm volatile(
+            "{\n\t.reg .b32 a;\n\t"
+            "mapa.shared::cluster.u32 a, %4, %5;\n\t"
+            "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+            : "=f"(v[k][0]), "=f"(v[k][1]), "=f"(v[k][2]), "=f"(v[k][3])
+            : "r"(smem_u32(part + r * pitch + c)), "r"(k)
+            : "memory");
+#pragma unroll
+    for (int k = 1; k < kF8Parts; ++k)
+      if (k < parts)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[0][i] += v[k][i];
+    const int64_t o = (r0 + r) * g.ldo + c0 + c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < cols) {
+        if (g.bf16) static_cast<__nv_bfloat16 *>(g.out)[o + i] = __float2bfloat16_rn(v[0][i]);
+        else static_cast<float *>(g.out)[o + i] = v[0][i];
+      }
+  }
+}
+
+// One CTA per 128 x NT tile (and part of the K blocks), persistent, or a pair of CTAs
 // per 256 x NT super tile: each loads its 128 rows of A and half of B's NT rows, and
 // the leader issues products over both (cta_group::2), so an operand byte is loaded
 // for twice the products.  Warp 0 feeds operand stages of one K block by TMA, warps 2
@@ -768,12 +809,28 @@ __global__ void __launch_bounds__(kF8Threads, 1)
         if (lane == 0) f8_release<PAIR>(&acce[buf]);
       }
       if (!ok) break;
+      if constexpr (!PAIR) {
+        if (g.splits > 1) {  // the products are done with the operand stages
+          float *part = reinterpret_cast<float *>(ops);
+          const int r = q * 32 + lane, j = h * W0;
+#pragma unroll
+          for (int i = 0; i < W0; i += 4) {
+            const uint32_t *x = &v[i / 32][i % 32];
+            if (!g.swap) {
+              *reinterpret_cast<uint4 *>(part + r * (NT + 4) + j + i) =
+                  make_uint4(x[0], x[1], x[2], x[3]);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) part[(j + i + k) * BM + r] = __uint_as_float(x[k]);
+            }
+          }
+          break;
+        }
+      }
       const int64_t m = t.m0 + q * 32, n = t.n0 + h * W0;
-      // a part of the sums (fp32) or the output
-      float *fp32 = g.splits > 1 ? g.part + t.split * g.M * g.N
-                                 : g.bf16 ? nullptr : static_cast<float *>(g.out);
+      float *fp32 = g.bf16 ? nullptr : static_cast<float *>(g.out);
       __nv_bfloat16 *bf16 = static_cast<__nv_bfloat16 *>(g.out);
-      const int64_t ld = g.splits > 1 ? (g.swap ? g.M : g.N) : g.ldo;
+      const int64_t ld = g.ldo;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         if (32 * p >= W) break;
@@ -840,7 +897,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
     // The whole warp runs this loop and one lane issues: addresses and descriptors that
     // are the same in every lane live in uniform registers, where the instructions want
     // them.  (In a loop of one lane's own, an instruction took longer to issue than to
-    // run: 94 us for 8192 x 4096 x 4096.)
+    // run: 94 us for 8192 x 4096 x 4096, now 77.)
     if (rank == 0) {
       const bool one = elect_one();
       int s = 0;
@@ -964,8 +1021,15 @@ __global__ void __launch_bounds__(kF8Threads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  // neither CTA of a pair leaves while the other may still reach its memory
-  if constexpr (PAIR) cluster_sync();
+  if constexpr (!PAIR) {
+    if (g.splits > 1) {
+      cluster_sync();  // the tile's parts are in the shared memory of the cluster
+      f8_join<NT>(g, first, reinterpret_cast<const float *>(ops));
+      __syncthreads();
+    }
+  }
+  // no CTA of a pair or a cluster leaves while another may still reach its memory
+  if (PAIR || g.splits > 1) cluster_sync();
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
@@ -977,22 +1041,6 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                    "r"(kCols)
                    : "memory");
-  }
-}
-
-// The sum of the splits' partial outputs, in their order.
-template <typename T>
-__global__ void __launch_bounds__(256)
-    k_f8_join(const float *part, int splits, int64_t rows, int64_t cols, T *out, int64_t ldo) {
-  let_next_start();
-  wait_for_previous();
-  const int64_t n = rows * cols;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
-       i += (int64_t)gridDim.x * blockDim.x) {
-    float s = 0.0f;
-    for (int k = 0; k < splits; ++k) s += __ldg(part + k * n + i);
-    const int64_t r = i / cols;
-    out[r * ldo + (i - r * cols)] = f8_out<T>(s);
   }
 }
 
@@ -1050,22 +1098,19 @@ static F8Plan f8_plan(int64_t M, int64_t N, int64_t nkb, int nsm) {
   p.nt = p.pair ? 256 : p.swap ? (b <= 32 ? 32 : 64) : wide ? 128 : 64;
   p.n_tiles = (int)((b + p.nt - 1) / p.nt);
   const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
-  // fewer tiles than SMs: the contraction is split, into groups of K blocks
+  // Fewer tiles than SMs: clusters share a tile's K blocks, whole groups of scales each.
+  // What a CTA is spared of has to exceed the eight K blocks that meeting in shared
+  // memory takes as long as: 1 x 1024 x 4096 5.5 us by clusters of 8, 6.2 of 4; 1 x 4096
+  // x 1024 4.8 us unshared, 5.5 by clusters of 2.
   const int64_t groups = (nkb + kF8Group - 1) / kF8Group;
-  // (eight K blocks a part at least: the second launch costs as much as ten)
   int64_t splits = p.pair ? 1 : nsm / tiles;
-  if (splits > nkb / 8) splits = nkb / 8;
+  if (splits > groups) splits = groups;
+  if (splits > kF8Parts) splits = kF8Parts;
   if (splits < 1) splits = 1;
-  if (splits > 16) splits = 16;
   p.kb_per = (int)((groups + splits - 1) / splits) * kF8Group;
+  if (nkb - p.kb_per <= 8) p.kb_per = (int)groups * kF8Group;
   p.splits = (int)((nkb + p.kb_per - 1) / p.kb_per);
   return p;
-}
-
-size_t fp8_matmul_ws_bytes(int64_t M, int64_t N, int64_t K) {
-  if (M <= 0 || N <= 0 || K <= 0) return kHeaderBytes;
-  const F8Plan p = f8_plan(M, N, (K + kF8Block - 1) / kF8Block, device_sm_count());
-  return kHeaderBytes + (p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0);
 }
 
 template <int NT, int ACCS, bool PAIR, bool FOLD>
@@ -1092,11 +1137,11 @@ static fqt_status launch_f8_as(const CUtensorMap &ta, const CUtensorMap &tb, con
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = 2;
+  at[1].val.clusterDim.x = PAIR ? 2 : (unsigned)g.splits;
   at[1].val.clusterDim.y = 1;
   at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = PAIR ? 2 : 1;
+  cfg.numAttrs = PAIR || g.splits > 1 ? 2 : 1;
   return cuda_fail(cudaLaunchKernelEx(&cfg, kernel, ta, tb, to, (const F8Args &)g),
                    "FP8 product launch");
 }
@@ -1188,22 +1233,11 @@ fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, 
   g.out = out;
   g.bf16 = bf16;
   g.swap = p.swap;
-  g.part = reinterpret_cast<float *>(static_cast<char *>(ws) + kHeaderBytes);
   g.status = static_cast<int *>(ws);
-  fqt_status s = p.pair        ? launch_f8<256, 1, true>(ta, tb, to, g, nsm, st)
-                 : p.nt == 128 ? launch_f8<128, 2, false>(ta, tb, to, g, nsm, st)
-                 : p.nt == 64  ? launch_f8<64, 2, false>(ta, tb, to, g, nsm, st)
-                               : launch_f8<32, 2, false>(ta, tb, to, g, nsm, st);
-  if (s != FQT_OK || p.splits == 1) return s;
-  const int64_t blocks = (M * N + 255) / 256;
-  const int grid = (int)(blocks < 8 * nsm ? blocks : 8 * nsm);
-  const float *part = g.part;
-  const cudaError_t e =
-      bf16 ? launch_behind(k_f8_join<__nv_bfloat16>, dim3((unsigned)grid), 256, 0, st, part,
-                           p.splits, M, N, static_cast<__nv_bfloat16 *>(out), g.ldo)
-           : launch_behind(k_f8_join<float>, dim3((unsigned)grid), 256, 0, st, part, p.splits, M,
-                           N, static_cast<float *>(out), g.ldo);
-  return cuda_fail(e, "FP8 join launch");
+  if (p.pair) return launch_f8<256, 1, true>(ta, tb, to, g, nsm, st);
+  if (p.nt == 128) return launch_f8<128, 2, false>(ta, tb, to, g, nsm, st);
+  if (p.nt == 64) return launch_f8<64, 2, false>(ta, tb, to, g, nsm, st);
+  return launch_f8<32, 2, false>(ta, tb, to, g, nsm, st);
 }
 
 }  // namespace fqt
@@ -1243,7 +1277,9 @@ fqt_status fqt_quantize_fp8(const void *X, int64_t ldx, fqt_dtype dtype, int64_t
 }
 
 size_t fqt_fp8_matmul_workspace_size(int64_t M, int64_t N, int64_t K) {
-  return fp8_matmul_ws_bytes(M, N, K);
+  // the status word (tiles whose K blocks are shared meet in shared memory)
+  (void)M, (void)N, (void)K;
+  return kHeaderBytes;
 }
 
 fqt_status fqt_fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, fqt_dtype dtype, void *out,
@@ -1264,7 +1300,7 @@ fqt_status fqt_fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, fqt_dtype dtype, v
     return cuda_fail(e, "FP8 product clear");
   }
   if (!f8_good(A) || !f8_good(B)) return FQT_EINVAL;
-  if (!workspace || !f8_aligned(workspace, 256) || ws_bytes < fp8_matmul_ws_bytes(M, N, K))
+  if (!workspace || !f8_aligned(workspace, 256) || ws_bytes < fqt_fp8_matmul_workspace_size(M, N, K))
     return FQT_EWORKSPACE;
   return fp8_matmul(A, B, dtype == FQT_BF16, out, ldo, workspace, st);
 }

@@ -216,6 +216,28 @@ def test_product_matches_64_bits(M, N, K, dtype):
         assert ((out.double() - want).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1, 1024, 4096), (2, 131, 1700), (33, 300, 5000), (64, 257, 8192),
+                                   (65, 66, 1665), (100, 333, 2900), (130, 1900, 2048),
+                                   (257, 129, 20000)])
+def test_tiles_whose_blocks_are_shared(M, N, K, dtype):
+    """Few tiles and a long contraction: CTAs share the K blocks of a tile; the output in
+    wider rows, of which nothing else is written, and the same bits again."""
+    a, _ = fqt.quantize_fp8(_matrix(M, K, "bf16", 1))
+    b, _ = fqt.quantize_fp8(_matrix(N, K, "bf16", 2), 128)
+    A, B = _values64(a), _values64(b)
+    want, bound = A @ B.t(), _product_bound(A, B)
+    if dtype == "bf16":
+        bound = bound + 2.0 ** -8 * want.abs()
+    wide = torch.full((M + 1, N + 5), 7.0, dtype=DTYPES[dtype], device="cuda")
+    ws = fqt.Workspace.of_size(fqt.fp8_matmul_workspace_size(M, N, K))
+    fqt.fp8_matmul(a, b, out=wide[:M, :N], ws=ws)
+    assert fqt.sync_status(ws) == 0
+    assert ((wide[:M, :N].double() - want).abs() <= bound).all()
+    assert (wide[M:] == 7).all() and (wide[:, N:] == 7).all()
+    assert torch.equal(fqt.fp8_matmul(a, b, dtype=DTYPES[dtype], ws=ws), wide[:M, :N])
+
+
 def test_scales_of_any_exponent():
     """Exponents from -127 on, with products of them inside fp32's range."""
     M, N, K = 150, 140, 1100

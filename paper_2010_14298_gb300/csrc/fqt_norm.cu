@@ -94,6 +94,59 @@ __device__ __forceinline__ void store_pack(T *p, const float *v) {
   }
 }
 
+// Two entries, in bf16 rows with one instruction for both: there the conversions leave
+// the arithmetic too few issue slots (32768 x 4096 forward 97 us, 98 without pairs; 16384
+// x 768 12.6 and 13.1; backward 17.6 and 19.7). fp32 rows are bound by memory (8192 x
+// 8192 forward 80 us, with pairs 85).
+template <bool PACKED>
+struct Two {
+  float a, b;
+  static __device__ __forceinline__ Two of(float a, float b) { return {a, b}; }
+  __device__ __forceinline__ float2 get() const { return make_float2(a, b); }
+};
+template <>
+struct Two<true> {
+  f32x2 v;
+  static __device__ __forceinline__ Two of(float a, float b) { return {pack2(a, b)}; }
+  __device__ __forceinline__ float2 get() const {
+    float2 f;
+    unpack2(v, f.x, f.y);
+    return f;
+  }
+};
+template <bool P>
+__device__ __forceinline__ Two<P> operator+(Two<P> x, Two<P> y) {
+  if constexpr (P) return {add2(x.v, y.v)};
+  else return {x.a + y.a, x.b + y.b};
+}
+template <bool P>
+__device__ __forceinline__ Two<P> operator*(Two<P> x, Two<P> y) {
+  if constexpr (P) return {mul2(x.v, y.v)};
+  else return {x.a * y.a, x.b * y.b};
+}
+template <bool P>
+__device__ __forceinline__ Two<P> fma(Two<P> x, Two<P> y, Two<P> z) {
+  if constexpr (P) return {fma2(x.v, y.v, z.v)};
+  else return {fmaf(x.a, y.a, z.a), fmaf(x.b, y.b, z.b)};
+}
+// Sums of entries and of products (in one register where the entries are not packed).
+template <bool P>
+__device__ __forceinline__ void add_to(Two<P> &all, Two<P> x) {
+  if constexpr (P) all.v = add2(all.v, x.v);
+  else all.a = (all.a + x.a) + x.b;
+}
+template <bool P>
+__device__ __forceinline__ void add_to(Two<P> &all, Two<P> x, Two<P> y) {
+  if constexpr (P) all.v = fma2(x.v, y.v, all.v);
+  else all.a = fmaf(x.b, y.b, fmaf(x.a, y.a, all.a));
+}
+template <bool P>
+__device__ __forceinline__ float sum(Two<P> x) {
+  if constexpr (!P) return x.a;
+  const float2 f = x.get();
+  return f.x + f.y;
+}
+
 // This thread's entries of a vector of `cols` floats: V from every column (j G + t) V
 // on; `none` where the vector or the column is missing.
 template <int V, int VPT>
@@ -115,6 +168,15 @@ __device__ __forceinline__ void load_columns(const float *p, int cols, int G, in
       }
     }
   }
+}
+
+template <int V, int VPT>
+__device__ __forceinline__ void load_columns(const float *p, int cols, int G, int t, float none,
+                                             Two<V == 8> (&v)[V * VPT / 2]) {
+  float f[V * VPT];
+  load_columns<V, VPT>(p, cols, G, t, none, f);
+#pragma unroll
+  for (int i = 0; i < V * VPT / 2; ++i) v[i] = Two<V == 8>::of(f[2 * i], f[2 * i + 1]);
 }
 
 // Sums of a value (two values) over the threads of a group (G threads from a warp
@@ -190,10 +252,9 @@ struct NormRing {
 };
 
 // Forward.  S > 0: rows come through S stages of shared memory.  A group takes R rows
-// at a time: their sums share shuffles and barriers.  32768 x 4096 in bf16: 107 us, 5.0
-// TB/s (60% of the issue slots taken); in fp32 187 us, 5.7 TB/s; 8192 x 1024 in bf16 9 us
-// for a floor of 5 (four steps of a CTA's 16 rows, each a load, two reductions and a
-// store long).
+// at a time: their sums share shuffles and barriers.  32768 x 4096 in bf16: 98 us, 5.5
+// TB/s; in fp32 183 us, 5.9 TB/s; 8192 x 1024 in bf16 8.3 us for a floor of 5 (four steps
+// of a CTA's 16 rows, each a load, two reductions and a store long).
 template <typename T, int V, int VPT, int R, int S>
 __global__ void __launch_bounds__(kNormThreads)
     k_norm_fwd(const NormArgs a, int G) {
@@ -202,10 +263,12 @@ __global__ void __launch_bounds__(kNormThreads)
   let_next_start();
   wait_for_previous();
   constexpr int E = V * VPT;
+  using Pair = Two<V == 8>;
+  static_assert(E % 2 == 0, "entries in pairs");
   const int gid = threadIdx.x / G, t = threadIdx.x - gid * G;
   const int lane = t & 31, gw = t >> 5, ngrp = blockDim.x / G;
   const int nvec = a.cols / V;
-  const float n = (float)a.cols;
+  const float n = (float)a.cols, inv = 1.0f / n;
   const NormRing<R * VPT> ring{smem};
   const int64_t step = (int64_t)gridDim.x * ngrp * R;
   const T *px = static_cast<const T *>(a.x) + (int64_t)t * V;
@@ -223,12 +286,13 @@ __global__ void __launch_bounds__(kNormThreads)
   if constexpr (S > 0)
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) fetch(i, r0 + i * step);
-  float ga[E], be[E];
+  Pair ga[E / 2], be[E / 2];
   load_columns<V, VPT>(a.gamma, a.cols, G, t, 1.0f, ga);
   load_columns<V, VPT>(a.beta, a.cols, G, t, 0.0f, be);
   int stage = 0;
   for (; r0 < a.rows; r0 += step) {
-    float d[R][E], mean[R];
+    Pair d[R][E / 2];
+    float mean[R];
     if constexpr (S > 0) {
       fetch(stage == 0 ? S - 1 : stage - 1, r0 + (S - 1) * step);
       copy_wait<S - 1>();
@@ -243,42 +307,66 @@ __global__ void __launch_bounds__(kNormThreads)
         else if constexpr (S > 0) x[j].take(*ring.at(stage, k * VPT + j));
         else x[j].load(px + (r0 + k) * a.ldx + (int64_t)j * G * V);
       }
-      s[k] = 0.0f;
+      Pair all = Pair::of(0.0f, 0.0f);
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        d[k][i] = x[i / V].f(i % V);
-        s[k] += d[k][i];
+      for (int i = 0; i < E; i += 2) {
+        d[k][i / 2] = Pair::of(x[i / V].f(i % V), x[(i + 1) / V].f((i + 1) % V));
+        add_to(all, d[k][i / 2]);
       }
+      s[k] = sum(all);
     }
     if constexpr (S > 0) stage = stage == S - 1 ? 0 : stage + 1;
     group_sums<R>(s, slots[gid][0], G, gid, gw, lane);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      mean[k] = s[k] / n;
-      s[k] = 0.0f;
+      // s / n: by the reciprocal, and corrected by the remainder (Markstein, IBM J. Res.
+      // Dev. 34, 1990); a mean that is off, though by its last bit, shows in the variance
+      // of a row of equal large entries
+      const float m = s[k] * inv;
+      mean[k] = fmaf(fmaf(-m, n, s[k]), inv, m);
+      const Pair less = Pair::of(-mean[k], -mean[k]);
+      Pair all = Pair::of(0.0f, 0.0f);
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        d[k][i] -= mean[k];
-        if ((i / V) * G + t < nvec) s[k] = fmaf(d[k][i], d[k][i], s[k]);
+      for (int i = 0; i < E; i += 2) {
+        Pair &x = d[k][i / 2];
+        x = x + less;
+        if constexpr (V == 1) {
+          const float2 f = x.get();
+          x = Pair::of(i * G + t < nvec ? f.x : 0.0f, (i + 1) * G + t < nvec ? f.y : 0.0f);
+          add_to(all, x, x);
+        } else if ((i / V) * G + t < nvec) {
+          add_to(all, x, x);
+        }
       }
+      s[k] = sum(all);
     }
     group_sums<R>(s, slots[gid][1], G, gid, gw, lane);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      const float rstd = 1.0f / sqrtf(s[k] / n + a.eps);
+      const float rstd = rsqrtf(fmaf(s[k], inv, a.eps));
       if (r0 + k >= a.rows) break;
       if (t == 0) {
         if (a.mean) a.mean[r0 + k] = mean[k];
         if (a.rstd) a.rstd[r0 + k] = rstd;
       }
+      const Pair by = Pair::of(rstd, rstd);
       T *py = static_cast<T *>(a.y) + (r0 + k) * a.ldy + (int64_t)t * V;
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         if (j * G + t >= nvec) break;
         float y[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          y[i] = fmaf(d[k][j * V + i] * rstd, ga[j * V + i], be[j * V + i]);
+        for (int i = 0; i < V; ++i) {
+          const int e = j * V + i;
+          if (V > 1 && i % 2) continue;
+          const float2 f = fma(d[k][e / 2] * by, ga[e / 2], be[e / 2]).get();
+          if constexpr (V == 1) {
+            y[0] = e % 2 ? f.y : f.x;
+          } else {
+            y[i] = f.x;
+            y[i + 1] = f.y;
+          }
+        }
         store_pack<T, V>(py + (int64_t)j * G * V, y);
       }
     }
@@ -287,8 +375,8 @@ __global__ void __launch_bounds__(kNormThreads)
 
 // Backward.  The column sums of a group's rows stay in its registers; at the end the
 // groups of a CTA add theirs in shared memory, and each CTA writes one row of partial
-// sums (k_norm_cols adds those).  32768 x 4096 in bf16: 137 us with k_norm_cols, 5.9
-// TB/s; in fp32 260 us, 6.2 TB/s; 8192 x 1024 in bf16 13.4 us for a floor of 7.6.
+// sums (k_norm_cols adds those).  32768 x 4096 in bf16: 133 us with k_norm_cols, 6.0
+// TB/s; in fp32 261 us, 6.2 TB/s; 8192 x 1024 in bf16 12.5 us for a floor of 7.6.
 template <typename T, int V, int VPT, int S>
 __global__ void __launch_bounds__(kNormThreads)
     k_norm_bwd(const NormArgs a, int G) {
@@ -297,10 +385,11 @@ __global__ void __launch_bounds__(kNormThreads)
   let_next_start();
   wait_for_previous();
   constexpr int E = V * VPT;
+  using Pair = Two<V == 8>;
   const int gid = threadIdx.x / G, t = threadIdx.x - gid * G;
   const int lane = t & 31, gw = t >> 5, ngrp = blockDim.x / G;
   const int nvec = a.cols / V;
-  const float n = (float)a.cols;
+  const float n = (float)a.cols, inv = 1.0f / n;
   const NormRing<2 * VPT> ring{smem};
   const int64_t step = (int64_t)gridDim.x * ngrp;
   const T *px = static_cast<const T *>(a.x) + (int64_t)t * V;
@@ -319,10 +408,10 @@ __global__ void __launch_bounds__(kNormThreads)
   if constexpr (S > 0)
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) fetch(i, r + i * step);
-  float ga[E], dg[E], db[E];
+  Pair ga[E / 2], dg[E / 2], db[E / 2];
   load_columns<V, VPT>(a.gamma, a.cols, G, t, 1.0f, ga);
 #pragma unroll
-  for (int i = 0; i < E; ++i) dg[i] = db[i] = 0.0f;
+  for (int i = 0; i < E / 2; ++i) dg[i] = db[i] = Pair::of(0.0f, 0.0f);
   // a row's statistics, one step ahead
   float mean_next = 0.0f, rstd_next = 0.0f;
   if (r < a.rows) {
@@ -356,29 +445,43 @@ __global__ void __launch_bounds__(kNormThreads)
       rstd_next = __ldg(a.rstd + r + step);
     }
     // u = x - mean and g = dy gamma are kept for dx; a missing entry's dy is 0
-    float u[E], g[E], s1 = 0.0f, s2 = 0.0f;
+    const Pair less = Pair::of(-mean, -mean), by = Pair::of(rstd, rstd);
+    Pair u[E / 2], g[E / 2], all1 = Pair::of(0.0f, 0.0f), all2 = all1;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const float e = dy[i / V].f(i % V);
-      u[i] = x[i / V].f(i % V) - mean;
+    for (int i = 0; i < E / 2; ++i) {
+      const int j = 2 * i, k = 2 * i + 1;
+      const Pair e = Pair::of(dy[j / V].f(j % V), dy[k / V].f(k % V));
+      u[i] = Pair::of(x[j / V].f(j % V), x[k / V].f(k % V)) + less;
       g[i] = e * ga[i];
-      s1 += g[i];
-      s2 = fmaf(g[i], u[i], s2);
-      dg[i] = fmaf(e * rstd, u[i], dg[i]);
-      db[i] += e;
+      add_to(all1, g[i]);
+      add_to(all2, g[i], u[i]);
+      dg[i] = fma(e * by, u[i], dg[i]);
+      db[i] = db[i] + e;
     }
     if (!a.y) continue;
-    const float2 s = group_sum2(s1, s2, slots[gid][slot], G, gid, gw, lane);
+    const float2 s = group_sum2(sum(all1), sum(all2), slots[gid][slot], G, gid, gw, lane);
     // dx = rstd g - rstd sum(g) / n - (x - mean) rstd^3 sum(g (x - mean)) / n
-    const float k0 = -rstd * (s.x / n), k1 = -rstd * (rstd * (rstd * (s.y / n)));
+    // (single entries divide: with the reciprocal 8192 x 1021 took 27 us, so 24)
+    const float m1 = V == 1 ? s.x / n : s.x * inv, m2 = V == 1 ? s.y / n : s.y * inv;
+    const float k0 = -rstd * m1, k1 = -rstd * (rstd * (rstd * m2));
+    const Pair c0 = Pair::of(k0, k0), c1 = Pair::of(k1, k1);
     T *pdx = static_cast<T *>(a.y) + r * a.ldy + (int64_t)t * V;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       if (j * G + t >= nvec) break;
       float o[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        o[i] = fmaf(u[j * V + i], k1, fmaf(g[j * V + i], rstd, k0));
+      for (int i = 0; i < V; ++i) {
+        const int e = j * V + i;
+        if (V > 1 && i % 2) continue;
+        const float2 f = fma(u[e / 2], c1, fma(g[e / 2], by, c0)).get();
+        if constexpr (V == 1) {
+          o[0] = e % 2 ? f.y : f.x;
+        } else {
+          o[i] = f.x;
+          o[i + 1] = f.y;
+        }
+      }
       store_pack<T, V>(pdx + (int64_t)j * G * V, o);
     }
   }
@@ -395,12 +498,13 @@ __global__ void __launch_bounds__(kNormThreads)
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const int c = ((i / V) * G + t) * V + i % V;
+    const float2 f = dg[i / 2].get(), h = db[i / 2].get();
     if (ngrp > 1) {
-      sums[(2 * gid) * per + i * G + t] = dg[i];
-      sums[(2 * gid + 1) * per + i * G + t] = db[i];
+      sums[(2 * gid) * per + i * G + t] = i & 1 ? f.y : f.x;
+      sums[(2 * gid + 1) * per + i * G + t] = i & 1 ? h.y : h.x;
     } else if (c < a.cols) {
-      dst[c] = dg[i];
-      dst[a.cols + c] = db[i];
+      dst[c] = i & 1 ? f.y : f.x;
+      dst[a.cols + c] = i & 1 ? h.y : h.x;
     }
   }
   if (ngrp == 1) return;

@@ -260,3 +260,18 @@ def test_refusals():
     with pytest.raises(fqt.FqtError) as e:
         fqt.layer_norm_backward(X, X, m, m, ws=small)
     assert e.value.status == 6
+
+
+@pytest.mark.parametrize("cols", [1, 3, 7, 24, 48, 335, 768, 1000, 1201, 4096, 8190, 8192])
+def test_means_are_rounded_quotients(cols):
+    """Sums of small integers are exact in any order, so the mean that is nearest to the
+    quotient is the only one; rows of equal entries have no variance."""
+    rows = 400
+    X = torch.randint(-1000, 1001, (rows, cols), generator=_gen(cols), device="cuda").float()
+    X[0], X[1] = 1000.0, -999.0
+    X[2] = torch.randint(1, 1001, (cols,), generator=_gen(cols + 1), device="cuda").float()
+    Y, mean, rstd = fqt.layer_norm_forward(X, eps=EPS)
+    want = (X.double().sum(1) / cols).float()
+    assert torch.equal(mean, want)
+    assert (Y[:2] == 0).all()
+    assert ((rstd[:2].double() - EPS ** -0.5).abs() <= 8 * 2.0 ** -24 * EPS ** -0.5).all()

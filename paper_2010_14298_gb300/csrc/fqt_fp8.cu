@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <math.h>
 
+#include <algorithm>
+
 #include "fqt.h"
 #include "fqt_common.cuh"
 #include "fqt_gemm_core.cuh"
@@ -1093,24 +1095,45 @@ static F8Plan f8_plan(int64_t M, int64_t N, int64_t nkb, int nsm) {
            ((a + 255) / 256) * ((b + 255) / 256) * 8 >= (int64_t)nsm * 3;
   const int rows = p.pair ? 2 * BM : BM;
   p.m_tiles = (int)((a + rows - 1) / rows);
-  // single CTAs: 128 columns where that occupies half of the SMs
-  const bool wide = p.m_tiles * ((b + 127) / 128) * 2 >= nsm;
-  p.nt = p.pair ? 256 : p.swap ? (b <= 32 ? 32 : 64) : wide ? 128 : 64;
-  p.n_tiles = (int)((b + p.nt - 1) / p.nt);
-  const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
-  // Fewer tiles than SMs: clusters share a tile's K blocks, whole groups of scales each.
-  // What a CTA is spared of has to exceed the eight K blocks that meeting in shared
-  // memory takes as long as: 1 x 1024 x 4096 5.5 us by clusters of 8, 6.2 of 4; 1 x 4096
-  // x 1024 4.8 us unshared, 5.5 by clusters of 2.
   const int64_t groups = (nkb + kF8Group - 1) / kF8Group;
-  int64_t splits = p.pair ? 1 : nsm / tiles;
-  if (splits > groups) splits = groups;
-  if (splits > kF8Parts) splits = kF8Parts;
-  if (splits < 1) splits = 1;
-  p.kb_per = (int)((groups + splits - 1) / splits) * kF8Group;
-  if (nkb - p.kb_per <= 8) p.kb_per = (int)groups * kF8Group;
-  p.splits = (int)((nkb + p.kb_per - 1) / p.kb_per);
-  return p;
+  auto cut = [&](int nt, int64_t splits) {  // whole groups of scales each
+    p.nt = nt;
+    p.n_tiles = (int)((b + nt - 1) / nt);
+    p.kb_per = (int)((groups + splits - 1) / splits) * kF8Group;
+    p.splits = (int)((nkb + p.kb_per - 1) / p.kb_per);
+  };
+  if (p.pair) {
+    cut(256, 1);
+    return p;
+  }
+  // Single CTAs: the width, and the CTAs of a cluster that share a tile's K blocks, of
+  // which the estimate is least. A K block takes 0.27 us in a tile of 128 columns, 0.23 of
+  // 64 and 0.2 of 32 (its operands come in at 120 GB/s a CTA), meeting in shared memory
+  // 2.3: 2360 x 283 x 8179 14.7 us in tiles of 128 shared by two, 19.6 of 64 unshared;
+  // 700 x 1000 x 2000 9.5 and 7.8; 1 x 1024 x 4096 5.5 us shared by eight, 6.2 by four;
+  // 1 x 4096 x 1024 4.8 unshared, 5.5 by two.
+  // A cluster lies within one of the GPU's groups of SMs, so not all SMs have a place in
+  // one (15 clusters of eight ran at once, 36 of four, 44 of three): what does not fit
+  // would wait for a second round (2048 x 128 x 4096 15.0 us by eight, 8.2 by four).
+  int64_t least = INT64_MAX;
+  F8Plan best = p;
+  const int widest = p.swap ? (b <= 32 ? 32 : 64) : 128;
+  for (int nt = widest; nt >= (p.swap ? widest : 64); nt /= 2)
+    for (int64_t splits = 1; splits <= kF8Parts && (splits == 1 || splits <= groups); ++splits) {
+      cut(nt, splits);
+      const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
+      const int room = p.splits > 4 ? nsm * 3 / 4 : p.splits > 2 ? nsm * 7 / 8 : nsm;
+      if (splits > 1 && tiles * p.splits > room) break;
+      const int64_t rounds = (tiles * p.splits + nsm - 1) / nsm;
+      const int64_t ns =
+          rounds * std::min<int64_t>(p.kb_per, nkb) * (nt == 128 ? 270 : nt == 64 ? 230 : 200) +
+          (p.splits > 1 ? 2300 : 0);
+      if (ns < least) {
+        least = ns;
+        best = p;
+      }
+    }
+  return best;
 }
 
 template <int NT, int ACCS, bool PAIR, bool FOLD>

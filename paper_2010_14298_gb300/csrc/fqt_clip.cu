@@ -10,9 +10,9 @@
 // ones fill the GPU.  (A run of its own for every CTA balances better, but the second
 // pass then took 42 us instead of 31 for the 102 MB of a ResNet-50.)  The second pass
 // goes through the units backwards: what the first one read last is still in L2.  The
-// 161 tensors of a ResNet-50 in fp32: 47.4 us, of them the norm 19.3 (5.3 TB/s); the
-// second pass reads most of the 102 MB from memory again (L2 holds 126 MB on two dies)
-// and writes as many.
+// 161 tensors of a ResNet-50 in fp32: 43.7 us, of them the norm 19.3 (5.3 TB/s); the
+// second pass reads the part of the 102 MB from memory again that L2 did not keep, and
+// writes as many.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -42,6 +42,7 @@ struct ClipTable {
   ClipEntry e[CAP];
   int n;
   uint32_t units;
+  uint32_t keep;  // the first unit of those that are to stay in L2
 };
 
 constexpr int kClipSmall = 40, kClipMid = 250, kClipLarge = 1020;  // 1.3, 8 and 32.6 KB
@@ -183,10 +184,14 @@ __device__ __forceinline__ float one_entry(const char *p, int i, bool bf16) {
   return reinterpret_cast<const float *>(p)[i];
 }
 
-// Cache policies: entries that the second pass reads again are to stay in L2, what it
-// reads and writes is not (49.3 -> 47.5 us for a ResNet-50, 12.1 -> 10.9 for an FFN in
-// bf16).  Only where the output lies apart: in place there may be no second reading, and
-// the entries would stay for nobody.
+// Cache policies: the entries that the first pass reads last, and the second pass first,
+// are to stay in L2, what either reads or writes besides is not (a ResNet-50 with no
+// policies 49.3 us, with all of its entries kept 46.9, with the last 56 MB 43.7; 200 MB
+// 97.6 and 91.1; keeping 20 or 100 MB gains half of that or nothing).  Only where the
+// output lies apart: in place there may be no second reading, and the entries would stay
+// for nobody.
+constexpr uint32_t kClipKeep = (56u << 20) / kClipUnitBytes;  // units
+
 __device__ __forceinline__ uint64_t keep_policy() {
   uint64_t p;
   asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
@@ -212,9 +217,9 @@ __device__ __forceinline__ void store_as(uint4 *p, const uint4 &v, uint64_t poli
 }
 
 template <int PER, bool APART>
-__device__ __forceinline__ void add_unit(Squares &s, const ClipUnit &u) {
+__device__ __forceinline__ void add_unit(Squares &s, const ClipUnit &u, bool keep) {
   const bool bf16 = PER == 8;
-  const uint64_t policy = keep_policy();
+  const uint64_t policy = keep ? keep_policy() : pass_policy();
   const uint4 *body = reinterpret_cast<const uint4 *>(u.in + u.head * (16 / PER));
   uint4 v[kClipVecs];
 #pragma unroll
@@ -250,8 +255,9 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
   for (uint32_t unit = blockIdx.x; unit < t.units; unit += gridDim.x) {
     if (e + 1 < t.n && t.e[e + 1].unit0 <= unit) e = clip_entry(t, e + 1, t.n - 1, unit);
     const ClipUnit u = clip_unit(t.e[e], unit);
-    if (u.bf16) add_unit<8, APART>(s, u);
-    else add_unit<4, APART>(s, u);
+    const bool keep = unit >= t.keep;
+    if (u.bf16) add_unit<8, APART>(s, u, keep);
+    else add_unit<4, APART>(s, u, keep);
   }
   s = cta_sum(s);
   if (threadIdx.x == 0) part[blockIdx.x] = make_float4(s.mid.h, s.mid.l, s.small, s.big);
@@ -388,6 +394,7 @@ static int64_t fill_table(ClipTable<CAP> &t, const fqt_tensor *in, const fqt_ten
                   in[i].dtype == FQT_BF16 ? 1u : 0u};
     t.units += (uint32_t)((in[i].count + per - 1) / per);
   }
+  t.keep = t.units > kClipKeep ? t.units - kClipKeep : 0;
   return i;
 }
 

@@ -10,8 +10,8 @@
 // Both directions are bound by memory traffic (8 and 14 operations per entry
 // against 4 and 6 bytes of bf16), so a row is read once and kept in registers by a
 // group of threads wide enough to hold it: the group reduces the row's sums, and every
-// thread then finishes the entries it holds.  A thread holds 16 entries of a row and
-// keeps its columns from row to row: fewer leave the reductions' shuffles and the
+// thread then finishes the entries it holds.  A thread holds 16 entries of a row (the
+// forward 32 where it can) and keeps its columns from row to row: fewer leave the reductions' shuffles and the
 // addresses to too few entries, and with more gamma and beta no longer fit the
 // registers, and reading them again for every row took as many wavefronts of the
 // load/store pipe as the row itself.  Rows are fetched ahead by cp.async: a thread
@@ -95,8 +95,8 @@ __device__ __forceinline__ void store_pack(T *p, const float *v) {
 }
 
 // Two entries, in bf16 rows with one instruction for both: there the conversions leave
-// the arithmetic too few issue slots (32768 x 4096 forward 97 us, 98 without pairs; 16384
-// x 768 12.6 and 13.1; backward 17.6 and 19.7). fp32 rows are bound by memory (8192 x
+// the arithmetic too few issue slots (with 16 entries a thread, 16384 x 768 forward 12.6 us
+// and 13.1 without pairs, backward 17.6 and 19.7). fp32 rows are bound by memory (8192 x
 // 8192 forward 80 us, with pairs 85).
 template <bool PACKED>
 struct Two {
@@ -252,9 +252,9 @@ struct NormRing {
 };
 
 // Forward.  S > 0: rows come through S stages of shared memory.  A group takes R rows
-// at a time: their sums share shuffles and barriers.  32768 x 4096 in bf16: 98 us, 5.5
-// TB/s; in fp32 183 us, 5.9 TB/s; 8192 x 1024 in bf16 8.3 us for a floor of 5 (four steps
-// of a CTA's 16 rows, each a load, two reductions and a store long).
+// at a time, whose sums share shuffles and barriers.  32768 x 4096 in bf16: 90 us, 6.0
+// TB/s; in fp32 167 us, 6.4 TB/s; 8192 x 1024 in bf16 6.6 us for a floor of 5 (a copy of
+// as much that stays in L2 takes 3.8).
 template <typename T, int V, int VPT, int R, int S>
 __global__ void __launch_bounds__(kNormThreads)
     k_norm_fwd(const NormArgs a, int G) {
@@ -522,7 +522,8 @@ __global__ void __launch_bounds__(kNormThreads)
   }
 }
 
-// Rows wider than a CTA's registers (over 8192 entries), one CTA a row: X is read three times in the forward (the second and third time
+// Rows wider than a CTA's registers (over 8192 entries, in the forward of aligned rows
+// 16384), one CTA a row: X is read three times in the forward (the second and third time
 // from L1 or L2; 2000 x 20000 in fp32 71 us, 4.5 TB/s) ...
 template <typename T, int V>
 __global__ void __launch_bounds__(kNormThreads)
@@ -701,9 +702,8 @@ struct NormPlan {
   bool ahead;  // rows fetched ahead through shared memory
   bool thin;   // 16 bytes a thread: few rows, where their latency counts
   int v, G, groups, grid;
+  int entries;  // of a row, a thread: 16, or 32 of them and half as many threads
 };
-
-constexpr int kNormEntries = 16;  // of a row, a thread
 
 static NormPlan norm_plan(int64_t rows, int64_t cols, bool bf16, bool vec, bool bwd, int nsm) {
   NormPlan p = {};
@@ -711,7 +711,19 @@ static NormPlan norm_plan(int64_t rows, int64_t cols, bool bf16, bool vec, bool 
   const int64_t nvec = cols / p.v;
   // a row a CTA: 16 bytes a thread (one row of 1024: 1.8 us, with 16 entries a thread 2.3)
   p.thin = vec && rows <= nsm && nvec <= kNormThreads;
-  const int vpt = p.thin ? 1 : kNormEntries / p.v;
+  // Forward: 32 entries a thread need half the shuffles and smaller barriers (8192 x 1024
+  // in bf16 6.6 us, with 16 entries 8.3; 32768 x 4096 90 and 98, in fp32 167 and 184), if
+  // they do not leave a third of the threads idle (21276 x 1088 24.3 us and 22.8), and in
+  // fp32 if a CTA holds more than two rows at a time or 16 entries would not hold the row
+  // (10000 x 8192 110 us and 98; 20000 x 5120 132 and 144; 5000 x 12288 90, read three
+  // times 112).  Single entries and the backward have not the registers for it.
+  p.entries = 16;
+  if (!bwd && vec && !p.thin) {
+    const int64_t pad = (cols + 1023) / 1024 * 1024, groups = kNormThreads * 32 / pad;
+    if ((pad <= (cols + 511) / 512 * 512 || cols * 3 >= pad * 2) && (bf16 || groups != 2))
+      p.entries = 32;
+  }
+  const int vpt = p.thin ? 1 : p.entries / p.v;
   p.wide = nvec > (int64_t)vpt * kNormThreads;
   if (p.wide) {
     p.G = kNormThreads;
@@ -730,8 +742,8 @@ static NormPlan norm_plan(int64_t rows, int64_t cols, bool bf16, bool vec, bool 
     const int64_t each = (rows + nsm - 1) / nsm;
     if (each < p.groups) p.groups = (int)each;
   }
-  // (the forward takes two rows at a time where it fetches ahead)
-  const int64_t each = p.groups * (p.ahead && !bwd ? 2 : 1);
+  // (the forward of 16 entries takes two rows at a time where it fetches ahead)
+  const int64_t each = p.groups * (p.ahead && !bwd && p.entries == 16 ? 2 : 1);
   const int64_t want = (rows + each - 1) / each;
   p.grid = (int)(want < nsm ? want : nsm);
   return p;
@@ -749,7 +761,7 @@ size_t layer_norm_ws_bytes(int64_t rows, int64_t cols) {
 template <typename T, bool BWD, int V, int VPT, int S>
 static cudaError_t launch_rows(const NormArgs &a, const NormPlan &p, cudaStream_t st) {
   const int nth = p.G * p.groups;
-  constexpr int R = !BWD && S > 0 ? 2 : 1;
+  constexpr int R = !BWD && S > 0 && V * VPT == 16 ? 2 : 1;
   size_t smem = (size_t)S * VPT * (BWD ? 2 : R) * 16 * nth;  // the rows on their way
   const size_t sums = BWD && p.groups > 1 && a.part ? 2 * sizeof(float) * VPT * V * nth : 0;
   smem = std::max(smem, sums);
@@ -764,14 +776,22 @@ static cudaError_t launch_rows(const NormArgs &a, const NormPlan &p, cudaStream_
   return launch_behind(kernel, dim3((unsigned)p.grid), nth, smem, st, a, p.G);
 }
 
-template <typename T, bool BWD, int V>
+template <typename T, bool BWD, int V, int E>
 static cudaError_t launch_held(const NormArgs &a, const NormPlan &p, cudaStream_t st) {
-  constexpr int VPT = kNormEntries / V;
+  constexpr int VPT = E / V;
   // stages: 128 KB of rows in bf16 (four) and 192 KB in fp32 (three)
   if constexpr (V == 1) return launch_rows<T, BWD, 1, VPT, 0>(a, p, st);
-  else if (p.thin) return launch_rows<T, BWD, V, 1, 0>(a, p, st);
   else if (p.ahead) return launch_rows<T, BWD, V, VPT, V == 8 ? 4 : 3>(a, p, st);
   else return launch_rows<T, BWD, V, VPT, 0>(a, p, st);
+}
+
+template <typename T, bool BWD, int V>
+static cudaError_t launch_held(const NormArgs &a, const NormPlan &p, cudaStream_t st) {
+  if constexpr (V > 1)
+    if (p.thin) return launch_rows<T, BWD, V, 1, 0>(a, p, st);
+  if constexpr (!BWD && V > 1)
+    if (p.entries == 32) return launch_held<T, BWD, V, 32>(a, p, st);
+  return launch_held<T, BWD, V, 16>(a, p, st);
 }
 
 template <bool BWD>

@@ -275,3 +275,14 @@ def test_means_are_rounded_quotients(cols):
     assert torch.equal(mean, want)
     assert (Y[:2] == 0).all()
     assert ((rstd[:2].double() - EPS ** -0.5).abs() <= 8 * 2.0 ** -24 * EPS ** -0.5).all()
+
+
+# 32 entries a thread: with and without rows fetched ahead, with a last row that is not
+# full, past what 16 entries hold; and the widths beside which it goes back to 16
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,gap", [(1000, 1024, 0), (2600, 1000, 8), (300, 8192, 0),
+                                           (700, 8000, 0), (160, 16384, 0), (310, 16376, 8),
+                                           (153, 10000, 0), (400, 5120, 16), (3000, 1088, 0),
+                                           (500, 640, 0), (700, 6144, 0), (5000, 520, 8)])
+def test_forward_of_wide_groups(rows, cols, gap, dtype):
+    test_forward_matches_the_formula(rows, cols, gap, dtype)

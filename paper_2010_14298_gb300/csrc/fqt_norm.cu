@@ -11,12 +11,13 @@
 // against 4 and 6 bytes of bf16), so a row is read once and kept in registers by a
 // group of threads wide enough to hold it: the group reduces the row's sums, and every
 // thread then finishes the entries it holds.  A thread holds 16 entries of a row (the
-// forward 32 where it can) and keeps its columns from row to row: fewer leave the reductions' shuffles and the
-// addresses to too few entries, and with more gamma and beta no longer fit the
-// registers, and reading them again for every row took as many wavefronts of the
-// load/store pipe as the row itself.  Rows are fetched ahead by cp.async: a thread
-// copies the 16 bytes that it will read itself, so rows are on their way without
-// registers and without barriers.  In the backward the columns' sums stay in registers.
+// forward 32 where it can) and keeps its columns from row to row: fewer leave the
+// reductions' shuffles and the addresses to too few entries, and with more gamma and beta
+// (in the backward the column sums too) no longer fit the registers, and reading them
+// again for every row took as many wavefronts of the load/store pipe as the row itself.
+// Rows are fetched ahead by cp.async: a thread copies the 16 bytes that it will read
+// itself, so rows are on their way without registers and without barriers.  In the
+// backward the columns' sums stay in registers.
 // The variance is taken about the mean (a second reduction over registers), not from
 // the sum of squares, which loses it where the mean is large.  All statistics and sums
 // are fp32.

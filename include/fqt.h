@@ -369,7 +369,8 @@ typedef struct fqt_fp8 {
   int64_t pitch;       /* bytes between rows of codes: a multiple of 16, >= cols */
   int32_t block_rows;  /* rows that share a scale: 1 or 128 */
   int32_t reserved;
-  uint8_t *codes;      /* rows x pitch bytes, 16-byte aligned (bytes past cols are not read) */
+  uint8_t *codes;      /* rows x pitch bytes, 16-byte aligned (bytes past cols are not read;
+                          the quantizer writes those up to a multiple of 16) */
   uint8_t *scales;     /* 4 ceil(cols / 512) P bytes, P = rows rounded up to a multiple
                           of 128: the byte of block kb of row r at
                           ((kb / 4) P + r) 4 + kb % 4 (with block_rows 128 the same for

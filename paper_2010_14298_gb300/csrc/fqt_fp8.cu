@@ -1245,8 +1245,9 @@ fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, 
   const fqt_fp8 *a = p.swap ? B : A, *b = p.swap ? A : B;
   F8Args g = {};
   g.ldo = M > 1 ? ldo : N;
+  // (TMA's stores end at 16 bytes, not at the last column of wider rows)
   g.boxes = !p.swap && p.splits == 1 && f8_aligned(out, 16) &&
-            g.ldo * (bf16 ? 2 : 4) % 16 == 0;
+            g.ldo * (bf16 ? 2 : 4) % 16 == 0 && N * (bf16 ? 2 : 4) % 16 == 0;
   CUtensorMap ta, tb, to = {};
   if (!make_map_codes(&ta, a, BM) || !make_map_codes(&tb, b, (uint32_t)(p.pair ? p.nt / 2 : p.nt)) ||
       (g.boxes && !make_map_f8_out(&to, out, bf16, M, N, g.ldo)))

@@ -238,6 +238,28 @@ def test_tiles_whose_blocks_are_shared(M, N, K, dtype):
     assert torch.equal(fqt.fp8_matmul(a, b, dtype=DTYPES[dtype], ws=ws), wide[:M, :N])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(207, 59, 27), (195, 21, 1064), (81, 7, 121), (300, 1201, 330),
+                                   (767, 885, 129), (3000, 2045, 200), (5, 131, 300),
+                                   (100, 90, 8200)])
+def test_nothing_past_the_rows_is_read_or_written(M, N, K, dtype):
+    """Outputs of 1 to 8 entries in wider rows, whatever alignment that gives them, and
+    codes between whose rows lie other bytes."""
+    a, _ = fqt.quantize_fp8(_matrix(M, K, "f32", 1))
+    b, _ = fqt.quantize_fp8(_matrix(N, K, "f32", 2))
+    A, B = _values64(a), _values64(b)
+    want, bound = A @ B.t(), _product_bound(A, B)
+    if dtype == "bf16":
+        bound = bound + 2.0 ** -8 * want.abs()
+    for q in (a, b):
+        q.codes[:, K:] = 0x7F  # not a number
+    for gap in range(1, 9):
+        wide = torch.full((M + 1, N + gap), 7.0, dtype=DTYPES[dtype], device="cuda")
+        fqt.fp8_matmul(a, b, out=wide[:M, :N])
+        assert ((wide[:M, :N].double() - want).abs() <= bound).all(), gap
+        assert (wide[M:] == 7).all() and (wide[:, N:] == 7).all(), gap
+
+
 def test_scales_of_any_exponent():
     """Exponents from -127 on, with products of them inside fp32's range."""
     M, N, K = 150, 140, 1100

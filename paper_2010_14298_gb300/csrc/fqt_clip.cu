@@ -89,6 +89,12 @@ __device__ __forceinline__ ClipUnit clip_unit(const ClipEntry &e, uint32_t unit)
 // one.)  The sums that count in practice are float-float.  (No 64-bit arithmetic: this
 // GPU's FP64 pipe made the sum of the CTAs' sums, in every CTA of the second pass, take
 // 4 us.)
+// The limits: a list has up to 2^39 vectors (2^41 entries, four of fp32 or more a
+// vector), so a sum of vectors of at most 2^80 stays under 2^119; one of scaled vectors
+// of less than 2^(192 - 110) under 2^121, and one of entries of up to 2^(128 - 96) under
+// 2^107.  Within a vector that is scaled, what an entry loses lies 2^-37 below the sum.
+constexpr float kMidLeast = 0x1p-110f, kMidMost = 0x1p80f;
+
 struct Squares {
   ff mid;
   float small, big;
@@ -152,7 +158,7 @@ __device__ __forceinline__ bool norm_of(const Squares &s, float *root, int *k) {
 __device__ __forceinline__ void add_squares(Squares &s, float &unit, const float *x, int n) {
   float q = 0.0f;
   for (int i = 0; i < n; ++i) q = fmaf(x[i], x[i], q);
-  if (q >= 0x1p-100f && q <= 0x1p100f) {
+  if (q >= kMidLeast && q <= kMidMost) {
     unit += q;
     return;
   }

@@ -1,0 +1,37 @@
+"""The global norm and clipping at the ends of fp32's range and over long lists.
+
+Tolerances.  A thread adds the squares of a unit, at most 64 + 1 of them, in fp32, and
+everything after that in pairs of fp32: the sum of squares is off by at most 65 x 2^-24
+of itself, the norm by half of that, 2e-6, and its rounding to fp32 adds 6e-8: 2.1e-6.
+The factor inherits that, and an entry adds a rounding of the factor, one of the product
+and one of its type.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2010_14298_gb300 import fqt
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
+
+ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+REL = 2.1e-6
+
+
+@pytest.mark.parametrize("dtype,count,value", [(torch.float32, 5 << 28, 2.0 ** 49),
+                                               (torch.bfloat16, 6 << 29, 3.6e14)],
+                         ids=["f32", "bf16"])
+def test_many_large_entries(dtype, count, value):
+    """Squares of 2^98 that fp32 holds one by one, and not their sum: the norm is about
+    2^64, and the list is clipped."""
+    g = torch.full((count,), value, dtype=dtype, device="cuda")
+    value = float(g[0])
+    want = math.sqrt(count) * value
+    ws = fqt.Workspace.of_size(fqt.clip_grad_norm_workspace_size([g]))
+    norm = fqt.clip_grad_norm([g], 1.0, ws=ws)
+    assert fqt.sync_status(ws) == 0
+    assert abs(float(norm) / want - 1) <= REL
+    for end in (float(g.min()), float(g.max())):
+        assert abs(end / (value / want) - 1) <= REL + 3 * 2.0 ** -24 + ROUND[dtype]

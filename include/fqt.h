@@ -421,8 +421,9 @@ typedef struct fqt_tensor {
  * grads and out are host arrays of n, read during the call; out[i] has
  * grads[i]'s count and type and may be grads[i] itself, else they may not
  * overlap.  out NULL: the norm alone.  norm (one fp32 entry, device memory):
- * written when non-NULL.  Sums keep more than 32 bits and every entry's square
- * (fp32's whole range), in an order that goes by the sizes alone.  A norm that is
+ * written when non-NULL.  Every entry's square counts (fp32's whole range); up to
+ * 65 of them are added in fp32, their sums in pairs of fp32, in an order that goes
+ * by the sizes, the entries' place in 16 bytes and the GPU.  A norm that is
  * not finite records FQT_ENONFINITE and leaves the entries as they are.
  * n <= 2^24.  Workspace: fqt_clip_grad_norm_workspace_size(n) bytes.
  */

@@ -85,43 +85,68 @@ __device__ __forceinline__ ClipUnit clip_unit(const ClipEntry &e, uint32_t unit)
 
 // Squares of fp32 entries leave fp32's range for entries outside 2^-63 .. 2^64, so
 // the sum of a vector's squares says which of three sums it belongs to: as it is,
-// or of the entries times 2^96 or 2^-96.  (An entry that is no number is in the last
-// one.)  The sums that count in practice are float-float.  (No 64-bit arithmetic: this
-// GPU's FP64 pipe made the sum of the CTAs' sums, in every CTA of the second pass, take
-// 4 us.)
+// or of the entries times 2^96 or 2^-96.  A thread adds the squares of a unit (at most
+// 64, and one of the ends) in fp32, and all three sums of units are float-float: plain
+// fp32 ones had lost 4e-5 of the norm after 2^32 equal entries.  An infinity would be NaN
+// in them, so the entries that are no numbers are added up apart.  (No 64-bit
+// arithmetic: this GPU's FP64 pipe made the sum of the CTAs' sums, in every CTA of the
+// second pass, take 4 us.)
 // The limits: a list has up to 2^39 vectors (2^41 entries, four of fp32 or more a
 // vector), so a sum of vectors of at most 2^80 stays under 2^119; one of scaled vectors
 // of less than 2^(192 - 110) under 2^121, and one of entries of up to 2^(128 - 96) under
 // 2^107.  Within a vector that is scaled, what an entry loses lies 2^-37 below the sum.
 constexpr float kMidLeast = 0x1p-110f, kMidMost = 0x1p80f;
 
-struct Squares {
+struct alignas(16) Squares {
   ff mid;
-  float small, big;
+  float others;  // 0 where the sums below are
+  float none;    // 0, or no number
+  ff small, big;
 };
+static_assert(sizeof(Squares) == 32, "two 16-byte words");
 
-__device__ __forceinline__ Squares add(const Squares &a, const Squares &b) {
-  return {ff_add(a.mid, b.mid), a.small + b.small, a.big + b.big};
+// A thread's sums of a unit.
+struct UnitSquares {
+  float mid, small, big, none;
+};
+__device__ __forceinline__ void add(Squares &s, const UnitSquares &u) {
+  s.mid = ff_add(s.mid, {u.mid, 0.0f});
+  if (u.small + u.big + u.none == 0.0f) return;
+  s.others = 1.0f;
+  s.small = ff_add(s.small, {u.small, 0.0f});
+  s.big = ff_add(s.big, {u.big, 0.0f});
+  s.none += u.none;
 }
 
-__device__ __forceinline__ Squares from_lane(const Squares &s, int o) {  // lane ^ o
-  return {{__shfl_xor_sync(0xffffffffu, s.mid.h, o), __shfl_xor_sync(0xffffffffu, s.mid.l, o)},
-          __shfl_xor_sync(0xffffffffu, s.small, o),
-          __shfl_xor_sync(0xffffffffu, s.big, o)};
+// The sum over the lanes that differ in the bits under 2 FIRST, in a fixed order.
+template <int FIRST>
+__device__ __forceinline__ ff warp_sum(ff x) {
+#pragma unroll
+  for (int o = FIRST; o > 0; o >>= 1)
+    x = ff_add(x, {__shfl_xor_sync(0xffffffffu, x.h, o), __shfl_xor_sync(0xffffffffu, x.l, o)});
+  return x;
+}
+// (Few lists hold others than the middle sum: adding up all took 1 us of a call.)
+template <int FIRST>
+__device__ __forceinline__ Squares warp_sum(Squares s) {
+  const bool all = __any_sync(0xffffffffu, s.others != 0.0f);
+  s.mid = warp_sum<FIRST>(s.mid);
+  if (!all) return s;
+  s.others = 1.0f;
+  s.small = warp_sum<FIRST>(s.small);
+  s.big = warp_sum<FIRST>(s.big);
+#pragma unroll
+  for (int o = FIRST; o > 0; o >>= 1) s.none += __shfl_xor_sync(0xffffffffu, s.none, o);
+  return s;
 }
 
 // The sum over the CTA's threads, in thread 0, in a fixed order.
 __device__ __forceinline__ Squares cta_sum(Squares s) {
   __shared__ Squares sums[kClipThreads / 32];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s = add(s, from_lane(s, o));
+  s = warp_sum<16>(s);
   if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
   __syncthreads();
-  if (threadIdx.x < 32) {
-    s = sums[threadIdx.x % (kClipThreads / 32)];
-#pragma unroll
-    for (int o = kClipThreads / 64; o > 0; o >>= 1) s = add(s, from_lane(s, o));
-  }
+  if (threadIdx.x < 32) s = warp_sum<kClipThreads / 64>(sums[threadIdx.x % (kClipThreads / 32)]);
   return s;
 }
 
@@ -131,22 +156,22 @@ __device__ __forceinline__ Squares cta_sum(Squares s) {
 __device__ __forceinline__ bool norm_of(const Squares &s, float *root, int *k) {
   float t = ff_round(s.mid);
   int unit = 0;
-  if (!(s.big == 0.0f)) {  // NaN too
-    t = s.big + t * 0x1p-96f * 0x1p-96f;
+  if (s.big.h != 0.0f) {
+    t = ff_round(s.big) + t * 0x1p-96f * 0x1p-96f;
     unit = 96;
   } else if (t > 0.0f) {
-    t += s.small * 0x1p-96f * 0x1p-96f;
+    t += ff_round(s.small) * 0x1p-96f * 0x1p-96f;
   } else {
-    t = s.small;
+    t = ff_round(s.small);
     unit = -96;
   }
   *k = 0;
   *root = 0.0f;
-  if (t == 0.0f) return true;
-  if (!isfinite(t)) {
-    *root = t;
+  if (!(s.none == 0.0f)) {  // NaN too
+    *root = s.none;
     return false;
   }
+  if (t == 0.0f) return true;
   int e;
   float m = frexpf(t, &e);  // m in [1/2, 1)
   e -= 1;                   // 2 m in [1, 2)
@@ -155,11 +180,11 @@ __device__ __forceinline__ bool norm_of(const Squares &s, float *root, int *k) {
   return true;
 }
 
-__device__ __forceinline__ void add_squares(Squares &s, float &unit, const float *x, int n) {
+__device__ __forceinline__ void add_squares(UnitSquares &s, const float *x, int n) {
   float q = 0.0f;
   for (int i = 0; i < n; ++i) q = fmaf(x[i], x[i], q);
   if (q >= kMidLeast && q <= kMidMost) {
-    unit += q;
+    s.mid += q;
     return;
   }
   const float f = q < 1.0f ? 0x1p96f : 0x1p-96f;
@@ -169,7 +194,8 @@ __device__ __forceinline__ void add_squares(Squares &s, float &unit, const float
     r = fmaf(y, y, r);
   }
   if (q < 1.0f) s.small += r;
-  else s.big += r;
+  else if (isfinite(r)) s.big += r;
+  else s.none += r;
 }
 
 __device__ __forceinline__ void widen(const uint4 &v, bool bf16, float (&x)[8]) {
@@ -234,29 +260,29 @@ __device__ __forceinline__ void add_unit(Squares &s, const ClipUnit &u, bool kee
     v[k] = make_uint4(0u, 0u, 0u, 0u);
     if (i < u.nvec) v[k] = APART ? load_as(body + i, policy) : __ldg(body + i);
   }
-  float sum = 0.0f;
+  UnitSquares sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int k = 0; k < kClipVecs; ++k) {
     float x[8];
     widen(v[k], bf16, x);
-    add_squares(s, sum, x, PER);
+    add_squares(sum, x, PER);
   }
   // what lies outside the 16-byte vectors: under PER entries at either end
   if ((int)threadIdx.x < u.count - u.nvec * PER) {
     const int i = (int)threadIdx.x < u.head ? threadIdx.x : threadIdx.x + u.nvec * PER;
     const float x = one_entry(u.in, i, bf16);
-    add_squares(s, sum, &x, 1);
+    add_squares(sum, &x, 1);
   }
-  s.mid = ff_add(s.mid, {sum, 0.0f});
+  add(s, sum);
 }
 
 // part[CTA]: the sum of its units' squares.
 template <int CAP, bool APART>
 __global__ void __launch_bounds__(kClipThreads, kClipCtas)
-    k_clip_squares(const __grid_constant__ ClipTable<CAP> t, float4 *part) {
+    k_clip_squares(const __grid_constant__ ClipTable<CAP> t, Squares *part) {
   let_next_start();
   wait_for_previous();
-  Squares s = {{0.0f, 0.0f}, 0.0f, 0.0f};
+  Squares s = {};
   int e = 0;
   for (uint32_t unit = blockIdx.x; unit < t.units; unit += gridDim.x) {
     if (e + 1 < t.n && t.e[e + 1].unit0 <= unit) e = clip_entry(t, e + 1, t.n - 1, unit);
@@ -266,18 +292,27 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
     else add_unit<4, APART>(s, u, keep);
   }
   s = cta_sum(s);
-  if (threadIdx.x == 0) part[blockIdx.x] = make_float4(s.mid.h, s.mid.l, s.small, s.big);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
 // The factor, from the partial sums (every CTA adds them in the same order); CTA 0
 // writes the norm.
-__device__ __forceinline__ float clip_factor(const float4 *part, int nparts, float max_norm,
+__device__ __forceinline__ float clip_factor(const Squares *part, int nparts, float max_norm,
                                              float *norm_out, int *status) {
   __shared__ float factor;
-  Squares s = {{0.0f, 0.0f}, 0.0f, 0.0f};
+  Squares s = {};
   for (int i = threadIdx.x; i < nparts; i += kClipThreads) {
-    const float4 v = __ldcg(part + i);
-    s = add(s, {{v.x, v.y}, v.z, v.w});
+    const float4 v = __ldcg(reinterpret_cast<const float4 *>(part + i));
+    s.mid = ff_add(s.mid, {v.x, v.y});
+    s.others += v.z;
+    s.none += v.w;
+  }
+  if (s.others != 0.0f) {
+    for (int i = threadIdx.x; i < nparts; i += kClipThreads) {
+      const float4 v = __ldcg(reinterpret_cast<const float4 *>(part + i) + 1);
+      s.small = ff_add(s.small, {v.x, v.y});
+      s.big = ff_add(s.big, {v.z, v.w});
+    }
   }
   s = cta_sum(s);
   if (threadIdx.x == 0) {
@@ -350,7 +385,7 @@ __device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
 
 template <int CAP, bool APART>
 __global__ void __launch_bounds__(kClipThreads, kClipCtas)
-    k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const float4 *part, int nparts,
+    k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const Squares *part, int nparts,
                  float max_norm, float *norm_out, int *status) {
   let_next_start();
   wait_for_previous();
@@ -370,7 +405,7 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
 
 // The norm alone.
 __global__ void __launch_bounds__(kClipThreads)
-    k_clip_norm(const float4 *part, int nparts, float *norm_out, int *status) {
+    k_clip_norm(const Squares *part, int nparts, float *norm_out, int *status) {
   let_next_start();
   wait_for_previous();
   clip_factor(part, nparts, INFINITY, norm_out, status);
@@ -383,7 +418,7 @@ static int clip_grid(int nsm) { return kClipCtas * nsm; }
 
 size_t clip_ws_bytes(int64_t n) {
   const int64_t launches = n > 0 ? (n + kClipLarge - 1) / kClipLarge : 1;
-  return kHeaderBytes + (size_t)launches * clip_grid(device_sm_count()) * sizeof(float4);
+  return kHeaderBytes + (size_t)launches * clip_grid(device_sm_count()) * sizeof(Squares);
 }
 
 // Entries first .. of the lists, as many as a table holds; returns the next one.
@@ -408,7 +443,7 @@ template <int CAP, bool APART>
 static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_t n,
                              float max_norm, float *norm, void *ws, cudaStream_t st) {
   const int most = clip_grid(device_sm_count());
-  float4 *part = reinterpret_cast<float4 *>(static_cast<char *>(ws) + kHeaderBytes);
+  Squares *part = reinterpret_cast<Squares *>(static_cast<char *>(ws) + kHeaderBytes);
   int *status = static_cast<int *>(ws);
   ClipTable<CAP> t;
   int nparts = 0;
@@ -423,7 +458,7 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
   }
   if (!out || nparts == 0) {
     const cudaError_t e =
-        launch_behind(k_clip_norm, dim3(1), kClipThreads, 0, st, (const float4 *)part, nparts,
+        launch_behind(k_clip_norm, dim3(1), kClipThreads, 0, st, (const Squares *)part, nparts,
                       norm, status);
     return cuda_fail(e, "gradient norm launch");
   }
@@ -435,7 +470,7 @@ static fqt_status clip_lists(const fqt_tensor *in, const fqt_tensor *out, int64_
     const int grid = t.units < (uint32_t)most ? (int)t.units : most;
     const cudaError_t e =
         launch_behind(k_clip_scale<CAP, APART>, dim3((unsigned)grid), kClipThreads, 0, st, t,
-                      (const float4 *)part, nparts, max_norm, first ? norm : nullptr, status);
+                      (const Squares *)part, nparts, max_norm, first ? norm : nullptr, status);
     if (e != cudaSuccess) return cuda_fail(e, "gradient clipping launch");
     first = false;
   }

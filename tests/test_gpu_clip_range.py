@@ -35,3 +35,13 @@ def test_many_large_entries(dtype, count, value):
     assert abs(float(norm) / want - 1) <= REL
     for end in (float(g.min()), float(g.max())):
         assert abs(end / (value / want) - 1) <= REL + 3 * 2.0 ** -24 + ROUND[dtype]
+
+
+@pytest.mark.parametrize("value", [1.1e-38, 1.1e-20, 1.3e-16, 0.7, 1.1e13, 1.1e20, 1.1e30])
+def test_long_lists_of_equal_entries(value):
+    """2^32 entries of any size: the sums of those whose squares fp32 does not hold keep
+    as many bits as the others'."""
+    t = torch.full((1 << 26,), value, device="cuda")
+    grads = fqt.TensorList([t] * 64)
+    want = math.sqrt(float(1 << 32)) * float(t[0].double())
+    assert abs(float(fqt.grad_norm(grads)) / want - 1) <= REL

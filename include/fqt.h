@@ -423,8 +423,10 @@ typedef struct fqt_tensor {
  * overlap.  out NULL: the norm alone.  norm (one fp32 entry, device memory):
  * written when non-NULL.  Every entry's square counts (fp32's whole range); up to
  * 65 of them are added in fp32, their sums in pairs of fp32, in an order that goes
- * by the sizes, the entries' place in 16 bytes and the GPU.  A norm that is
- * not finite records FQT_ENONFINITE and leaves the entries as they are.
+ * by the sizes, the entries' place in 16 bytes and the GPU.  An entry that is not
+ * finite records FQT_ENONFINITE, makes the norm infinite or NaN and leaves all
+ * entries as they are.  A norm of finite entries that passes fp32's range is
+ * written as infinity; the entries are scaled by what it is.
  * n <= 2^24.  Workspace: fqt_clip_grad_norm_workspace_size(n) bytes.
  */
 FQT_API size_t fqt_clip_grad_norm_workspace_size(int64_t n);

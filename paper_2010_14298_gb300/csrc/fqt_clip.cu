@@ -295,11 +295,30 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
+// The factor f times a power of two p.  p is 1 unless the factor is below 2^-100, where
+// f alone would leave fp32's normal numbers and the products, no smaller for it than
+// the largest norm asked for, would have as few bits as f.  Then f is 1/4 to 1/2 (p is
+// not below 2^-148), so x f does not overflow and x f p is rounded once.
+struct Factor {
+  float f, p;
+  __device__ __forceinline__ bool one() const { return f == 1.0f; }
+  __device__ __forceinline__ float of(float x) const { return x * f * p; }
+};
+
+// quotient 2^-k, the quotient in fp32
+__device__ __forceinline__ Factor make_factor(float quotient, int k) {
+  int e;
+  const float m = frexpf(quotient, &e);  // m in [1/2, 1), or 0
+  if (e - k >= -100) return {ldexpf(quotient, -k), 1.0f};
+  const int down = min(k - e - 1, 148);
+  return {ldexpf(m, e - k + down), ldexpf(1.0f, -down)};
+}
+
 // The factor, from the partial sums (every CTA adds them in the same order); CTA 0
 // writes the norm.
-__device__ __forceinline__ float clip_factor(const Squares *part, int nparts, float max_norm,
+__device__ __forceinline__ Factor clip_factor(const Squares *part, int nparts, float max_norm,
                                              float *norm_out, int *status) {
-  __shared__ float factor;
+  __shared__ Factor factor;
   Squares s = {};
   for (int i = threadIdx.x; i < nparts; i += kClipThreads) {
     const float4 v = __ldcg(reinterpret_cast<const float4 *>(part + i));
@@ -321,7 +340,7 @@ __device__ __forceinline__ float clip_factor(const Squares *part, int nparts, fl
     const bool good = norm_of(s, &root, &k);
     const float norm = ldexpf(root, k);  // infinite where it passes fp32
     // max_norm / norm, the quotient of numbers in fp32's middle first
-    factor = good && norm > max_norm ? ldexpf(max_norm / root, -k) : 1.0f;
+    factor = good && norm > max_norm ? make_factor(max_norm / root, k) : Factor{1.0f, 1.0f};
     if (blockIdx.x == 0) {
       if (norm_out) *norm_out = norm;
       if (!good) record_status(status, FQT_ENONFINITE);
@@ -332,7 +351,7 @@ __device__ __forceinline__ float clip_factor(const Squares *part, int nparts, fl
 }
 
 template <int PER, bool APART>
-__device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
+__device__ __forceinline__ void scale_unit(const ClipUnit &u, const Factor f) {
   const bool bf16 = PER == 8;
   // vectors where the output lies on the same bytes of 16 as the input
   const bool vec = ((reinterpret_cast<uintptr_t>(u.in) ^ reinterpret_cast<uintptr_t>(u.out)) &
@@ -357,13 +376,13 @@ __device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (bf16) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * j] * f, x[2 * j + 1] * f);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f.of(x[2 * j]), f.of(x[2 * j + 1]));
         w[j] = *reinterpret_cast<const uint32_t *>(&b);
       } else {
-        w[j] = __float_as_uint(x[j] * f);
+        w[j] = __float_as_uint(f.of(x[j]));
       }
     }
-    const uint4 y = f == 1.0f ? v[k] : make_uint4(w[0], w[1], w[2], w[3]);
+    const uint4 y = f.one() ? v[k] : make_uint4(w[0], w[1], w[2], w[3]);
     if constexpr (APART) store_as(out + i, y, policy);
     else out[i] = y;
   }
@@ -373,12 +392,12 @@ __device__ __forceinline__ void scale_unit(const ClipUnit &u, float f) {
     const int i = j < head ? j : j + nvec * PER;
     if (bf16) {
       const unsigned short raw = reinterpret_cast<const unsigned short *>(u.in)[i];
-      const __nv_bfloat16 y = __float2bfloat16_rn(one_entry(u.in, i, true) * f);
-      reinterpret_cast<unsigned short *>(u.out)[i] = f == 1.0f ? raw : __bfloat16_as_ushort(y);
+      const __nv_bfloat16 y = __float2bfloat16_rn(f.of(one_entry(u.in, i, true)));
+      reinterpret_cast<unsigned short *>(u.out)[i] = f.one() ? raw : __bfloat16_as_ushort(y);
     } else {
       const uint32_t raw = reinterpret_cast<const uint32_t *>(u.in)[i];
       reinterpret_cast<uint32_t *>(u.out)[i] =
-          f == 1.0f ? raw : __float_as_uint(__uint_as_float(raw) * f);
+          f.one() ? raw : __float_as_uint(f.of(__uint_as_float(raw)));
     }
   }
 }
@@ -389,14 +408,14 @@ __global__ void __launch_bounds__(kClipThreads, kClipCtas)
                  float max_norm, float *norm_out, int *status) {
   let_next_start();
   wait_for_previous();
-  const float f = clip_factor(part, nparts, max_norm, norm_out, status);
+  const Factor f = clip_factor(part, nparts, max_norm, norm_out, status);
   int e = t.n - 1;
   // the units of the CTA of this number in the first pass, from the last to the first
   const uint32_t mine = (t.units - 1 - blockIdx.x) / gridDim.x;
   for (uint32_t k = 0; k <= mine; ++k) {
     const uint32_t unit = blockIdx.x + (mine - k) * gridDim.x;
     if (t.e[e].unit0 > unit) e = clip_entry(t, 0, e - 1, unit);
-    if (f == 1.0f && t.e[e].in == t.e[e].out) continue;  // nothing to change in place
+    if (f.one() && t.e[e].in == t.e[e].out) continue;  // nothing to change in place
     const ClipUnit u = clip_unit(t.e[e], unit);
     if (u.bf16) scale_unit<8, APART>(u, f);
     else scale_unit<4, APART>(u, f);

@@ -45,3 +45,23 @@ def test_long_lists_of_equal_entries(value):
     grads = fqt.TensorList([t] * 64)
     want = math.sqrt(float(1 << 32)) * float(t[0].double())
     assert abs(float(fqt.grad_norm(grads)) / want - 1) <= REL
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("max_norm", [1e30, 1.0, 1e-3, 1e-30])
+@pytest.mark.parametrize("top", [1e37, 3e38])
+def test_factors_that_fp32_does_not_hold(top, max_norm, dtype):
+    """max_norm / norm under fp32's normal numbers, or under all of them: the entries,
+    which are no larger than the norm, are still rounded once.  A norm past fp32 is
+    written as infinity, and is no entry that is not finite."""
+    grads = [(torch.linspace(0.1, 1.0, n, device="cuda") * top).to(dtype) for n in (40003, 7, 512)]
+    want = math.sqrt(math.fsum(float((g.double() ** 2).sum()) for g in grads))
+    out = [torch.full_like(g, 7.0) for g in grads]
+    ws = fqt.Workspace.of_size(fqt.clip_grad_norm_workspace_size(grads))
+    norm = float(fqt.clip_grad_norm(grads, max_norm, out=out, ws=ws))
+    assert fqt.sync_status(ws) == 0
+    assert norm == math.inf if want > 3.5e38 else abs(norm / want - 1) <= REL
+    for g, o in zip(grads, out):
+        ref = g.double() * (max_norm / want)
+        tol = (REL + 3 * 2.0 ** -24 + ROUND[dtype]) * ref.abs()
+        assert ((o.double() - ref).abs() <= tol).all()

@@ -148,7 +148,8 @@ class FfnBlock:
         return diff.square().sum() / (2 * x.shape[0])
 
     def check(self) -> int:
-        """The first condition that the kernels of the last steps recorded, or 0."""
+        """A condition that the kernels of the steps since the last call recorded, or 0
+        (the up projection's before the down projection's, the norm's and the clipping's)."""
         states = [self.up.check(), self.down.check(), fqt.sync_status(self.ws)]
         return next((s for s in states if s), 0)
 
@@ -178,8 +179,9 @@ def main(argv=None):
         end.synchronize()
         times.append(start.elapsed_time(end))
         print(f"step {i}: loss {float(loss):.4f}, gradient norm {float(block.norm):.4f}")
-    if block.check():
-        raise SystemExit(f"a kernel recorded: {fqt.status_string(block.check())}")
+    state = block.check()  # which clears it
+    if state:
+        raise SystemExit(f"a kernel recorded: {fqt.status_string(state)}")
     print(f"{a.format}: {sorted(times)[len(times) // 2]:.3f} ms a step")
 
 

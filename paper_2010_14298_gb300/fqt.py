@@ -604,29 +604,49 @@ def _row_stride(t, rows, cols):
     return ld if rows > 1 else cols
 
 
+# A kernel follows any address: a call's other tensors and its workspace are on the
+# first tensor's GPU, by its number.
+def _elsewhere(t, name, dev):
+    if dev < 0:
+        return ValueError(f"{name} is not on a GPU")
+    return ValueError(f"{name} is on {t.device}, not on GPU {dev} as the call's first tensor")
+
+
+def _scratch(ws, dev):
+    """A workspace's bytes and their number."""
+    buf = ws.buf
+    if buf.get_device() != dev:
+        raise _elsewhere(buf, "the workspace", dev)
+    return buf, ws.nbytes
+
+
 def _matrix(t, name):
-    if not t.is_cuda:
-        raise ValueError(f"{name} is not on a GPU")
     if t.dim() != 2:
         raise ValueError(f"{name} has {t.dim()} dimensions, not two")
     return t.shape
 
 
 def _rows_in(t, name, stream):
-    """A matrix to read, its sizes and its row pitch; one laid out otherwise is copied."""
+    """A matrix to read, its sizes, its row pitch and its GPU; one laid out otherwise is
+    copied."""
+    dev = t.get_device()
+    if dev < 0:
+        raise _elsewhere(t, name, dev)
     rows, cols = _matrix(t, name)
     ld = _row_stride(t, rows, cols)
     if ld is None:
         with _on(stream):
             t = t.contiguous()
         ld = cols
-    return t, rows, cols, ld
+    return t, rows, cols, ld, dev
 
 
-def _rows_out(t, name, rows, cols, dtype, like, stream):
+def _rows_out(t, name, rows, cols, dtype, dev, like, stream):
     """A matrix to write (a new one for None), and its row pitch."""
     if t is None:
         return _new((rows, cols), dtype, like, stream), cols
+    if t.get_device() != dev:
+        raise _elsewhere(t, name, dev)
     if t.dtype != dtype or _matrix(t, name) != (rows, cols):
         raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, not {dtype} {(rows, cols)}")
     ld = _row_stride(t, rows, cols)
@@ -635,12 +655,15 @@ def _rows_out(t, name, rows, cols, dtype, like, stream):
     return t, ld
 
 
-def _vector(t, name, n, like=None, stream=None):
+_f32 = torch.float32
+
+
+def _vector(t, name, n, dev, like=None, stream=None):
     """n contiguous fp32 entries on the GPU (new ones for None, where `like` is given)."""
     if t is None:
         return None if like is None else _new((n,), torch.float32, like, stream)
-    if not (t.is_cuda and t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()):
-        raise ValueError(f"{name} is no contiguous float32 vector of {n} entries on the GPU")
+    if not (t.get_device() == dev and t.dtype is _f32 and t.numel() == n and t.is_contiguous()):
+        raise ValueError(f"{name} is no contiguous float32 vector of {n} entries on GPU {dev}")
     return t
 
 
@@ -650,12 +673,12 @@ def layer_norm_forward(X: torch.Tensor, gamma: Optional[torch.Tensor] = None,
                        rstd: torch.Tensor = None, stream=None):
     """(Y, mean, rstd): layer norm of the rows of X (fqt_layer_norm_forward).
     gamma and beta are fp32 (None: 1 and 0); Y has X's type."""
-    X, rows, cols, ldx = _rows_in(X, "X", stream)
-    _vector(gamma, "gamma", cols)
-    _vector(beta, "beta", cols)
-    Y, ldy = _rows_out(out, "out", rows, cols, X.dtype, X, stream)
-    mean = _vector(mean, "mean", rows, X, stream)
-    rstd = _vector(rstd, "rstd", rows, X, stream)
+    X, rows, cols, ldx, dev = _rows_in(X, "X", stream)
+    _vector(gamma, "gamma", cols, dev)
+    _vector(beta, "beta", cols, dev)
+    Y, ldy = _rows_out(out, "out", rows, cols, X.dtype, dev, X, stream)
+    mean = _vector(mean, "mean", rows, dev, X, stream)
+    rstd = _vector(rstd, "rstd", rows, dev, X, stream)
     st = native().layer_norm_forward(X, ldx, _dtype_code(X), rows, cols, gamma, beta, eps, Y, ldy,
                                      mean, rstd, _raw_stream(stream))
     if st:
@@ -676,24 +699,26 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
     and grad_w choose them, None stands for one that was not asked for."""
     if dY.shape != X.shape or dY.dtype != X.dtype:
         raise ValueError(f"dY is {dY.dtype} {tuple(dY.shape)}, X {X.dtype} {tuple(X.shape)}")
-    X, rows, cols, ldx = _rows_in(X, "X", stream)
-    dY, _, _, lddy = _rows_in(dY, "dY", stream)
-    _vector(mean, "mean", rows)
-    _vector(rstd, "rstd", rows)
-    _vector(gamma, "gamma", cols)
-    dX, lddx, dgamma, dbeta, nbytes = None, cols, None, None, 0
+    X, rows, cols, ldx, dev = _rows_in(X, "X", stream)
+    dY, _, _, lddy, there = _rows_in(dY, "dY", stream)
+    if there != dev:
+        raise _elsewhere(dY, "dY", dev)
+    _vector(mean, "mean", rows, dev)
+    _vector(rstd, "rstd", rows, dev)
+    _vector(gamma, "gamma", cols, dev)
+    dX, lddx, dgamma, dbeta, buf, nbytes = None, cols, None, None, None, 0
     if grad_x:
-        dX, lddx = _rows_out(out_x, "out_x", rows, cols, X.dtype, X, stream)
+        dX, lddx = _rows_out(out_x, "out_x", rows, cols, X.dtype, dev, X, stream)
     if grad_w:
-        dgamma = _vector(out_gamma, "out_gamma", cols, X, stream)
-        dbeta = _vector(out_beta, "out_beta", cols, X, stream)
+        dgamma = _vector(out_gamma, "out_gamma", cols, dev, X, stream)
+        dbeta = _vector(out_beta, "out_beta", cols, dev, X, stream)
         if ws is None:
             with _on(stream):
                 ws = Workspace.of_size(layer_norm_workspace_size(rows, cols), X.device)
-        nbytes = ws.nbytes
+        buf, nbytes = _scratch(ws, dev)
     st = native().layer_norm_backward(dY, lddy, X, ldx, _dtype_code(X), rows, cols, mean, rstd,
-                                      gamma, dX, lddx, dgamma, dbeta,
-                                      ws.buf if grad_w else None, nbytes, _raw_stream(stream))
+                                      gamma, dX, lddx, dgamma, dbeta, buf, nbytes,
+                                      _raw_stream(stream))
     if st:
         _check(st, "fqt_layer_norm_backward")
     return dX, dgamma, dbeta
@@ -765,14 +790,14 @@ class Fp8Tensor:
         return v * s.repeat_interleave(FP8_BLOCK, 1)[:, :self.cols]
 
 
-def _fp8_out(t, name, rows, cols, block_rows, like, stream):
+def _fp8_out(t, name, rows, cols, block_rows, dev, like, stream):
     if t is None:
         with _on(stream):
             return Fp8Tensor.empty(rows, cols, block_rows, like.device)
     if t.rows != rows or t.cols != cols:
         raise ValueError(f"{name} is {t.rows} x {t.cols}, not {rows} x {cols}")
-    if not t.codes.is_cuda:
-        raise ValueError(f"{name} is not on a GPU")
+    if t.codes.get_device() != dev:
+        raise _elsewhere(t.codes, name, dev)
     return t
 
 
@@ -781,15 +806,16 @@ def quantize_fp8(X: torch.Tensor, block_rows: int = 1, q: Fp8Tensor = None, qt: 
     """(X, X^T) in 8-bit floating point (fqt_quantize_fp8): the blocks of the first
     run along X's rows, those of the second along its columns.  `rows` and `cols` ask
     for them (a tensor given for one does too), None stands for one that was not."""
-    X, n, k, ldx = _rows_in(X, "X", stream)
+    X, n, k, ldx, dev = _rows_in(X, "X", stream)
     if rows or q is not None:
-        q = _fp8_out(q, "q", n, k, block_rows, X, stream)
+        q = _fp8_out(q, "q", n, k, block_rows, dev, X, stream)
     if cols or qt is not None:
-        qt = _fp8_out(qt, "qt", k, n, block_rows, X, stream)
+        qt = _fp8_out(qt, "qt", k, n, block_rows, dev, X, stream)
     if ws is None:
         with _on(stream):
             ws = Workspace.of_size(256, X.device)
-    st = native().quantize_fp8(X, ldx, _dtype_code(X), n, k, block_rows, q, qt, ws.buf, ws.nbytes,
+    buf, nbytes = _scratch(ws, dev)
+    st = native().quantize_fp8(X, ldx, _dtype_code(X), n, k, block_rows, q, qt, buf, nbytes,
                                _raw_stream(stream))
     if st:
         _check(st, "fqt_quantize_fp8")
@@ -808,17 +834,20 @@ def fp8_matmul(A: Fp8Tensor, B: Fp8Tensor, out: torch.Tensor = None, dtype=torch
     """A B^T (fqt_fp8_matmul) in out's type, or a new tensor of `dtype`."""
     if A.cols != B.cols:
         raise ValueError(f"A has {A.cols} columns, B {B.cols}")
-    if not (A.codes.is_cuda and B.codes.is_cuda):
-        raise ValueError("A and B are not on a GPU")
+    dev = A.codes.get_device()
+    if dev < 0:
+        raise _elsewhere(A.codes, "A", dev)
+    if B.codes.get_device() != dev:
+        raise _elsewhere(B.codes, "B", dev)
     if out is not None:
         dtype = out.dtype
-    out, ldo = _rows_out(out, "out", A.rows, B.rows, dtype, A.codes, stream)
+    out, ldo = _rows_out(out, "out", A.rows, B.rows, dtype, dev, A.codes, stream)
     if ws is None:
         with _on(stream):
             ws = Workspace.of_size(fp8_matmul_workspace_size(A.rows, B.rows, A.cols),
                                    A.codes.device)
-    st = native().fp8_matmul(A, B, _dtype_code(out), out, ldo, ws.buf, ws.nbytes,
-                             _raw_stream(stream))
+    buf, nbytes = _scratch(ws, dev)
+    st = native().fp8_matmul(A, B, _dtype_code(out), out, ldo, buf, nbytes, _raw_stream(stream))
     if st:
         _check(st, "fqt_fp8_matmul")
     return out
@@ -866,13 +895,14 @@ def _clip(grads, out, max_norm, norm, ws, stream):
         if out is not grads and (out._kinds != grads._kinds
                                  or out[0].device != grads[0].device):
             raise ValueError("out has other sizes, types or another GPU than the gradients")
-    norm = _vector(norm, "norm", 1, grads[0], stream)
+    dev = grads[0].get_device()
+    norm = _vector(norm, "norm", 1, dev, grads[0], stream)
     if ws is None:
         with _on(stream):
             ws = Workspace.of_size(clip_grad_norm_workspace_size(grads), grads[0].device)
+    buf, nbytes = _scratch(ws, dev)
     st = native().clip_grad_norm(grads.address, out.address if out is not None else None,
-                                 len(grads), max_norm, norm, ws.buf, ws.nbytes,
-                                 _raw_stream(stream))
+                                 len(grads), max_norm, norm, buf, nbytes, _raw_stream(stream))
     if st:
         _check(st, "fqt_clip_grad_norm")
     return norm

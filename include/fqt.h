@@ -396,8 +396,9 @@ FQT_API fqt_status fqt_quantize_fp8(const void *X, int64_t ldx, fqt_dtype dtype,
  * out = A B^T (M x N, fp32 or bf16) of A (M x K) and B (N x K):
  *   out_mn = sum over K blocks of sa sb sum_(k in block) E4M3(a_mk) E4M3(b_nk),
  * exact products summed on the tensor cores in fp32, which drop what lies below
- * an accumulator's last bit: for an fp32 output at most 1024 terms to an
- * accumulator, the accumulators then added in fp32; one rounding to bf16.  A
+ * an accumulator's last bit at every 32 terms: at most 1024 terms to an
+ * accumulator for an fp32 output and 8192 for a bf16 one, the accumulators then
+ * added in fp32; one rounding to bf16.  A
  * linear layer's passes, for X (tokens x D), W (C x D) and dH (tokens x C): the
  * forward from X and W, grad_X from dH and W^T, grad_W from dH^T and X^T.
  * M, N, K <= 2^22.  Workspace: fqt_fp8_matmul_workspace_size(M, N, K) bytes.

@@ -409,12 +409,13 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
 // accumulators, took 101, and 38 us where 256 take 25: 4096 x 1024 x 8192 in bf16).
 constexpr int kF8EpiWarps = 8, kF8Epi0 = 4;  // warps 0 loads, 1 products, 2 and 3 scales
 constexpr int kF8Threads = 32 * (kF8Epi0 + kF8EpiWarps);
-// K blocks of an accumulator of an fp32 output: a step of the tensor core drops what lies
-// below the accumulator's last bit (5e-7 of the result after 8192 terms of equal size,
-// over 1e-6 where a few terms are large, 8e-6 after 65536), so every 1024 terms the sums
-// move to fp32 registers, rounded to nearest.  A bf16 output rounds a thousand times as
-// much away: one accumulator takes all of K.
-constexpr int kF8Chunk = 8;
+// K blocks of an accumulator: a step of the tensor core drops what lies below the
+// accumulator's last bit, which adds up where the terms have one sign (5e-7 of the result
+// after 8192 terms of equal size, 8e-6 after 65536; 3e-4 there, and 1.8e-2 after 2^21,
+// where the first few terms are as large as all others together).  So after 1024 terms
+// for an fp32 output, and after 8192 for a bf16 one, which rounds up to 4e-3 away, the
+// sums move to fp32 registers, rounded to nearest.
+constexpr int kF8Chunk = 8, kF8ChunkBf16 = 64;
 constexpr int kF8Group = 4;             // K blocks whose scales share a 32-bit word
 constexpr int kF8Ring = 4;              // groups of scales in shared memory
 constexpr size_t kF8RingBytes = 1536;   // 128 of A's rows, up to 256 of B's
@@ -430,6 +431,7 @@ struct F8Args {
   int64_t spa, spb;
   int64_t M, N;  // rows of A and of B
   int nkb;       // K blocks
+  int chunk;     // of them, to an accumulator
   int m_tiles, n_tiles, splits, kb_per;
   int64_t items;
   void *out;
@@ -707,7 +709,7 @@ __device__ __forceinline__ void f8_join(const F8Args &g, int64_t it, const float
 // and 3 in turn the scales of four K blocks, warp 1 issues a K block's four products;
 // the eight epilogue warps (quadrant of rows x half of the columns) take an accumulator
 // into registers, hand it back and store it.  ACCS accumulators of NT columns: with two
-// the products go on meanwhile.  FOLD: an accumulator holds kF8Chunk K blocks, and the
+// the products go on meanwhile.  FOLD: an accumulator holds g.chunk K blocks, and the
 // epilogue adds them up.
 template <int NT, int ACCS, bool PAIR, bool FOLD>
 __global__ void __launch_bounds__(kF8Threads, 1)
@@ -789,7 +791,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       if constexpr (FOLD)
 #pragma unroll
         for (int i = 0; i < 32 * P; ++i) v[i / 32][i % 32] = 0u;
-      for (int kb = t.kb0; kb < t.kb1; kb = FOLD ? kb + kF8Chunk : t.kb1, ++c) {
+      for (int kb = t.kb0; kb < t.kb1; kb = FOLD ? kb + g.chunk : t.kb1, ++c) {
         const int buf = c % ACCS;
         if (!f8_wait(&accf[buf], (c / ACCS) & 1u, g.status)) {
           *abort_flag = 1;
@@ -924,8 +926,8 @@ __global__ void __launch_bounds__(kF8Threads, 1)
       for (int64_t it = first; ok && it < g.items && !*abort_flag; it += step) {
         const F8Item t = f8_item<NT, PAIR>(g, it);
         uint32_t sa = 0;
-        for (int k0 = t.kb0; ok && k0 < t.kb1; k0 = FOLD ? k0 + kF8Chunk : t.kb1, ++c) {
-          const int k1 = FOLD ? min(k0 + kF8Chunk, t.kb1) : t.kb1, buf = c % ACCS;
+        for (int k0 = t.kb0; ok && k0 < t.kb1; k0 = FOLD ? k0 + g.chunk : t.kb1, ++c) {
+          const int k1 = FOLD ? min(k0 + g.chunk, t.kb1) : t.kb1, buf = c % ACCS;
           if (!f8_wait(&acce[buf], ((c / ACCS) & 1u) ^ 1u, g.status)) {
             ok = false;
             break;
@@ -1182,7 +1184,8 @@ static fqt_status launch_f8_as(const CUtensorMap &ta, const CUtensorMap &tb, con
 template <int NT, int ACCS, bool PAIR>
 static fqt_status launch_f8(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &to,
                             F8Args &g, int nsm, cudaStream_t st) {
-  if (!g.bf16 && g.kb_per > kF8Chunk)
+  g.chunk = g.bf16 ? kF8ChunkBf16 : kF8Chunk;
+  if (g.kb_per > g.chunk)
     return launch_f8_as<NT, ACCS, PAIR, true>(ta, tb, to, g, nsm, st);
   return launch_f8_as<NT, ACCS, PAIR, false>(ta, tb, to, g, nsm, st);
 }

@@ -33,6 +33,18 @@ def _bound(K, per):
     return min(K, per) / 32 * 2.0 ** -23 + (-(-K // per) + 8) * 2.0 ** -24
 
 
+# tiles of pairs, of single CTAs, and shared by clusters
+@pytest.mark.parametrize("first", [0.0, 2.0])
+@pytest.mark.parametrize("M,N,K", [(2048, 2048, 16384), (2048, 2048, 65536), (1280, 1280, 65536),
+                                   (40, 5000, 65536), (128, 256, 524288)])
+def test_fp32_outputs_of_one_sign(M, N, K, first):
+    a, _ = fqt.quantize_fp8(_rows(M, K, 1, first))
+    b, _ = fqt.quantize_fp8(_rows(N, K, 2))
+    want = a.dequantize().double() @ b.dequantize().double().t()
+    out = fqt.fp8_matmul(a, b)
+    assert ((out.double() / want - 1).abs() <= _bound(K, 1024)).all()
+
+
 def _repeated(q, times):
     """q's rows, all of them that many times."""
     return fqt.Fp8Tensor(q.codes.repeat(times, 1), q.scales.repeat(1, times, 1), q.rows * times,

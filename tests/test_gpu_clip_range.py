@@ -65,3 +65,27 @@ def test_factors_that_fp32_does_not_hold(top, max_norm, dtype):
         ref = g.double() * (max_norm / want)
         tol = (REL + 3 * 2.0 ** -24 + ROUND[dtype]) * ref.abs()
         assert ((o.double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("counts", [[64, 3, 100_000] * 700, [5] * 1021, [1 << 20] * 90],
+                         ids=["2100", "1021", "90"])
+def test_in_place_as_into_other_tensors(counts):
+    """The same bits, over more tensors than one launch takes too, and none changed where
+    the norm is small enough."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    grads = [torch.randn(n, generator=gen, device="cuda").to(
+        torch.bfloat16 if i % 3 == 0 else torch.float32) for i, n in enumerate(counts)]
+    before = [g.clone() for g in grads]
+    want = math.sqrt(math.fsum(float((g.double() ** 2).sum()) for g in grads))
+    out = [torch.full_like(g, 7.0) for g in grads]
+    apart = fqt.clip_grad_norm(grads, want / 3, out=out)
+    norm = fqt.clip_grad_norm(grads, want / 3)
+    assert torch.equal(norm, apart) and abs(float(norm) / want - 1) <= REL
+    for g, o, b in zip(grads, out, before):
+        assert torch.equal(g, o)
+        ref = b.double() / 3
+        assert ((g.double() - ref).abs()
+                <= (REL + 3 * 2.0 ** -24 + ROUND[g.dtype]) * ref.abs()).all()
+    fqt.clip_grad_norm(grads, want)
+    assert all(torch.equal(g, o) for g, o in zip(grads, out))

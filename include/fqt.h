@@ -366,7 +366,7 @@ FQT_API fqt_status fqt_layer_norm_backward(const void *dY, int64_t lddy, const v
  */
 typedef struct fqt_fp8 {
   int64_t rows, cols;
-  int64_t pitch;       /* bytes between rows of codes: a multiple of 16, >= cols */
+  int64_t pitch;       /* bytes between rows of codes: a multiple of 16, >= cols, < 2^40 */
   int32_t block_rows;  /* rows that share a scale: 1 or 128 */
   int32_t reserved;
   uint8_t *codes;      /* rows x pitch bytes, 16-byte aligned (bytes past cols are not read;

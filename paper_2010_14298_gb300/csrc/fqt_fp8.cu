@@ -1196,10 +1196,10 @@ static bool f8_aligned(const void *p, size_t n) {
 
 static int64_t scale_rows(int64_t rows) { return (rows + kF8Block - 1) / kF8Block * kF8Block; }
 
-// a code matrix whose rows and pitch stay inside 32-bit coordinates and 64-bit offsets
+// a code matrix whose pitch a tensor map takes, and its offsets 64 bits
 static bool f8_good(const fqt_fp8 *q) {
   return q->codes && q->scales && f8_aligned(q->codes, 16) && f8_aligned(q->scales, 16) &&
-         q->pitch % 16 == 0 && q->pitch >= q->cols;
+         q->pitch % 16 == 0 && q->pitch >= q->cols && q->pitch < ((int64_t)1 << 40);
 }
 
 fqt_status quantize_fp8(const void *X, int64_t ldx, bool bf16, int64_t rows, int64_t cols,

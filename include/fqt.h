@@ -320,7 +320,8 @@ FQT_API fqt_status fqt_grad_w_fixed_scratch(const fqt_qtensor *q_b1,
  * hold, but their tensors need only the alignment of their entries, and rows
  * may be any number of entries apart (`ld...`, at least the number of columns
  * where there is more than one row).  Entries on 16 bytes are read faster, and
- * the order of an fp32 sum goes by that and by the sizes, never by timing.
+ * the order of an fp32 sum goes by that, by the sizes and by the GPU, never by
+ * timing.
  * Outputs may not overlap inputs.
  */
 
@@ -370,7 +371,7 @@ typedef struct fqt_fp8 {
   int32_t block_rows;  /* rows that share a scale: 1 or 128 */
   int32_t reserved;
   uint8_t *codes;      /* rows x pitch bytes, 16-byte aligned (bytes past cols are not read;
-                          the quantizer writes those up to a multiple of 16) */
+                          the quantizer may write those up to a multiple of 16) */
   uint8_t *scales;     /* 4 ceil(cols / 512) P bytes, P = rows rounded up to a multiple
                           of 128: the byte of block kb of row r at
                           ((kb / 4) P + r) 4 + kb % 4 (with block_rows 128 the same for

@@ -254,8 +254,8 @@ struct NormRing {
 
 // Forward.  S > 0: rows come through S stages of shared memory.  A group takes R rows
 // at a time, whose sums share shuffles and barriers.  32768 x 4096 in bf16: 90 us, 6.0
-// TB/s; in fp32 167 us, 6.4 TB/s; 8192 x 1024 in bf16 6.6 us for a floor of 5 (a copy of
-// as much that stays in L2 takes 3.8).
+// TB/s; in fp32 167 us, 6.4 TB/s; 8192 x 1024 in bf16 8.3 us on new rows, for a floor of
+// 5, and 6.6 on rows that stay in L2 from call to call (a copy of as much takes 3.8 there).
 template <typename T, int V, int VPT, int R, int S>
 __global__ void __launch_bounds__(kNormThreads)
     k_norm_fwd(const NormArgs a, int G) {
@@ -377,7 +377,8 @@ __global__ void __launch_bounds__(kNormThreads)
 // Backward.  The column sums of a group's rows stay in its registers; at the end the
 // groups of a CTA add theirs in shared memory, and each CTA writes one row of partial
 // sums (k_norm_cols adds those).  32768 x 4096 in bf16: 133 us with k_norm_cols, 6.0
-// TB/s; in fp32 261 us, 6.2 TB/s; 8192 x 1024 in bf16 12.5 us for a floor of 7.6.
+// TB/s; in fp32 261 us, 6.2 TB/s; 8192 x 1024 in bf16 16.0 us on new rows, for a floor of
+// 7.6, and 12.5 on rows that stay in L2 from call to call.
 template <typename T, int V, int VPT, int S>
 __global__ void __launch_bounds__(kNormThreads)
     k_norm_bwd(const NormArgs a, int G) {
@@ -713,7 +714,8 @@ static NormPlan norm_plan(int64_t rows, int64_t cols, bool bf16, bool vec, bool 
   // a row a CTA: 16 bytes a thread (one row of 1024: 1.8 us, with 16 entries a thread 2.3)
   p.thin = vec && rows <= nsm && nvec <= kNormThreads;
   // Forward: 32 entries a thread need half the shuffles and smaller barriers (8192 x 1024
-  // in bf16 6.6 us, with 16 entries 8.3; 32768 x 4096 90 and 98, in fp32 167 and 184), if
+  // in bf16 8.3 us, with 16 entries 8.9, and 6.6 and 8.3 on rows in L2; 32768 x 4096 90 and
+  // 98, in fp32 167 and 184), if
   // they do not leave a third of the threads idle (21276 x 1088 24.3 us and 22.8), and in
   // fp32 if a CTA holds more than two rows at a time or 16 entries would not hold the row
   // (10000 x 8192 110 us and 98; 20000 x 5120 132 and 144; 5000 x 12288 90, read three

@@ -6,8 +6,8 @@ One training step is the layer norm, the two linear layers in a low-bit format,
 their gradients, the norm's gradients, and the clipping of all gradients to a global
 norm.  The linear layers run in 8-bit floating point with a scale per block of 128
 ("fp8"), or fully quantized ("int8": 8-bit activations and weights, 8-bit BHQ output
-gradients, 8-bit stochastic gradients for the weights).  Everything that a step writes
-is allocated once.
+gradients, 8-bit stochastic gradients for the weights).  What these operators write is
+allocated once; the ReLU, the residual sums and the loss between them are PyTorch's.
 
     python -m paper_2010_14298_gb300.ffn --tokens 8192 --width 1024 --hidden 4096
 """

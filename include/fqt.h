@@ -408,6 +408,64 @@ FQT_API size_t fqt_fp8_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
 FQT_API fqt_status fqt_fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, fqt_dtype dtype, void *out,
                                   int64_t ldo, void *workspace, size_t ws_bytes, void *stream);
 
+/*
+ * out = A1 B1^T + A2 B2^T (M x N) of A1 (M x K1), B1 (N x K1), A2 (M x K2), B2
+ * (N x K2): one product whose K blocks are those of both pairs, summed and rounded as
+ * fqt_fp8_matmul's.  The gradient of an input that two projections share, for the
+ * gradients of their outputs and W^T of each.  Either K may be 0.
+ */
+FQT_API size_t fqt_fp8_matmul_sum_workspace_size(int64_t M, int64_t N, int64_t K1, int64_t K2);
+FQT_API fqt_status fqt_fp8_matmul_sum(const fqt_fp8 *A1, const fqt_fp8 *B1, const fqt_fp8 *A2,
+                                      const fqt_fp8 *B2, fqt_dtype dtype, void *out, int64_t ldo,
+                                      void *workspace, size_t ws_bytes, void *stream);
+
+/* The activation of a gated feed-forward block. */
+typedef enum fqt_act {
+  FQT_SILU = 0,      /* g / (1 + e^-g) */
+  FQT_GELU = 1,      /* g Phi(g), Phi the normal distribution function */
+  FQT_GELU_TANH = 2, /* g / (1 + e^-z), z = 2 (2/pi)^(1/2) (g + 0.044715 g^3) */
+  FQT_RELU = 3,      /* max(g, 0) */
+  FQT_SIGMOID = 4    /* 1 / (1 + e^-g) */
+} fqt_act;
+
+/*
+ * Both projections of a gated feed-forward block, its activation and its product, for
+ * A (M x K, the tokens), Bg and Bu (N x K, the gate's and the up projection's weights):
+ *   g = A Bg^T, u = A Bu^T  (summed as fqt_fp8_matmul's, in fp32),  a_mn = act(g_mn) u_mn
+ * out (M x N, fp32 or bf16): a, rounded once.  q: a, gate: g, up: u as 8-bit matrices
+ * with blocks of 128 entries of a row, each rounded once from fp32; q is the next
+ * layer's operand, gate and up are what fqt_fp8_gated_backward reads.  Each output may
+ * be NULL, not all; the caller sets the pointers and the pitch of the 8-bit ones, the
+ * call their sizes.  Entries of an 8-bit output that are not finite record
+ * FQT_ENONFINITE, take the NaN code and count for no scale.  K = 0: zeros.
+ * `dtype` is out's, and with it (or where out is NULL, as for bf16) the number of
+ * terms to an accumulator.  Workspace: fqt_fp8_gated_matmul_workspace_size bytes.
+ */
+FQT_API size_t fqt_fp8_gated_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
+FQT_API fqt_status fqt_fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fqt_fp8 *Bu,
+                                        fqt_act act, fqt_dtype dtype, void *out, int64_t ldo,
+                                        fqt_fp8 *q, fqt_fp8 *gate, fqt_fp8 *up, void *workspace,
+                                        size_t ws_bytes, void *stream);
+
+/*
+ * The backward pass of the activation and the product, from dA (rows x cols, fp32 or
+ * bf16) and the 8-bit g and u (rows x cols) that the forward left:
+ *   dg = dA u act'(g),  du = dA act(g),  a = act(g) u
+ * in fp32.  dgate, dup: dg and du in dA's type.  qgate, qup: dg and du as 8-bit
+ * matrices (for the input's gradient); qgate_t, qup_t: their transposes (cols x rows,
+ * for the two weights' gradients); product_t: a's transpose (for the gradient of the
+ * next layer's weight).  Blocks of 128 entries of a row, entries that are not finite as
+ * in fqt_fp8_gated_matmul.  Each output may be NULL, not all.  act'(0) of FQT_RELU is 0.
+ * Workspace: fqt_fp8_gated_backward_workspace_size bytes.
+ */
+FQT_API size_t fqt_fp8_gated_backward_workspace_size(int64_t rows, int64_t cols);
+FQT_API fqt_status fqt_fp8_gated_backward(const void *dA, int64_t ldda, fqt_dtype dtype,
+                                          const fqt_fp8 *gate, const fqt_fp8 *up, fqt_act act,
+                                          void *dgate, int64_t lddg, void *dup, int64_t lddu,
+                                          fqt_fp8 *qgate, fqt_fp8 *qup, fqt_fp8 *qgate_t,
+                                          fqt_fp8 *qup_t, fqt_fp8 *product_t, void *workspace,
+                                          size_t ws_bytes, void *stream);
+
 /* A dense tensor: `count` entries (fp32 or bf16) at `data`, in one run. */
 typedef struct fqt_tensor {
   void *data;

@@ -1,0 +1,401 @@
+// fqt_gated.cuh -- the activations of a gated feed-forward block, and what its product
+// kernel does with the sums of both projections.
+#pragma once
+
+#include <type_traits>
+
+#include "fqt_fp8_core.cuh"
+
+namespace fqt {
+
+// ---------------------------------------------------------------------------
+// Activations
+// ---------------------------------------------------------------------------
+// sigma(z) = 1 / (1 + e^-z).  e^-z by the hardware's base-2 exponential (its argument is
+// rounded: relative error |z| 2^-24) and its reciprocal: about 3e-7 of the result for the
+// |z| < 4 that matter, where tanh.approx would leave 5e-4.
+__device__ __forceinline__ float sigmoid_of(float z) {
+  return __fdividef(1.0f, 1.0f + __expf(-z));
+}
+
+// gelu's tanh form is g sigma(z(g)), z = 2 sqrt(2 / pi) (g + 0.044715 g^3).  Past |g| = 64
+// sigma is 0 or 1, and g^2 times a slope of 0 would be no number.
+constexpr float kTanhScale = 1.5957691216057308f, kTanhCube = 0.044715f;
+__device__ __forceinline__ float tanh_arg(float g) { return fminf(fmaxf(g, -64.0f), 64.0f); }
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float g) {
+  if constexpr (ACT == FQT_SILU) {
+    return g * sigmoid_of(g);
+  } else if constexpr (ACT == FQT_GELU) {
+    return g * normcdff(g);
+  } else if constexpr (ACT == FQT_GELU_TANH) {
+    const float c = tanh_arg(g);
+    const float s = sigmoid_of(kTanhScale * (c + kTanhCube * c * c * c));
+    return g * s;
+  } else if constexpr (ACT == FQT_RELU) {
+    return g <= 0.0f ? 0.0f : g;  // NaN stays
+  } else {
+    return sigmoid_of(g);
+  }
+}
+
+// act(g) and act'(g).  sigma and 1 - sigma both come from e^-|z|, so neither loses digits
+// where it is small.
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
+  if constexpr (ACT == FQT_RELU) {
+    a = act_of<ACT>(g);
+    d = g > 0.0f ? 1.0f : 0.0f;
+  } else if constexpr (ACT == FQT_GELU) {
+    const float cdf = normcdff(g);
+    a = g * cdf;
+    d = fmaf(g, 0.3989422804014327f * __expf(-0.5f * g * g), cdf);
+  } else {
+    float z = g, c = g;
+    if constexpr (ACT == FQT_GELU_TANH) {
+      c = tanh_arg(g);
+      z = kTanhScale * (c + kTanhCube * c * c * c);
+    }
+    const float t = __expf(-fabsf(z)), p = __fdividef(1.0f, 1.0f + t), q = t * p;
+    const float s = z >= 0.0f ? p : q, r = z >= 0.0f ? q : p;  // r = 1 - s
+    if constexpr (ACT == FQT_SIGMOID) {
+      a = g != g ? g : s;
+      d = g != g ? g : s * r;
+    } else if constexpr (ACT == FQT_SILU) {
+      a = g * s;
+      d = fmaf(g * r, s, s);
+    } else {
+      a = g * s;
+      d = fmaf(c * r * s, kTanhScale * fmaf(3.0f * kTanhCube * c, c, 1.0f), s);
+      if (g != g) d = g;  // the clamp takes NaN away
+    }
+  }
+}
+
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  switch (act) {
+    case FQT_SILU: f(std::integral_constant<int, FQT_SILU>()); break;
+    case FQT_GELU: f(std::integral_constant<int, FQT_GELU>()); break;
+    case FQT_GELU_TANH: f(std::integral_constant<int, FQT_GELU_TANH>()); break;
+    case FQT_RELU: f(std::integral_constant<int, FQT_RELU>()); break;
+    default: f(std::integral_constant<int, FQT_SIGMOID>());
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The product kernel's operands
+// ---------------------------------------------------------------------------
+// The right operand of a tile are 128 rows of the gate's weights and the same 128 of the up
+// projection's (of a pair's CTAs, each loads one).  With few tokens the left operand are
+// g.part rows of each, and what is left of its 128 rows is not used.
+template <int NT, bool PAIR>
+__device__ __forceinline__ void f8_load_gated(const F8Of<F8_GATED>::Maps &maps,
+                                              const F8GatedArgs &g, uint8_t *stage,
+                                              const F8Item &t, int kb, int rank, uint64_t *full) {
+  const int32_t k = kb * kF8Block, m = (int32_t)t.m0, n = (int32_t)(t.n0 / 2);
+  if constexpr (NT <= 64) {
+    const uint32_t half = (uint32_t)g.part * kF8Block;
+    mbar_expect_tx(full, 2 * half + NT * kF8Block);
+    tma_load_2d(stage, &maps.a, k, m, full);
+    tma_load_2d(stage + half, &maps.b2, k, m, full);
+    tma_load_2d(stage + kTileBytes, &maps.b, k, 0, full);
+  } else if constexpr (PAIR) {  // the leader's barrier counts both CTAs' bytes
+    if (rank == 0) mbar_expect_tx(full, (uint32_t)(4 * kTileBytes));
+    const uint32_t bar = leader_addr(full);
+    tma_load_2d_pair(stage, &maps.a, k, m, bar);
+    tma_load_2d_pair(stage + kTileBytes, rank ? &maps.b2 : &maps.b, k, n, bar);
+  } else {
+    mbar_expect_tx(full, (uint32_t)(3 * kTileBytes));
+    tma_load_2d(stage, &maps.a, k, m, full);
+    tma_load_2d(stage + kTileBytes, &maps.b, k, n, full);
+    tma_load_2d(stage + 2 * kTileBytes, &maps.b2, k, n, full);
+  }
+}
+
+// The scales of four K blocks for row 32 i + lane of the left operand (i < 4) or row
+// 32 (i - 4) + lane of the right one; 1 past the ends, where the codes are zeros, so that
+// such rows' sums are zeros too.
+template <int NT>
+__device__ __forceinline__ uint32_t f8_gated_scales(const F8GatedArgs &g, const F8Item &t,
+                                                    int64_t group, int i, int lane) {
+  const uint32_t *from;
+  int64_t r, rows, pitch;
+  if constexpr (NT <= 64) {
+    const int at = 32 * i;
+    if (i >= 4) {
+      from = g.sb, pitch = g.spb, rows = g.N, r = at - BM + lane;
+    } else {
+      from = at < g.part ? g.sa : g.s2, pitch = g.spa;
+      rows = at < 2 * g.part ? g.M : 0, r = t.m0 + at % g.part + lane;
+    }
+  } else if (i < 4) {
+    from = g.sa, pitch = g.spa, rows = g.M, r = t.m0 + 32 * i + lane;
+  } else {
+    from = i < 8 ? g.sb : g.s2, pitch = g.spb, rows = g.N, r = t.n0 / 2 + 32 * (i & 3) + lane;
+  }
+  return r < rows ? __ldg(from + group * pitch + r) : 0x7F7F7F7Fu;
+}
+
+// ---------------------------------------------------------------------------
+// The product kernel's epilogue
+// ---------------------------------------------------------------------------
+// The largest finite magnitude of n values (fp32 bits); odd: some are not finite.
+template <int N>
+__device__ __forceinline__ uint32_t f8_top(const uint32_t *v, bool &odd) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = max(m, v[i] & 0x7FFFFFFFu);
+  odd = m >= 0x7F800000u;
+  if (odd) {
+    m = 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t x = v[i] & 0x7FFFFFFFu;
+      m = max(m, x < 0x7F800000u ? x : 0u);
+    }
+  }
+  return m;
+}
+
+// Four codes of fp32 values (bits) times inv; ODD: infinities take the NaN code (y + 0 y).
+template <bool ODD>
+__device__ __forceinline__ uint32_t f8_codes4(const uint32_t *v, float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = __uint_as_float(v[i]) * inv;
+    if constexpr (ODD) y[i] = fmaf(y[i], 0.0f, y[i]);
+  }
+  return f8_pair(y[0], y[1]) | f8_pair(y[2], y[3]) << 16;
+}
+
+// 64 columns of a warp's 32 rows as codes, by way of its box and TMA.
+template <bool ODD>
+__device__ __forceinline__ void f8_box_codes(float *box, int lane, const uint32_t *v, float inv) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    *reinterpret_cast<uint4 *>(box + box_off(lane, k) / 4) =
+        make_uint4(f8_codes4<ODD>(v + 16 * k, inv), f8_codes4<ODD>(v + 16 * k + 4, inv),
+                   f8_codes4<ODD>(v + 16 * k + 8, inv), f8_codes4<ODD>(v + 16 * k + 12, inv));
+}
+
+__device__ __forceinline__ void f8_store_codes(const CUtensorMap *map, float *box, int lane,
+                                               int64_t m0, int64_t n, const uint32_t *v, float inv,
+                                               bool odd) {
+  if (lane == 0) bulk_wait_read(0);
+  __syncwarp();
+  if (__any_sync(0xffffffffu, odd)) f8_box_codes<true>(box, lane, v, inv);
+  else f8_box_codes<false>(box, lane, v, inv);
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_2d(map, (int32_t)n, (int32_t)m0, box);
+    bulk_commit();
+  }
+}
+
+// A barrier of the two warps that hold a quadrant's rows; true if either says so.
+__device__ __forceinline__ bool f8_either(int quadrant, bool mine) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %2, 0;\n\t"
+      "barrier.cta.red.or.pred q, %1, 64, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(quadrant + 1), "r"((uint32_t)mine)
+      : "memory");
+  return r != 0;
+}
+
+// One super tile's (or tile's) accumulator holds g in its first 128 columns and u in the
+// others, for the same 128 hidden columns.  A warp takes 64 columns of both for its 32 rows
+// (a lane a row), so a is formed in registers, and a row's block of 128 is two lanes' 64,
+// which exchange their maxima through shared memory.  g and u leave first, then a takes g's
+// registers.  Both warps of a quadrant leave the loop together, whatever made one of them
+// stop: they meet at named barriers.
+template <int ACCS, bool PAIR, bool FOLD>
+__device__ __forceinline__ void f8_gated_epilogue(const F8Of<F8_GATED>::Maps &maps,
+                                                  const F8GatedArgs &g, uint32_t tmem,
+                                                  uint64_t *accf, uint64_t *acce,
+                                                  volatile int *abort_flag, float *box,
+                                                  uint32_t *tops, int q, int h, int lane,
+                                                  int64_t first, int64_t step) {
+  constexpr int NT = 256;
+  const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 64);
+  const bool keeps = g.gate.codes || g.up.codes, codes = keeps || g.q.codes;
+  // of a row's halves: tops[(tensor * 2 + half) * 128 + row]
+  uint32_t *mine = tops + h * 128 + q * 32 + lane, *other = tops + (1 - h) * 128 + q * 32 + lane;
+  uint32_t c = 0;
+  for (int64_t it = first; it < g.items; it += step) {
+    if (codes ? f8_either(q, *abort_flag) : *abort_flag) break;
+    const F8Item t = f8_item<NT, PAIR>(g, it);
+    uint32_t v[4][32];  // 64 columns of g, 64 of u
+    bool ok = true;
+    if constexpr (FOLD)
+#pragma unroll
+      for (int i = 0; i < 128; ++i) v[i / 32][i % 32] = 0u;
+    for (int kb = t.kb0; kb < t.kb1; kb = FOLD ? kb + g.chunk : t.kb1, ++c) {
+      const int buf = c % ACCS;
+      if (!f8_wait(&accf[buf], (c / ACCS) & 1u, g.status)) {
+        *abort_flag = 1;
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const uint32_t from = lane_base + (uint32_t)(buf * NT);
+      if constexpr (!FOLD) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) tmem_ld32_nw(from + (p >> 1) * 128 + (p & 1) * 32, v[p]);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) tmem_wait_ld(v[p]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 128; j += 16) {  // 16 columns at a time: registers
+          uint32_t r[16];
+          tmem_ld16_nw(from + (j >> 6) * 128 + (j & 63), r);
+          tmem_wait_ld(r);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            uint32_t &x = v[j / 32][j % 32 + i];
+            x = __float_as_uint(__uint_as_float(x) + __uint_as_float(r[i]));
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) f8_release<PAIR>(&acce[buf]);
+    }
+    const int64_t m0 = t.m0 + q * 32, n0 = t.n0 / 2, n = n0 + h * 64;
+    const bool row = m0 + lane < g.M;
+    bool odd_g = false, odd_u = false, odd_a = false;
+    if (keeps) {
+      const uint32_t mg = f8_top<64>(v[0], odd_g), mu = f8_top<64>(v[2], odd_u);
+      if ((odd_g && g.gate.codes) || (odd_u && g.up.codes)) record_status(g.status, FQT_ENONFINITE);
+      mine[0] = mg;
+      mine[256] = mu;
+      if (f8_either(q, !ok)) break;
+      const int eg = f8_exponent(max(mg, other[0])), eu = f8_exponent(max(mu, other[256]));
+      if (g.gate.codes) {
+        if (m0 < g.M && n < g.N)
+          f8_store_codes(&maps.gate, box, lane, m0, n, v[0], pow2(-eg), odd_g);
+        if (row && h == 0) g.gate.scales[scale_at(n0 / kF8Block, g.sp, m0 + lane)] = eg + 127;
+      }
+      if (g.up.codes) {
+        if (m0 < g.M && n < g.N)
+          f8_store_codes(&maps.up, box, lane, m0, n, v[2], pow2(-eu), odd_u);
+        if (row && h == 0) g.up.scales[scale_at(n0 / kF8Block, g.sp, m0 + lane)] = eu + 127;
+      }
+    }
+    if (!codes && !ok) break;
+    with_act(g.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) {
+        uint32_t &x = v[i / 32][i % 32];
+        x = __float_as_uint(act_of<act.value>(__uint_as_float(x)) *
+                            __uint_as_float(v[2 + i / 32][i % 32]));
+      }
+    });
+    if (g.out && ok) {
+      float *fp32 = static_cast<float *>(g.out);
+      __nv_bfloat16 *bf16 = static_cast<__nv_bfloat16 *>(g.out);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int64_t np = n + 32 * p;
+        if (g.boxes && g.bf16)
+          f8_store_box<__nv_bfloat16>(g, &maps.out, box, lane, m0, np, v[p]);
+        else if (g.boxes)
+          f8_store_box<float>(g, &maps.out, box, lane, m0, np, v[p]);
+        else if (g.bf16)
+          f8_store_rows<__nv_bfloat16>(g, bf16, g.ldo, box, lane, m0, np, v[p]);
+        else
+          f8_store_rows<float>(g, fp32, g.ldo, box, lane, m0, np, v[p]);
+      }
+    }
+    if (g.q.codes) {
+      const uint32_t ma = f8_top<64>(v[0], odd_a);
+      if (odd_a) record_status(g.status, FQT_ENONFINITE);
+      mine[512] = ma;
+      if (f8_either(q, !ok)) break;
+      const int ea = f8_exponent(max(ma, other[512]));
+      if (m0 < g.M && n < g.N)
+        f8_store_codes(&maps.q, box, lane, m0, n, v[0], pow2(-ea), odd_a);
+      if (row && h == 0) g.q.scales[scale_at(n0 / kF8Block, g.sp, m0 + lane)] = ea + 127;
+    }
+  }
+  if (lane == 0) bulk_wait_all();
+}
+
+// W consecutive entries of the shared memory of a cluster's CTA.
+template <int W>
+__device__ __forceinline__ void f8_remote(const float *p, int cta, uint32_t (&v)[W]) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(cta));
+  if constexpr (W == 4)
+    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                 : "r"(a)
+                 : "memory");
+  else if constexpr (W == 2)
+    asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(a)
+                 : "memory");
+  else
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v[0]) : "r"(a) : "memory");
+}
+
+// W consecutive codes of lane's values, whose block (the warp's) has the maximum m.
+template <int W>
+__device__ __forceinline__ void f8_put_codes(const F8Codes &o, const F8GatedArgs &g, int64_t token,
+                                             int64_t j, const uint32_t (&v)[W], int lane) {
+  static_assert(W == 4, "a block of 128 entries is a warp's");
+  if (!o.codes) return;
+  bool odd;
+  const uint32_t m = __reduce_max_sync(0xffffffffu, f8_top<W>(v, odd));
+  if (odd) record_status(g.status, FQT_ENONFINITE);
+  const int e = f8_exponent(m);
+  // (rows of codes are whole 16 bytes)
+  if (j < g.M)
+    *reinterpret_cast<uint32_t *>(o.codes + token * o.pitch + j) = f8_codes4<true>(v, pow2(-e));
+  if (lane == 0) o.scales[scale_at(j / kF8Block, g.sp, token)] = e + 127;
+}
+
+// Few tokens: g and u of this CTA's hidden columns (g.part each) lie in its shared memory,
+// a token's 128 sums in a row (g, then u).  The CTAs of a cluster hold the 32 W columns of
+// whole blocks; a warp takes a token, a lane W columns.
+template <int W>
+__device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float *part) {
+  const int parts = 32 * W / g.part, self = (int)(blockIdx.x % parts);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t j = (int64_t)(blockIdx.x / parts) * 32 * W + lane * W;
+  const int cta = lane * W / g.part, at = lane * W % g.part;
+  for (int64_t token = self + parts * warp; token < g.N; token += parts * (kF8Threads / 32)) {
+    uint32_t a[W], u[W];
+    f8_remote<W>(part + token * BM + at, cta, a);
+    f8_remote<W>(part + token * BM + g.part + at, cta, u);
+    if constexpr (W == 4) {
+      f8_put_codes<W>(g.gate, g, token, j, a, lane);
+      f8_put_codes<W>(g.up, g, token, j, u, lane);
+    }
+    with_act(g.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < W; ++i)
+        a[i] = __float_as_uint(act_of<act.value>(__uint_as_float(a[i])) * __uint_as_float(u[i]));
+    });
+    if (g.out) {
+      const int64_t o = token * g.ldo + j;
+#pragma unroll
+      for (int i = 0; i < W; ++i)
+        if (j + i < g.M) {
+          if (g.bf16)
+            static_cast<__nv_bfloat16 *>(g.out)[o + i] = __float2bfloat16_rn(__uint_as_float(a[i]));
+          else
+            static_cast<float *>(g.out)[o + i] = __uint_as_float(a[i]);
+        }
+    }
+    if constexpr (W == 4) f8_put_codes<W>(g.q, g, token, j, a, lane);
+  }
+}
+
+}  // namespace fqt

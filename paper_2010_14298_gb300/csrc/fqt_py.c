@@ -378,6 +378,60 @@ static PyObject *py_fp8_matmul(PyObject *self, PyObject *const *a, Py_ssize_t n)
   CALL(fqt_fp8_matmul(A, B, dt, out, ldo, t.ws, t.bytes, t.stream))
 }
 
+/* fp8_matmul_sum(A1, B1, A2, B2, dtype, out, ldo, ws, bytes, stream) */
+static PyObject *py_fp8_matmul_sum(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(10)
+  void *out;
+  fqt_fp8 s[4], *q[4];
+  Tail t;
+  const fqt_dtype dt = (fqt_dtype)INT(4);
+  const int64_t ldo = I64(6);
+  if (PyErr_Occurred()) return NULL;
+  for (int i = 0; i < 4; ++i)
+    if (fill_fp8(a[i], &s[i], &q[i])) return NULL;
+  if (tensor_ptr(a[5], &out) || tail(a + 7, &t)) return NULL;
+  CALL(fqt_fp8_matmul_sum(q[0], q[1], q[2], q[3], dt, out, ldo, t.ws, t.bytes, t.stream))
+}
+
+/* fp8_gated_matmul(A, Bg, Bu, act, dtype, out, ldo, q, gate, up, ws, bytes, stream) */
+static PyObject *py_fp8_gated_matmul(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(13)
+  void *out;
+  fqt_fp8 s[6], *q[6];
+  Tail t;
+  const fqt_act act = (fqt_act)INT(3);
+  const fqt_dtype dt = (fqt_dtype)INT(4);
+  const int64_t ldo = I64(6);
+  if (PyErr_Occurred()) return NULL;
+  for (int i = 0; i < 6; ++i)
+    if (fill_fp8(a[i < 3 ? i : i + 4], &s[i], &q[i])) return NULL;
+  if (tensor_ptr(a[5], &out) || tail(a + 10, &t)) return NULL;
+  CALL(fqt_fp8_gated_matmul(q[0], q[1], q[2], act, dt, out, ldo, q[3], q[4], q[5], t.ws, t.bytes,
+                            t.stream))
+}
+
+/* fp8_gated_backward(dA, ldda, dtype, gate, up, act, dgate, lddg, dup, lddu, qgate, qup,
+ * qgate_t, qup_t, product_t, ws, bytes, stream) */
+static PyObject *py_fp8_gated_backward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  NARGS(18)
+  void *da, *dg, *du;
+  fqt_fp8 s[7], *q[7];
+  Tail t;
+  const int64_t ldda = I64(1), lddg = I64(7), lddu = I64(9);
+  const fqt_dtype dt = (fqt_dtype)INT(2);
+  const fqt_act act = (fqt_act)INT(5);
+  if (PyErr_Occurred()) return NULL;
+  for (int i = 0; i < 7; ++i)
+    if (fill_fp8(a[i < 2 ? i + 3 : i + 8], &s[i], &q[i])) return NULL;
+  if (tensor_ptr(a[0], &da) || tensor_ptr(a[6], &dg) || tensor_ptr(a[8], &du) || tail(a + 15, &t))
+    return NULL;
+  CALL(fqt_fp8_gated_backward(da, ldda, dt, q[0], q[1], act, dg, lddg, du, lddu, q[2], q[3], q[4],
+                              q[5], q[6], t.ws, t.bytes, t.stream))
+}
+
 /* clip_grad_norm(grads, out, n, max_norm, norm, ws, bytes, stream), the lists by address */
 static PyObject *py_clip_grad_norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
@@ -416,6 +470,10 @@ static PyMethodDef kMethods[] = {
      NULL},
     {"quantize_fp8", (PyCFunction)(void (*)(void))py_quantize_fp8, METH_FASTCALL, NULL},
     {"fp8_matmul", (PyCFunction)(void (*)(void))py_fp8_matmul, METH_FASTCALL, NULL},
+    {"fp8_matmul_sum", (PyCFunction)(void (*)(void))py_fp8_matmul_sum, METH_FASTCALL, NULL},
+    {"fp8_gated_matmul", (PyCFunction)(void (*)(void))py_fp8_gated_matmul, METH_FASTCALL, NULL},
+    {"fp8_gated_backward", (PyCFunction)(void (*)(void))py_fp8_gated_backward, METH_FASTCALL,
+     NULL},
     {"clip_grad_norm", (PyCFunction)(void (*)(void))py_clip_grad_norm, METH_FASTCALL, NULL},
     {"workspace_size", (PyCFunction)(void (*)(void))py_workspace_size, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};

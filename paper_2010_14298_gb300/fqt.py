@@ -127,6 +127,19 @@ def load(build_if_missing: bool = True):
         lib.fqt_fp8_matmul_workspace_size.restype = sz
         lib.fqt_fp8_matmul.argtypes = [FP, FP, i32, P, i64, P, sz, P]
         lib.fqt_fp8_matmul.restype = i32
+        lib.fqt_fp8_matmul_sum_workspace_size.argtypes = [i64, i64, i64, i64]
+        lib.fqt_fp8_matmul_sum_workspace_size.restype = sz
+        lib.fqt_fp8_matmul_sum.argtypes = [FP, FP, FP, FP, i32, P, i64, P, sz, P]
+        lib.fqt_fp8_matmul_sum.restype = i32
+        lib.fqt_fp8_gated_matmul_workspace_size.argtypes = [i64, i64, i64]
+        lib.fqt_fp8_gated_matmul_workspace_size.restype = sz
+        lib.fqt_fp8_gated_matmul.argtypes = [FP, FP, FP, i32, i32, P, i64, FP, FP, FP, P, sz, P]
+        lib.fqt_fp8_gated_matmul.restype = i32
+        lib.fqt_fp8_gated_backward_workspace_size.argtypes = [i64, i64]
+        lib.fqt_fp8_gated_backward_workspace_size.restype = sz
+        lib.fqt_fp8_gated_backward.argtypes = [P, i64, i32, FP, FP, i32, P, i64, P, i64, FP, FP,
+                                               FP, FP, FP, P, sz, P]
+        lib.fqt_fp8_gated_backward.restype = i32
         lib.fqt_clip_grad_norm_workspace_size.argtypes = [i64]
         lib.fqt_clip_grad_norm_workspace_size.restype = sz
         lib.fqt_clip_grad_norm.argtypes = [P, P, i64, f32, P, P, sz, P]
@@ -850,6 +863,171 @@ def fp8_matmul(A: Fp8Tensor, B: Fp8Tensor, out: torch.Tensor = None, dtype=torch
     st = native().fp8_matmul(A, B, _dtype_code(out), out, ldo, buf, nbytes, _raw_stream(stream))
     if st:
         _check(st, "fqt_fp8_matmul")
+    return out
+
+
+def fp8_matmul_sum_workspace_size(M: int, N: int, K1: int, K2: int) -> int:
+    return int(load().fqt_fp8_matmul_sum_workspace_size(M, N, K1, K2))
+
+
+def _fp8_in(t, name, dev):
+    """An 8-bit matrix to read, on that GPU (None: on any)."""
+    there = t.codes.get_device()
+    if there < 0 or (dev is not None and there != dev):
+        raise _elsewhere(t.codes, name, -1 if there < 0 else dev)
+    return there
+
+
+def fp8_matmul_sum(A1: Fp8Tensor, B1: Fp8Tensor, A2: Fp8Tensor, B2: Fp8Tensor,
+                   out: torch.Tensor = None, dtype=torch.float32, ws: Workspace = None,
+                   stream=None) -> torch.Tensor:
+    """A1 B1^T + A2 B2^T (fqt_fp8_matmul_sum) in out's type, or a new tensor of `dtype`:
+    the gradient of an input that two layers share."""
+    if A1.cols != B1.cols or A2.cols != B2.cols:
+        raise ValueError(f"the pairs have {A1.cols} and {B1.cols}, {A2.cols} and {B2.cols} columns")
+    if A1.rows != A2.rows or B1.rows != B2.rows:
+        raise ValueError(f"the products are {A1.rows} x {B1.rows} and {A2.rows} x {B2.rows}")
+    dev = _fp8_in(A1, "A1", None)
+    for t, name in ((B1, "B1"), (A2, "A2"), (B2, "B2")):
+        _fp8_in(t, name, dev)
+    if out is not None:
+        dtype = out.dtype
+    out, ldo = _rows_out(out, "out", A1.rows, B1.rows, dtype, dev, A1.codes, stream)
+    if ws is None:
+        with _on(stream):
+            ws = Workspace.of_size(
+                fp8_matmul_sum_workspace_size(A1.rows, B1.rows, A1.cols, A2.cols), A1.codes.device)
+    buf, nbytes = _scratch(ws, dev)
+    st = native().fp8_matmul_sum(A1, B1, A2, B2, _dtype_code(out), out, ldo, buf, nbytes,
+                                 _raw_stream(stream))
+    if st:
+        _check(st, "fqt_fp8_matmul_sum")
+    return out
+
+
+# --- a gated feed-forward block --------------------------------------------
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
+
+
+def _act(name):
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"the activation is one of {tuple(ACTIVATIONS)}, not {name!r}")
+    return code
+
+
+def fp8_gated_matmul_workspace_size(M: int, N: int, K: int) -> int:
+    return int(load().fqt_fp8_gated_matmul_workspace_size(M, N, K))
+
+
+def fp8_gated_matmul(A: Fp8Tensor, Bg: Fp8Tensor, Bu: Fp8Tensor, act: str = "silu",
+                     out: torch.Tensor = None, q: Fp8Tensor = None, gate: Fp8Tensor = None,
+                     up: Fp8Tensor = None, dense: bool = True, codes: bool = False,
+                     keep: bool = False, dtype=torch.float32, ws: Workspace = None, stream=None):
+    """(a, its codes, g's, u's): both projections of a gated feed-forward block, g = A Bg^T
+    and u = A Bu^T, and a = act(g) u (fqt_fp8_gated_matmul).  `dense`, `codes` and `keep`
+    ask for a (in out's type, or `dtype`), its codes, and the codes of g and u that
+    fp8_gated_backward reads (a tensor given for one does too); None stands for one that
+    was not asked for."""
+    act = _act(act)
+    if A.cols != Bg.cols or A.cols != Bu.cols:
+        raise ValueError(f"A has {A.cols} columns, the weights {Bg.cols} and {Bu.cols}")
+    if Bg.rows != Bu.rows:
+        raise ValueError(f"the weights have {Bg.rows} and {Bu.rows} rows")
+    M, N = A.rows, Bg.rows
+    dev = _fp8_in(A, "A", None)
+    _fp8_in(Bg, "Bg", dev)
+    _fp8_in(Bu, "Bu", dev)
+    ldo, like = N, A.codes
+    if out is not None:
+        dtype = out.dtype
+    if dense or out is not None:
+        out, ldo = _rows_out(out, "out", M, N, dtype, dev, like, stream)
+        kind = _dtype_code(out)
+    else:
+        kind = BF16
+    if codes or q is not None:
+        q = _fp8_out(q, "q", M, N, 1, dev, like, stream)
+    if keep or gate is not None:
+        gate = _fp8_out(gate, "gate", M, N, 1, dev, like, stream)
+    if keep or up is not None:
+        up = _fp8_out(up, "up", M, N, 1, dev, like, stream)
+    if ws is None:
+        with _on(stream):
+            ws = Workspace.of_size(fp8_gated_matmul_workspace_size(M, N, A.cols), like.device)
+    buf, nbytes = _scratch(ws, dev)
+    st = native().fp8_gated_matmul(A, Bg, Bu, act, kind, out, ldo, q, gate, up, buf, nbytes,
+                                   _raw_stream(stream))
+    if st:
+        _check(st, "fqt_fp8_gated_matmul")
+    for t in (q, gate, up):
+        if t is not None:
+            t.block_rows = 1
+    return out, q, gate, up
+
+
+@dataclass
+class GatedGrads:
+    """What fp8_gated_backward makes, None for what was not asked for: dg and du (dense),
+    their codes by rows (``qgate``, ``qup``: tokens x hidden) and by columns (``qgate_t``,
+    ``qup_t``: hidden x tokens), and the codes of a by columns (``product_t``)."""
+    dgate: Optional[torch.Tensor] = None
+    dup: Optional[torch.Tensor] = None
+    qgate: Optional[Fp8Tensor] = None
+    qup: Optional[Fp8Tensor] = None
+    qgate_t: Optional[Fp8Tensor] = None
+    qup_t: Optional[Fp8Tensor] = None
+    product_t: Optional[Fp8Tensor] = None
+
+    @staticmethod
+    def empty(rows: int, cols: int, device="cuda"):
+        """All of the codes: what a training step's three products read."""
+        Q = lambda r, c: Fp8Tensor.empty(r, c, 1, device)  # noqa: E731
+        return GatedGrads(qgate=Q(rows, cols), qup=Q(rows, cols), qgate_t=Q(cols, rows),
+                          qup_t=Q(cols, rows), product_t=Q(cols, rows))
+
+
+def fp8_gated_backward_workspace_size(rows: int, cols: int) -> int:
+    return int(load().fqt_fp8_gated_backward_workspace_size(rows, cols))
+
+
+def fp8_gated_backward(dA: torch.Tensor, gate: Fp8Tensor, up: Fp8Tensor, act: str = "silu",
+                       out: GatedGrads = None, ws: Workspace = None, stream=None) -> GatedGrads:
+    """The backward pass of a = act(g) u from a's gradient and the 8-bit g and u that
+    fp8_gated_matmul kept (fqt_fp8_gated_backward): fills what `out` holds, or all of
+    GatedGrads.empty."""
+    act = _act(act)
+    dA, rows, cols, ldda, dev = _rows_in(dA, "dA", stream)
+    for t, name in ((gate, "gate"), (up, "up")):
+        _fp8_in(t, name, dev)
+        if t.rows != rows or t.cols != cols:
+            raise ValueError(f"{name} is {t.rows} x {t.cols}, dA {rows} x {cols}")
+    if out is None:
+        with _on(stream):
+            out = GatedGrads.empty(rows, cols, dA.device)
+    lddg = lddu = cols
+    if out.dgate is not None:
+        _, lddg = _rows_out(out.dgate, "dgate", rows, cols, dA.dtype, dev, dA, stream)
+    if out.dup is not None:
+        _, lddu = _rows_out(out.dup, "dup", rows, cols, dA.dtype, dev, dA, stream)
+    codes = ((out.qgate, "qgate", rows, cols), (out.qup, "qup", rows, cols),
+             (out.qgate_t, "qgate_t", cols, rows), (out.qup_t, "qup_t", cols, rows),
+             (out.product_t, "product_t", cols, rows))
+    for t, name, r, c in codes:
+        if t is not None:
+            _fp8_out(t, name, r, c, 1, dev, dA, stream)
+    if ws is None:
+        with _on(stream):
+            ws = Workspace.of_size(fp8_gated_backward_workspace_size(rows, cols), dA.device)
+    buf, nbytes = _scratch(ws, dev)
+    st = native().fp8_gated_backward(dA, ldda, _dtype_code(dA), gate, up, act, out.dgate, lddg,
+                                     out.dup, lddu, out.qgate, out.qup, out.qgate_t, out.qup_t,
+                                     out.product_t, buf, nbytes, _raw_stream(stream))
+    if st:
+        _check(st, "fqt_fp8_gated_backward")
+    for t, _, _, _ in codes:
+        if t is not None:
+            t.block_rows = 1
     return out
 
 

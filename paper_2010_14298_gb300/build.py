@@ -26,7 +26,8 @@ LIB = os.path.join(LIBDIR, "libfqt.so")
 # another interpreter finds no extension module under its own name
 PYEXT = os.path.join(LIBDIR, "_fqt_py" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["fqt_quant.cu", "fqt_codes.cu", "fqt_group.cu", "fqt_gemm.cu", "fqt_gemm_pair.cu", "fqt_conv.cu",
-           "fqt_norm.cu", "fqt_fp8.cu", "fqt_gated.cu", "fqt_clip.cu", "fqt_api.cu"]
+           "fqt_norm.cu", "fqt_fp8.cu", "fqt_gated.cu",
+           "fqt_gated_back.cu", "fqt_clip.cu", "fqt_api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
          "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]

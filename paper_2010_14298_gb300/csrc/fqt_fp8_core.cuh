@@ -945,7 +945,8 @@ __global__ void __launch_bounds__(kF8Threads, 1)
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-static bool make_map_codes(CUtensorMap *m, const fqt_fp8 *q, uint32_t box_rows) {
+static bool make_map_codes(CUtensorMap *m, const fqt_fp8 *q, uint32_t box_rows,
+                           bool swizzled = true) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[2] = {(cuuint64_t)q->cols, (cuuint64_t)q->rows};
@@ -953,7 +954,8 @@ static bool make_map_codes(CUtensorMap *m, const fqt_fp8 *q, uint32_t box_rows) 
   cuuint32_t box[2] = {kF8Block, box_rows};
   cuuint32_t es[2] = {1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, q->codes, dims, strides, box, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

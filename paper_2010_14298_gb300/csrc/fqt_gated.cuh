@@ -11,17 +11,31 @@ namespace fqt {
 // ---------------------------------------------------------------------------
 // Activations
 // ---------------------------------------------------------------------------
-// sigma(z) = 1 / (1 + e^-z).  e^-z by the hardware's base-2 exponential (its argument is
-// rounded: relative error |z| 2^-24) and its reciprocal: about 3e-7 of the result for the
-// |z| < 4 that matter, where tanh.approx would leave 5e-4.
+// sigma(z) = 1 / (1 + 2^(-z log2 e)) by the hardware's base-2 exponential and reciprocal:
+// the exponential's argument is rounded (relative error |z| 2^-24 of the result), they
+// themselves are 2 units off; tanh.approx would leave 5e-4.
+constexpr float kLog2E = 1.4426950408889634f;
+__device__ __forceinline__ float exp2_of(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float inverse_of(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ float sigmoid_of(float z) {
-  return __fdividef(1.0f, 1.0f + __expf(-z));
+  return inverse_of(__fadd_rn(1.0f, exp2_of(__fmul_rn(z, -kLog2E))));
 }
 
 // gelu's tanh form is g sigma(z(g)), z = 2 sqrt(2 / pi) (g + 0.044715 g^3).  Past |g| = 64
 // sigma is 0 or 1, and g^2 times a slope of 0 would be no number.
 constexpr float kTanhScale = 1.5957691216057308f, kTanhCube = 0.044715f;
 __device__ __forceinline__ float tanh_arg(float g) { return fminf(fmaxf(g, -64.0f), 64.0f); }
+__device__ __forceinline__ float tanh_z(float c) {
+  return __fmul_rn(kTanhScale, fmaf(__fmul_rn(__fmul_rn(kTanhCube, c), c), c, c));
+}
 
 template <int ACT>
 __device__ __forceinline__ float act_of(float g) {
@@ -30,9 +44,7 @@ __device__ __forceinline__ float act_of(float g) {
   } else if constexpr (ACT == FQT_GELU) {
     return g * normcdff(g);
   } else if constexpr (ACT == FQT_GELU_TANH) {
-    const float c = tanh_arg(g);
-    const float s = sigmoid_of(kTanhScale * (c + kTanhCube * c * c * c));
-    return g * s;
+    return g * sigmoid_of(tanh_z(tanh_arg(g)));
   } else if constexpr (ACT == FQT_RELU) {
     return g <= 0.0f ? 0.0f : g;  // NaN stays
   } else {
@@ -40,8 +52,9 @@ __device__ __forceinline__ float act_of(float g) {
   }
 }
 
-// act(g) and act'(g).  sigma and 1 - sigma both come from e^-|z|, so neither loses digits
-// where it is small.
+// act(g) and act'(g).  1 - sigma is e^-z sigma where it is the slope's factor on its own
+// (e^-z held below 2^126, so that neither loses digits where it is small); silu's slope is
+// s + a (1 - s), which a rounded 1 - s does not harm.
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
   if constexpr (ACT == FQT_RELU) {
@@ -49,27 +62,47 @@ __device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
     d = g > 0.0f ? 1.0f : 0.0f;
   } else if constexpr (ACT == FQT_GELU) {
     const float cdf = normcdff(g);
-    a = g * cdf;
-    d = fmaf(g, 0.3989422804014327f * __expf(-0.5f * g * g), cdf);
+    a = __fmul_rn(g, cdf);
+    const float phi = exp2_of(__fmul_rn(__fmul_rn(g, g), -0.5f * kLog2E));
+    d = fmaf(__fmul_rn(g, 0.3989422804014327f), phi, cdf);
+  } else if constexpr (ACT == FQT_SILU) {
+    const float s = sigmoid_of(g);
+    a = __fmul_rn(g, s);
+    d = fmaf(a, __fsub_rn(1.0f, s), s);
   } else {
-    float z = g, c = g;
-    if constexpr (ACT == FQT_GELU_TANH) {
-      c = tanh_arg(g);
-      z = kTanhScale * (c + kTanhCube * c * c * c);
-    }
-    const float t = __expf(-fabsf(z)), p = __fdividef(1.0f, 1.0f + t), q = t * p;
-    const float s = z >= 0.0f ? p : q, r = z >= 0.0f ? q : p;  // r = 1 - s
+    const float c = ACT == FQT_GELU_TANH ? tanh_arg(g) : g;
+    const float z = ACT == FQT_GELU_TANH ? tanh_z(c) : g;
+    const float t = exp2_of(fminf(__fmul_rn(z, -kLog2E), 126.0f));
+    const float s = inverse_of(__fadd_rn(1.0f, t)), r = __fmul_rn(t, s);  // r = 1 - s
     if constexpr (ACT == FQT_SIGMOID) {
-      a = g != g ? g : s;
-      d = g != g ? g : s * r;
-    } else if constexpr (ACT == FQT_SILU) {
-      a = g * s;
-      d = fmaf(g * r, s, s);
+      a = s;
+      d = __fmul_rn(s, r);
     } else {
-      a = g * s;
-      d = fmaf(c * r * s, kTanhScale * fmaf(3.0f * kTanhCube * c, c, 1.0f), s);
-      if (g != g) d = g;  // the clamp takes NaN away
+      a = __fmul_rn(g, s);
+      const float dz = __fmul_rn(kTanhScale, fmaf(__fmul_rn(3.0f * kTanhCube, c), c, 1.0f));
+      d = fmaf(__fmul_rn(__fmul_rn(c, r), s), dz, s);
     }
+    if (g != g) a = d = g;  // the limits take NaN away
+  }
+}
+
+// Of two values at a time; silu's in packed arithmetic, with the same roundings.
+template <int ACT>
+__device__ __forceinline__ void act_and_slope2(f32x2 g, f32x2 &a, f32x2 &d) {
+  if constexpr (ACT == FQT_SILU) {
+    float x, y;
+    unpack2(mul2(g, pack2(-kLog2E, -kLog2E)), x, y);
+    unpack2(add2(pack2(exp2_of(x), exp2_of(y)), pack2(1.0f, 1.0f)), x, y);
+    const f32x2 s = pack2(inverse_of(x), inverse_of(y));
+    a = mul2(g, s);
+    d = fma2(a, fma2(s, pack2(-1.0f, -1.0f), pack2(1.0f, 1.0f)), s);
+  } else {
+    float g0, g1, a0, a1, d0, d1;
+    unpack2(g, g0, g1);
+    act_and_slope<ACT>(g0, a0, d0);
+    act_and_slope<ACT>(g1, a1, d1);
+    a = pack2(a0, a1);
+    d = pack2(d0, d1);
   }
 }
 
@@ -396,6 +429,39 @@ __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float 
     }
     if constexpr (W == 4) f8_put_codes<W>(g.q, g, token, j, a, lane);
   }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+inline F8Codes codes_of(const fqt_fp8 *q) {
+  return q ? F8Codes{q->codes, q->scales, q->pitch} : F8Codes{nullptr, nullptr, 0};
+}
+
+inline bool act_known(fqt_act act) { return act >= FQT_SILU && act <= FQT_SIGMOID; }
+
+// An output of rows x cols codes: its pointers and its pitch; then its sizes.
+inline bool codes_fit(const fqt_fp8 *q, int64_t rows, int64_t cols) {
+  if (!q) return true;
+  fqt_fp8 v = *q;
+  v.rows = rows;
+  v.cols = cols;
+  return f8_good(&v);
+}
+inline void set_codes(fqt_fp8 *q, int64_t rows, int64_t cols) {
+  if (!q) return;
+  q->rows = rows;
+  q->cols = cols;
+  q->block_rows = 1;
+}
+
+// No two outputs in the same place.
+template <int N>
+inline bool all_apart(const fqt_fp8 *const (&q)[N]) {
+  for (int i = 0; i < N; ++i)
+    for (int j = i + 1; j < N; ++j)
+      if (q[i] && q[j] && (q[i]->codes == q[j]->codes || q[i]->scales == q[j]->scales)) return false;
+  return true;
 }
 
 }  // namespace fqt

@@ -35,10 +35,31 @@ __device__ __forceinline__ float pow2(int e) {
   return __uint_as_float(e > -127 ? (uint32_t)(e + 127) << 23 : 1u << 22);
 }
 
+// The same scale as its byte, and 2^-e: 2^e (the least with amax <= 1.75 2^(e + 8)) has amax's
+// exponent less 8, and one more where amax's significand passes 1.75, which a carry finds.
+__device__ __forceinline__ uint32_t f8_scale(uint32_t amax, float &inv) {
+  uint32_t field = (uint32_t)min(262 - (int)((amax + 0x1FFFFFu) >> 23), 254);  // of 2^-e
+  if (amax == 0u) field = 127u;
+  inv = __uint_as_float(field << 23);
+  return 254u - field;
+}
+
 // Codes of two values (lo, hi in the low and high byte), |.| <= 448 or NaN.
 __device__ __forceinline__ uint32_t f8_pair(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Codes of four values, |.| <= 448 or NaN, the first in the lowest byte.
+__device__ __forceinline__ uint32_t f8_four(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+      "mov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
 
@@ -97,6 +118,10 @@ struct F8Raw {
   __device__ __forceinline__ float f(int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
     else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ T entry(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __ushort_as_bfloat16((unsigned short)(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu));
   }
   __device__ __forceinline__ void set(int i, T x) {
     if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(x);
@@ -186,6 +211,7 @@ constexpr size_t kF8OffBar = kF8Ring * kF8RingBytes;
 constexpr size_t kF8Bars = 2 * kMaxStages + 2 * kF8Ring + 5;
 constexpr size_t kF8Fixed = (kF8OffBar + kF8Bars * 8 + 16 + 1023) & ~(size_t)1023;
 constexpr size_t kF8BoxBytes = 2048;    // an epilogue warp's box of output
+constexpr size_t kF8TopBytes = 3 * 2 * BM * 4;  // a gated block's maxima (fqt_gated.cuh)
 constexpr int kF8Parts = 8;             // CTAs that share a tile's K blocks at most
 constexpr int kF8Band = 8;              // row tiles of a band of tiles
 
@@ -225,6 +251,7 @@ struct F8Codes {
 struct F8GatedArgs : F8Args {
   const uint32_t *s2;
   int act, part;
+  int boxes_each;  // of an epilogue warp: 2 where codes leave by way of them
   F8Codes q, gate, up;  // outputs as codes, where asked for
   int64_t sp;           // rows of their scales
 };
@@ -619,12 +646,12 @@ __global__ void __launch_bounds__(kF8Threads, 1)
 
   if (KIND == F8_GATED && NT == 256 && warp >= kF8Epi0) {
     if constexpr (KIND == F8_GATED && NT == 256) {
-      uint8_t *boxes = ops + (size_t)g.stages * kStage;
+      uint8_t *tops = ops + (size_t)g.stages * kStage;
       f8_gated_epilogue<ACCS, PAIR, FOLD>(
           maps, g, tmem, accf, acce, abort_flag,
-          reinterpret_cast<float *>(boxes + (size_t)(warp - kF8Epi0) * kF8BoxBytes),
-          reinterpret_cast<uint32_t *>(boxes + kF8EpiWarps * kF8BoxBytes), warp & 3,
-          (warp - kF8Epi0) >> 2, lane, first, step);
+          reinterpret_cast<float *>(tops + kF8TopBytes +
+                                    (size_t)(warp - kF8Epi0) * g.boxes_each * kF8BoxBytes),
+          reinterpret_cast<uint32_t *>(tops), warp & 3, (warp - kF8Epi0) >> 2, lane, first, step);
     }
   } else if (warp >= kF8Epi0) {
     const int q = warp & 3, h = (warp - kF8Epi0) >> 2;
@@ -980,16 +1007,16 @@ template <int NT, int ACCS, bool PAIR, bool FOLD, int KIND>
 static fqt_status launch_f8_as(const typename F8Of<KIND>::Maps &maps,
                                typename F8Of<KIND>::Args &g, int nsm, cudaStream_t st) {
   constexpr size_t stage = kTileBytes + (PAIR ? NT / 2 : NT) * kF8Block;
-  // the epilogue's boxes, and a gated block's maxima (g, u and a, of two halves of 128 rows)
-  constexpr size_t boxes = (NT >= 64 ? kF8EpiWarps * kF8BoxBytes : 0) +
-                           (KIND == F8_GATED && NT == 256 ? 3 * 2 * BM * 4 : 0);
-  constexpr size_t room = 227 * 1024 - 1024 - kF8Fixed - boxes;
-  constexpr int stages = room / stage < kMaxStages ? (int)(room / stage) : kMaxStages;
-  constexpr size_t smem = 1024 + kF8Fixed + stages * stage + boxes;
-  g.stages = stages;
+  constexpr bool wide_gated = KIND == F8_GATED && NT == 256;
+  size_t boxes = NT >= 64 ? kF8EpiWarps * kF8BoxBytes : 0;
+  if constexpr (wide_gated) boxes = boxes * g.boxes_each + kF8TopBytes;
+  constexpr size_t most_smem = 227 * 1024;
+  const size_t room = most_smem - 1024 - kF8Fixed - boxes;
+  g.stages = (int)std::min<size_t>(room / stage, kMaxStages);
+  const size_t smem = 1024 + kF8Fixed + g.stages * stage + boxes;
   auto kernel = k_f8_mm<NT, ACCS, PAIR, FOLD, KIND>;
   static DeviceOnce once;
-  cudaError_t e = allow_smem(kernel, smem, once);
+  cudaError_t e = allow_smem(kernel, wide_gated ? most_smem : smem, once);
   if (e != cudaSuccess) return cuda_fail(e, "FP8 product attribute");
   const int64_t ctas = g.items * (PAIR ? 2 : 1);
   const int most = PAIR ? nsm & ~1 : nsm;

@@ -36,6 +36,7 @@ static fqt_status fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fq
   g.up = codes_of(up);
   g.sp = scale_rows(M);
   g.splits = 1;
+  g.boxes_each = q || gate || up ? 2 : 1;
   const fqt_fp8 *w = Bg;
   g.s2 = reinterpret_cast<const uint32_t *>(Bu->scales);
   F8Of<F8_GATED>::Maps maps = {};

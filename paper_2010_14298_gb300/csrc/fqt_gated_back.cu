@@ -25,7 +25,6 @@ __device__ __forceinline__ f32x2 f8_two(uint32_t w, int i) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
   return pack2(f.x, f.y);
 }
-__device__ __forceinline__ f32x2 both(float v) { return pack2(v, v); }
 __device__ __forceinline__ float f8_scale_of(uint32_t e) { return pow2((int)e - 127); }
 
 // Two columns: dg, du and a from da and the codes' values (before their scales).
@@ -43,76 +42,65 @@ __device__ __forceinline__ void back_two(f32x2 da, f32x2 g, f32x2 u, float sg, f
 // ---------------------------------------------------------------------------
 // Dense outputs alone
 // ---------------------------------------------------------------------------
-// 2^shift lanes take 8 columns each of a row, a thread 4 rows (on their way at once).  VEC:
-// the 8 columns are neighbours in 16-byte accesses; else a lane's columns are 2^shift apart,
-// neighbouring lanes' are neighbours, and a thread takes 2 rows (registers).
-template <bool VEC>
-constexpr int kBackRows = VEC ? 4 : 2;
+// 2^shift lanes take 8 neighbouring columns each of a row, a thread 4 rows (on their way at
+// once).  Rows of da or of an output that lie on no 16 bytes (WIDE false) go by way of shared
+// memory: entry by entry, but neighbouring lanes' are neighbours.  Bound by memory traffic.
+constexpr int kBackRows = 4;
 
-template <typename T, int ACT, bool VEC>
+template <typename T, int ACT, bool WIDE>
 __global__ void __launch_bounds__(256) k_f8_gated_back_dense(const F8BackArgs a, const int shift) {
-  constexpr int R = kBackRows<VEC>;
+  __shared__ __align__(16) T stage[WIDE ? 8 : 256 * 8];
   let_next_start();
   wait_for_previous();
-  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
-  const int64_t row0 = ((int64_t)blockIdx.x * R * 256 + threadIdx.x) >> shift;
-  const int64_t c0 = ((int64_t)blockIdx.y * lanes + (VEC ? lane : 0)) * 8;
+  const int lanes = WIDE ? 1 << shift : 32, lane = threadIdx.x & (lanes - 1);
+  const int64_t row0 = ((int64_t)blockIdx.x * kBackRows * 256 + threadIdx.x) >> shift;
+  const int first = (int)blockIdx.y * lanes * 8, c0 = first + lane * 8;
   const int step = 256 >> shift;  // rows between a thread's
-  auto col = [&](int j) { return VEC ? c0 + j : c0 + lane + (int64_t)lanes * j; };
-  if (col(0) >= a.cols) return;
-  F8Raw<T, 8> da[R];
-  uint2 cg[R], cu[R];
-  uint8_t sg[R][VEC ? 1 : 8], su[R][VEC ? 1 : 8];
+  T *group = stage + (WIDE ? 0 : (threadIdx.x / 32) * 256);
+  const int left = a.cols - first - lane;  // (entry by entry) columns from the lane's first on
+  F8Raw<T, 8> da[kBackRows];
+  uint2 cg[kBackRows], cu[kBackRows];
+  uint8_t sg[kBackRows], su[kBackRows];
+  const bool any = c0 < a.cols;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
+  for (int r = 0; r < kBackRows; ++r) {
     const int64_t row = row0 + r * step;
-    const bool in = row < a.rows;
-    if constexpr (VEC) {
-      da[r].load(static_cast<const T *>(a.da) + row * a.ldda + c0, in ? a.cols - c0 : 0);
-      // (codes past the last column are in the row's 16 bytes; theirs are not stored)
-      cg[r] = in ? __ldg(reinterpret_cast<const uint2 *>(a.gate.codes + row * a.gate.pitch + c0))
-                 : make_uint2(0u, 0u);
-      cu[r] = in ? __ldg(reinterpret_cast<const uint2 *>(a.up.codes + row * a.up.pitch + c0))
-                 : make_uint2(0u, 0u);
-      const int64_t at = in ? scale_at(c0 / kF8Block, a.sp, row) : 0;
-      sg[r][0] = __ldg(a.gate.scales + at);
-      su[r][0] = __ldg(a.up.scales + at);
+    const bool in = row < a.rows && any;
+    const T *p = static_cast<const T *>(a.da) + row * a.ldda;
+    if constexpr (WIDE) {
+      da[r].load(p + c0, in ? a.cols - c0 : 0);
     } else {
-      uint32_t g[2] = {0u, 0u}, u[2] = {0u, 0u};
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const bool there = in && col(j) < a.cols;
-        da[r].set(j, there ? static_cast<const T *>(a.da)[row * a.ldda + col(j)] : (T)0.0f);
-        if (there) {
-          g[j / 4] |= (uint32_t)__ldg(a.gate.codes + row * a.gate.pitch + col(j)) << 8 * (j % 4);
-          u[j / 4] |= (uint32_t)__ldg(a.up.codes + row * a.up.pitch + col(j)) << 8 * (j % 4);
-        }
-        const int64_t at = there ? scale_at(col(j) / kF8Block, a.sp, row) : 0;
-        sg[r][j] = __ldg(a.gate.scales + at);
-        su[r][j] = __ldg(a.up.scales + at);
+        da[r].set(j, row < a.rows && 32 * j < left ? p[first + lane + 32 * j] : (T)0.0f);
       }
-      cg[r] = make_uint2(g[0], g[1]);
-      cu[r] = make_uint2(u[0], u[1]);
     }
+    // (codes past the last column are in the row's 16 bytes; theirs are not stored)
+    cg[r] = in ? __ldg(reinterpret_cast<const uint2 *>(a.gate.codes + row * a.gate.pitch + c0))
+               : make_uint2(0u, 0u);
+    cu[r] = in ? __ldg(reinterpret_cast<const uint2 *>(a.up.codes + row * a.up.pitch + c0))
+               : make_uint2(0u, 0u);
+    const int64_t at = in ? scale_at(c0 / kF8Block, a.sp, row) : 0;
+    sg[r] = __ldg(a.gate.scales + at);
+    su[r] = __ldg(a.up.scales + at);
   }
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
+  for (int r = 0; r < kBackRows; ++r) {
     const int64_t row = row0 + r * step;
-    if (row >= a.rows) return;
+    if constexpr (!WIDE) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) group[lane + 32 * j] = da[r].entry(j);
+      __syncwarp();
+      da[r].take(group + lane * 8);
+      __syncwarp();
+    }
     uint32_t v[2][8];
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-      const f32x2 g = f8_two(j < 4 ? cg[r].x : cg[r].y, (j >> 1) & 1);
-      const f32x2 u = f8_two(j < 4 ? cu[r].x : cu[r].y, (j >> 1) & 1);
       f32x2 dg, du, unused;
-      if constexpr (VEC) {
-        back_two<ACT>(pack2(da[r].f(j), da[r].f(j + 1)), g, u, f8_scale_of(sg[r][0]),
-                      f8_scale_of(su[r][0]), dg, du, unused);
-      } else {  // two columns of blocks of their own
-        const f32x2 g2 = mul2(g, pack2(f8_scale_of(sg[r][j]), f8_scale_of(sg[r][j + 1])));
-        const f32x2 u2 = mul2(u, pack2(f8_scale_of(su[r][j]), f8_scale_of(su[r][j + 1])));
-        back_two<ACT>(pack2(da[r].f(j), da[r].f(j + 1)), g2, u2, 1.0f, 1.0f, dg, du, unused);
-      }
+      back_two<ACT>(pack2(da[r].f(j), da[r].f(j + 1)), f8_two(j < 4 ? cg[r].x : cg[r].y, (j >> 1) & 1),
+                    f8_two(j < 4 ? cu[r].x : cu[r].y, (j >> 1) & 1), f8_scale_of(sg[r]),
+                    f8_scale_of(su[r]), dg, du, unused);
       float x, y;
       unpack2(dg, x, y);
       v[0][j] = __float_as_uint(x), v[0][j + 1] = __float_as_uint(y);
@@ -124,14 +112,26 @@ __global__ void __launch_bounds__(256) k_f8_gated_back_dense(const F8BackArgs a,
       T *out = static_cast<T *>(k ? a.dup : a.dgate);
       if (!out) continue;
       out += row * (k ? a.lddu : a.lddg);
-      if (VEC && c0 + 8 <= a.cols) {
+      if constexpr (WIDE) {
+        if (row >= a.rows) continue;
+        if (c0 + 8 <= a.cols) {
 #pragma unroll
-        for (int j = 0; j < 8; j += 16 / (int)sizeof(T))
-          *reinterpret_cast<uint4 *>(out + c0 + j) = f8_pack<T>(&v[k][j]);
+          for (int j = 0; j < 8; j += 16 / (int)sizeof(T))
+            *reinterpret_cast<uint4 *>(out + c0 + j) = f8_pack<T>(&v[k][j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c0 + j < a.cols) out[c0 + j] = f8_out<T>(__uint_as_float(v[k][j]));
+        }
       } else {
 #pragma unroll
+        for (int j = 0; j < 8; j += 16 / (int)sizeof(T))
+          *reinterpret_cast<uint4 *>(group + lane * 8 + j) = f8_pack<T>(&v[k][j]);
+        __syncwarp();
+#pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (col(j) < a.cols) out[col(j)] = f8_out<T>(__uint_as_float(v[k][j]));
+          if (row < a.rows && 32 * j < left) out[first + lane + 32 * j] = group[lane + 32 * j];
+        __syncwarp();
       }
     }
   }
@@ -140,11 +140,12 @@ __global__ void __launch_bounds__(256) k_f8_gated_back_dense(const F8BackArgs a,
 // ---------------------------------------------------------------------------
 // Codes
 // ---------------------------------------------------------------------------
-// One persistent CTA an SM over 128 x 128 tiles.  A thread holds 4 rows x 8 columns of dg, du
-// and a in registers (96 of them), so it packs codes along either axis without exchanging
-// bytes; what it reads (da, both codes and their scales: 65 or 97 KB a tile) comes ahead of
-// time into shared memory by TMA, two tiles deep for bf16, one for fp32, so that loads run
-// under the arithmetic of the tile before.
+// One persistent CTA an SM over 128 x 128 tiles.  A warp takes 8 rows, a lane 4 columns of
+// them, and holds dg, du and a of its 32 entries in registers (96).  So a row's maximum is one
+// reduction of the warp, a column's needs no exchange within it, and a lane packs codes along
+// either axis without exchanging bytes.  What the tile reads (da, both codes and their scales:
+// 65 or 97 KB) comes ahead of time into shared memory by TMA, two tiles deep for bf16, one for
+// fp32, so that loads run under the arithmetic of the tile before.
 constexpr int kF8BackThreads = 512, kF8BackWarps = kF8BackThreads / 32;
 
 template <typename T>
@@ -155,31 +156,26 @@ struct F8BackShared {
     uint8_t gate[kF8Block * kF8Block], up[kF8Block * kF8Block];
     uint32_t sg[kF8Block], su[kF8Block];  // four blocks' scales of a row, one of them the tile's
   } in[stages];
-  // a column's 32 words of 4 rows' codes, word w at place w ^ 2 (column / 8): a warp's
-  // threads, 16 columns 8 apart x 2 words, write 32 banks
-  uint32_t tr[3][kF8Block * 32];
-  uint32_t top[3][kF8BackWarps][kF8Block];  // column maxima by warp
-  float inv[3][kF8Block];                   // and what a column's entries are multiplied by
+  uint2 tr[3][kF8Block * 16];  // a column's codes, 8 rows (a warp's) at a time: back_at
+  float top[3][kF8BackWarps][kF8Block];  // column maxima by warp
+  float inv[3][kF8Block];                // and what a column's entries are multiplied by
+  // of a warp's 8 rows: the scales of g, then of u; the maxima of dg, then of du, and what
+  // their entries are multiplied by
+  float scale[kF8BackWarps][16];
+  uint32_t row_top[kF8BackWarps][16];
+  float row_inv[kF8BackWarps][16];
   uint64_t full[stages];
 };
+
+// The place of a warp's 8 codes of a column: half a warp's lanes (columns 4 apart) write 32
+// banks, and half a warp that reads two columns' 16-byte chunks does, too.
+__device__ __forceinline__ int back_at(int col, int warp) {
+  return col * 16 + (warp ^ ((col >> 2 & 15) ^ (col & 1)));
+}
 
 struct F8BackMaps {
   CUtensorMap da, gate, up;
 };
-
-// The larger of m and |x|, |y| (NaN if one is).
-__device__ __forceinline__ float top2(float m, f32x2 v) {
-  float x, y, r;
-  unpack2(v, x, y);
-  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ float top3(float a, float b, float c) {
-  float r;
-  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ bool is_odd(float top) { return __float_as_uint(top) >= 0x7F800000u; }
 
 // Bytes (a multiple of 16, both ends on 16) into shared memory, counted by a barrier.
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes,
@@ -216,7 +212,6 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
   constexpr int S = F8BackShared<T>::stages;
   let_next_start();
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  const int cg = t & 15, rg = t >> 4;  // its 8 columns and its 4 rows
   if (t == 0) {
     for (int i = 0; i < S; ++i) mbar_init(&s.full[i], 1);
     fence_barrier_init();
@@ -227,13 +222,13 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
     for (int i = 0; i < S; ++i)
       if (blockIdx.x + (int64_t)i * gridDim.x < a.tiles)
         back_fetch(maps, a, s, i, blockIdx.x + (int64_t)i * gridDim.x, vec);
-  const bool by_rows = a.q[0].codes || a.q[1].codes;
   int n = 0;
   bool ok = true;
   for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++n) {
     const int64_t ct = tile / a.row_tiles, rt = tile - ct * a.row_tiles;
     const int64_t r0 = rt * kF8Block, c0 = ct * kF8Block;
-    const int64_t row = r0 + rg * 4, col = c0 + cg * 8;
+    const int64_t row = r0 + warp * 8, col = c0 + lane * 4;
+    const int rows = (int)min((int64_t)8, a.rows - row);  // of the warp's (it may have none)
     auto &in = s.in[n % S];
     if (!vec) {  // the warp's 8 rows, entry by entry, but neighbouring lanes read neighbours
       T e[8][kF8Block / 32];
@@ -249,27 +244,40 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
       __syncwarp();
     }
     ok = f8_wait(&s.full[n % S], (n / S) & 1, a.status);
-    f32x2 v[3][4][4];  // dg, du, a
+    f32x2 v[3][8][2];  // dg, du, a
     {
-      const uint4 wg = *reinterpret_cast<const uint4 *>(&in.sg[rg * 4]);
-      const uint4 wu = *reinterpret_cast<const uint4 *>(&in.su[rg * 4]);
-      const uint32_t sg[4] = {wg.x, wg.y, wg.z, wg.w}, su[4] = {wu.x, wu.y, wu.z, wu.w};
-      const int byte = 8 * (int)(ct & 3);
+      // lanes 0..7 prepare the scales of the warp's rows of g, lanes 8..15 of u (1 for rows past
+      // the end, which are zeros)
+      if (lane < 16) {
+        const uint32_t w = (lane < 8 ? in.sg : in.su)[warp * 8 + (lane & 7)];
+        s.scale[warp][lane] =
+            (lane & 7) < rows ? f8_scale_of(w >> 8 * (int)(ct & 3) & 255u) : 1.0f;
+      }
+      __syncwarp();
+      float4 fs[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = (rg * 4 + i) * kF8Block + cg * 8;
-        F8Raw<T, 8> da;
-        da.take(in.da + at);
-        const uint2 g = *reinterpret_cast<const uint2 *>(in.gate + at);
-        const uint2 u = *reinterpret_cast<const uint2 *>(in.up + at);
-        // (rows past the end: zeros, whatever their scale)
-        const bool there = row + i < a.rows;
-        const float fg = there ? f8_scale_of(sg[i] >> byte & 255u) : 1.0f;
-        const float fu = there ? f8_scale_of(su[i] >> byte & 255u) : 1.0f;
+      for (int i = 0; i < 8; ++i) {
+        if (i % 4 == 0) {
+          fs[0] = *reinterpret_cast<const float4 *>(&s.scale[warp][i]);
+          fs[1] = *reinterpret_cast<const float4 *>(&s.scale[warp][8 + i]);
+        }
+        const int r = warp * 8 + i, at = r * kF8Block + lane * 4;
+        f32x2 da[2];
+        if constexpr (sizeof(T) == 4) {
+          const float4 x = *reinterpret_cast<const float4 *>(in.da + at);
+          da[0] = pack2(x.x, x.y), da[1] = pack2(x.z, x.w);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2 *>(in.da + at);
+          da[0] = pack2(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u));
+          da[1] = pack2(__uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u));
+        }
+        const uint32_t g = *reinterpret_cast<const uint32_t *>(in.gate + at);
+        const uint32_t u = *reinterpret_cast<const uint32_t *>(in.up + at);
+        const float fg = i % 4 == 0 ? fs[0].x : i % 4 == 1 ? fs[0].y : i % 4 == 2 ? fs[0].z : fs[0].w;
+        const float fu = i % 4 == 0 ? fs[1].x : i % 4 == 1 ? fs[1].y : i % 4 == 2 ? fs[1].z : fs[1].w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          back_two<ACT>(pack2(da.f(2 * j), da.f(2 * j + 1)), f8_two(j < 2 ? g.x : g.y, j & 1),
-                        f8_two(j < 2 ? u.x : u.y, j & 1), fg, fu, v[0][i][j], v[1][i][j],
+        for (int j = 0; j < 2; ++j)
+          back_two<ACT>(da[j], f8_two(g, j), f8_two(u, j), fg, fu, v[0][i][j], v[1][i][j],
                         v[2][i][j]);
       }
     }
@@ -279,173 +287,147 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
       T *out = static_cast<T *>(k ? a.dup : a.dgate);
       if (!out) continue;
       const int64_t ld = k ? a.lddu : a.lddg;
-      const bool wide = f8_pitch_aligned<T>(out, ld) && col + 8 <= a.cols;
+      const bool wide = f8_pitch_aligned<T>(out, ld) && col + 4 <= a.cols;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (row + i >= a.rows) break;
-        uint32_t x[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float lo, hi;
-          unpack2(v[k][i][j], lo, hi);
-          x[2 * j] = __float_as_uint(lo), x[2 * j + 1] = __float_as_uint(hi);
-        }
+      for (int i = 0; i < 8; ++i) {
+        if (i >= rows) break;
+        float x[4];
+        unpack2(v[k][i][0], x[0], x[1]);
+        unpack2(v[k][i][1], x[2], x[3]);
         T *p = out + (row + i) * ld + col;
-        if (wide) {
-#pragma unroll
-          for (int j = 0; j < 8; j += 16 / (int)sizeof(T))
-            *reinterpret_cast<uint4 *>(p + j) = f8_pack<T>(&x[j]);
+        if (wide && sizeof(T) == 4) {
+          *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+        } else if (wide) {
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]);
+          const __nv_bfloat162 hi = __floats2bfloat162_rn(x[2], x[3]);
+          *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo),
+                                                     *reinterpret_cast<const uint32_t *>(&hi));
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (col + j < a.cols) p[j] = f8_out<T>(__uint_as_float(x[j]));
+          for (int j = 0; j < 4; ++j)
+            if (col + j < a.cols) p[j] = f8_out<T>(x[j]);
         }
       }
     }
-    // Maxima.  Entries that are not finite count for none and become NaN, whose code is
-    // NaN's.
-    float rm[8];  // of row i of dg (i) and of du (4 + i)
+    // Column maxima.  Entries that are not finite count for none and become NaN, whose code
+    // is NaN's.
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      if (!a.qt[k].codes && (k == 2 || !a.q[k].codes)) {
-        if (k < 2)
+      if (!a.qt[k].codes && (k == 2 || !a.q[k].codes)) continue;
+      float cm[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) rm[4 * k + i] = 0.0f;
-        continue;
+      for (int j = 0; j < 2; ++j) {
+        float x[8], y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) unpack2(v[k][i][j], x[i], y[i]);
+        cm[2 * j] = top3(top3(top3(x[0], x[1], x[2]), x[3], x[4]), top3(x[5], x[6], x[7]), 0.0f);
+        cm[2 * j + 1] = top3(top3(top3(y[0], y[1], y[2]), y[3], y[4]), top3(y[5], y[6], y[7]), 0.0f);
       }
-      float r[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        r[i] = top2(top2(top2(top2(0.0f, v[k][i][0]), v[k][i][1]), v[k][i][2]), v[k][i][3]);
-      float cm[8];
-      if (!is_odd(top3(top3(r[0], r[1], r[2]), r[3], 0.0f))) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float x[4], y[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) unpack2(v[k][i][j], x[i], y[i]);
-          cm[2 * j] = top3(top3(x[0], x[1], x[2]), x[3], 0.0f);
-          cm[2 * j + 1] = top3(top3(y[0], y[1], y[2]), y[3], 0.0f);
-        }
-      } else {
+      if (is_odd(top3(top3(cm[0], cm[1], cm[2]), cm[3], 0.0f))) {
         record_status(a.status, FQT_ENONFINITE);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) cm[j] = 0.0f;
+        for (int j = 0; j < 2; ++j) {
+          cm[2 * j] = cm[2 * j + 1] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          r[i] = 0.0f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int i = 0; i < 8; ++i) {
             float x[2];
             unpack2(v[k][i][j], x[0], x[1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              if (is_odd(fabsf(x[h]))) {
-                x[h] = __uint_as_float(0x7FFFFFFFu);
-              } else {
-                r[i] = fmaxf(r[i], fabsf(x[h]));
-                cm[2 * j + h] = fmaxf(cm[2 * j + h], fabsf(x[h]));
-              }
+              if (is_odd(x[h])) x[h] = __uint_as_float(0x7FFFFFFFu);
+              else cm[2 * j + h] = fmaxf(cm[2 * j + h], fabsf(x[h]));
             }
             v[k][i][j] = pack2(x[0], x[1]);
           }
         }
       }
-      if (k < 2)
+      *reinterpret_cast<float4 *>(&s.top[k][warp][lane * 4]) =
+          make_float4(cm[0], cm[1], cm[2], cm[3]);
+    }
+    // row maxima (of what are numbers now): lane c keeps row c % 8 of tensor c / 8
+    if (a.q[0].codes || a.q[1].codes) {
+      uint32_t mine = 0u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rm[4 * k + i] = r[i];
-      if (a.qt[k].codes) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          cm[j] = fmaxf(cm[j], __shfl_xor_sync(0xffffffffu, cm[j], 16));
-        if (lane < 16) {
-          float4 *to = reinterpret_cast<float4 *>(&s.top[k][warp][cg * 8]);
-          to[0] = make_float4(cm[0], cm[1], cm[2], cm[3]);
-          to[1] = make_float4(cm[4], cm[5], cm[6], cm[7]);
-        }
+      for (int c = 0; c < 16; ++c) {
+        float x[4];
+        unpack2(v[c / 8][c % 8][0], x[0], x[1]);
+        unpack2(v[c / 8][c % 8][1], x[2], x[3]);
+        const float m = top3_number(top3_number(x[0], x[1], x[2]), x[3], 0.0f);
+        const uint32_t r = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+        if (lane == c) mine = r;
       }
+      if (lane < 16) s.row_top[warp][lane] = mine;
     }
     if (__syncthreads_or(!ok)) break;
-    if (t == 0 && tile + (int64_t)S * gridDim.x < a.tiles)  // everybody has read the stage
+    // the scales: three quarters of the threads a column of one tensor each, the others two
+    // rows; one of the others also asks for the next tile, as everybody has read this one's
+    // stage
+    if (t == kF8BackThreads - 1 && tile + (int64_t)S * gridDim.x < a.tiles)
       back_fetch(maps, a, s, n % S, tile + (int64_t)S * gridDim.x, vec);
-    if (by_rows) {
-      // The 8 maxima over the 16 lanes of a row group, halving what a lane holds: lane cg
-      // ends with tensor cg / 8's row cg / 2 % 4, and hands its factor to the others.
-      float m[4];
+    if (t < 3 * kF8Block && a.qt[t / kF8Block].codes) {
+      const int k = t / kF8Block, j = t % kF8Block;
+      float m = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float keep = cg & 8 ? rm[4 + i] : rm[i], give = cg & 8 ? rm[i] : rm[4 + i];
-        m[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 8));
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float keep = cg & 4 ? m[2 + i] : m[i], give = cg & 4 ? m[i] : m[2 + i];
-        m[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 4));
-      }
-      const float keep = cg & 2 ? m[1] : m[0], give = cg & 2 ? m[0] : m[1];
-      m[0] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 2));
-      m[0] = fmaxf(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
-      const int e = f8_exponent(__float_as_uint(m[0]));
-      const float inv = pow2(-e);
-      const F8Codes &mine = a.q[cg >> 3];
-      if (!(cg & 1) && mine.codes && row + (cg >> 1 & 3) < a.rows)
-        mine.scales[scale_at(ct, a.sp, row + (cg >> 1 & 3))] = (uint8_t)(e + 127);
+      for (int w = 0; w < kF8BackWarps; w += 2) m = top3(m, s.top[k][w][j], s.top[k][w + 1][j]);
+      const uint32_t e = f8_scale(__float_as_uint(m), s.inv[k][j]);
+      if (c0 + j < a.cols) a.qt[k].scales[scale_at(rt, a.spt, c0 + j)] = (uint8_t)e;
+    }
+    if (t >= 3 * kF8Block) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        uint8_t *to = a.q[k].codes + row * a.q[k].pitch + col;
+        const int r = t - 3 * kF8Block;  // of the tile's
+        if (!a.q[k].codes) continue;
+        const uint32_t e = f8_scale(s.row_top[r / 8][k * 8 + r % 8], s.row_inv[r / 8][k * 8 + r % 8]);
+        if (r0 + r < a.rows) a.q[k].scales[scale_at(ct, a.sp, r0 + r)] = (uint8_t)e;
+      }
+    }
+    __syncthreads();
+    const bool there = col < a.cols;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x2 f = both(__shfl_sync(0xffffffffu, inv, (lane & 16) | k << 3 | i << 1));
-          if (!a.q[k].codes || row + i >= a.rows || col >= a.cols) continue;
-          uint32_t c[4];
+    for (int kk = 0; kk < 3; ++kk) {
+      const int k = 2 - kk;  // a first, which has no rows
+      if (a.qt[k].codes) {
+        const float4 f = *reinterpret_cast<const float4 *>(&s.inv[k][lane * 4]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float x, y;
-            unpack2(mul2(v[k][i][j], f), x, y);
-            c[j] = f8_pair(x, y);
-          }
-          *reinterpret_cast<uint2 *>(to + i * a.q[k].pitch) =
-              make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+        for (int j = 0; j < 2; ++j) {
+          const f32x2 f2 = j ? pack2(f.z, f.w) : pack2(f.x, f.y);
+          float x[8], y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) unpack2(mul2(v[k][i][j], f2), x[i], y[i]);
+          s.tr[k][back_at(lane * 4 + 2 * j, warp)] =
+              make_uint2(f8_four(x[0], x[1], x[2], x[3]), f8_four(x[4], x[5], x[6], x[7]));
+          s.tr[k][back_at(lane * 4 + 2 * j + 1, warp)] =
+              make_uint2(f8_four(y[0], y[1], y[2], y[3]), f8_four(y[4], y[5], y[6], y[7]));
+        }
+      }
+      if (k < 2 && a.q[k < 2 ? k : 0].codes) {
+        const F8Codes &q = a.q[k < 2 ? k : 0];
+        uint8_t *to = q.codes + row * q.pitch + col;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const f32x2 f = both(s.row_inv[warp][k * 8 + i]);
+          float x[4];
+          unpack2(mul2(v[k][i][0], f), x[0], x[1]);
+          unpack2(mul2(v[k][i][1], f), x[2], x[3]);
+          if (there && i < rows) *reinterpret_cast<uint32_t *>(to) = f8_four(x[0], x[1], x[2], x[3]);
+          to += q.pitch;
         }
       }
     }
     if (!a.qt[0].codes && !a.qt[1].codes && !a.qt[2].codes) continue;
-    if (t < 3 * kF8Block && a.qt[t / kF8Block].codes) {
-      const int k = t / kF8Block, j = t % kF8Block;
-      uint32_t m = 0u;
-#pragma unroll
-      for (int w = 0; w < kF8BackWarps; ++w) m = max(m, s.top[k][w][j]);
-      const int e = f8_exponent(m);
-      s.inv[k][j] = pow2(-e);
-      if (c0 + j < a.cols) a.qt[k].scales[scale_at(rt, a.spt, c0 + j)] = (uint8_t)(e + 127);
-    }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       if (!a.qt[k].codes) continue;
+      const int j = t >> 3, ch = t & 7;
+      const uint2 *from[2] = {&s.tr[k][back_at(j, 2 * ch)], &s.tr[k][back_at(j, 2 * ch + 1)]};
+      uint8_t *to = a.qt[k].codes + (c0 + j) * a.qt[k].pitch + r0 + ch * 16;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 f = *reinterpret_cast<const float2 *>(&s.inv[k][cg * 8 + 2 * j]);
-        float x[4], y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) unpack2(mul2(v[k][i][j], pack2(f.x, f.y)), x[i], y[i]);
-        uint32_t *to = &s.tr[k][(cg * 8 + 2 * j) * 32 + (rg ^ (2 * cg))];
-        to[0] = f8_pair(x[0], x[1]) | f8_pair(x[2], x[3]) << 16;
-        to[32] = f8_pair(y[0], y[1]) | f8_pair(y[2], y[3]) << 16;
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      if (!a.qt[k].codes) continue;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int at = h * kF8BackThreads + t, j = at >> 3, ch = at & 7;
-        if (c0 + j >= a.cols || r0 + ch * 16 >= a.rows) continue;
-        const uint2 *pairs = reinterpret_cast<const uint2 *>(s.tr[k] + j * 32);
-        const uint2 lo = pairs[(2 * ch) ^ (j >> 3)], hi = pairs[(2 * ch + 1) ^ (j >> 3)];
-        *reinterpret_cast<uint4 *>(a.qt[k].codes + (c0 + j) * a.qt[k].pitch + r0 + ch * 16) =
-            make_uint4(lo.x, lo.y, hi.x, hi.y);
+      for (int h = 0; h < 2; ++h) {  // columns j and j + 64: the same places of their words
+        const uint2 lo = from[0][64 * 16 * h], hi = from[1][64 * 16 * h];
+        if (c0 + j + 64 * h < a.cols && r0 + ch * 16 < a.rows)
+          *reinterpret_cast<uint4 *>(to) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        to += 64 * a.qt[k].pitch;
       }
     }
   }
@@ -482,8 +464,8 @@ static fqt_status launch_back(F8BackArgs &a, const fqt_fp8 *gate, const fqt_fp8 
                       (!a.dup || f8_pitch_aligned<T>(a.dup, a.lddu));
     const int64_t chunks = ((int64_t)a.cols + 7) / 8;
     int shift = 0;
-    while (shift < 5 && ((int64_t)1 << shift) < chunks) ++shift;
-    const int64_t rows = (int64_t)(wide ? kBackRows<true> : kBackRows<false>) * 256 >> shift;
+    while (shift < 5 && (!wide || ((int64_t)1 << shift) < chunks)) ++shift;
+    const int64_t rows = (int64_t)kBackRows * 256 >> shift;
     const dim3 grid((unsigned)((a.rows + rows - 1) / rows),
                     (unsigned)((chunks + (1 << shift) - 1) >> shift));
     auto kernel = wide ? k_f8_gated_back_dense<T, ACT, true> : k_f8_gated_back_dense<T, ACT, false>;

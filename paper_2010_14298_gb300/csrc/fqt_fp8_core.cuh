@@ -211,7 +211,8 @@ constexpr size_t kF8OffBar = kF8Ring * kF8RingBytes;
 constexpr size_t kF8Bars = 2 * kMaxStages + 2 * kF8Ring + 5;
 constexpr size_t kF8Fixed = (kF8OffBar + kF8Bars * 8 + 16 + 1023) & ~(size_t)1023;
 constexpr size_t kF8BoxBytes = 2048;    // an epilogue warp's box of output
-constexpr size_t kF8TopBytes = 3 * 2 * BM * 4;  // a gated block's maxima (fqt_gated.cuh)
+constexpr size_t kF8TopBytes = 4 * 4 * BM * 4;  // a gated block's maxima (fqt_gated.cuh)
+constexpr size_t kF8QuadBoxes = 3 * 32 * 128;   // and four warps' boxes of codes
 constexpr int kF8Parts = 8;             // CTAs that share a tile's K blocks at most
 constexpr int kF8Band = 8;              // row tiles of a band of tiles
 
@@ -232,8 +233,11 @@ struct F8Args {
 };
 
 // What a product is made of: one pair of matrices; the sum of two pairs' products; or a
-// gated block's projections, whose epilogue joins them (fqt_gated.cuh).
-enum F8Kind { F8_ONE, F8_SUM, F8_GATED };
+// gated block's projections, whose epilogue joins them (fqt_gated.cuh),
+// with codes for outputs, a dense output, or both.
+enum F8Kind { F8_ONE, F8_SUM, F8_GATED, F8_GATED_DENSE, F8_GATED_BOTH };
+constexpr bool f8_gated(int kind) { return kind >= F8_GATED; }
+constexpr bool f8_gated_with_codes(int kind) { return kind == F8_GATED || kind == F8_GATED_BOTH; }
 
 // Two pairs: their K blocks follow one another, the second's from a group of scales on.
 struct F8SumArgs : F8Args {
@@ -251,7 +255,6 @@ struct F8Codes {
 struct F8GatedArgs : F8Args {
   const uint32_t *s2;
   int act, part;
-  int boxes_each;  // of an epilogue warp: 2 where codes leave by way of them
   F8Codes q, gate, up;  // outputs as codes, where asked for
   int64_t sp;           // rows of their scales
 };
@@ -277,6 +280,10 @@ struct F8Of<F8_GATED> {
     CUtensorMap a, b, out, b2, q, gate, up;
   };
 };
+template <>
+struct F8Of<F8_GATED_DENSE> : F8Of<F8_GATED> {};
+template <>
+struct F8Of<F8_GATED_BOTH> : F8Of<F8_GATED> {};
 
 // mbar_wait without its read of the timer at the first miss, which takes longer than a
 // K block's products: the timer is read after a few tries that sleep.
@@ -384,16 +391,17 @@ struct F8Item {
 template <int NT, bool PAIR>
 __device__ __forceinline__ F8Item f8_item(const F8Args &g, int64_t it) {
   F8Item t;
-  const int64_t r = PAIR ? it : it / g.splits;
+  // (in 32 bits: at most 2^31 tiles, and 2^15 parts of few)
+  const uint32_t i = (uint32_t)it, r = PAIR ? i : i / (uint32_t)g.splits;
   // bands of kF8Band row tiles, so that the tiles in flight share rows of both operands
-  const int64_t band = r / ((int64_t)kF8Band * g.n_tiles);
-  const int64_t in = r - band * kF8Band * g.n_tiles;
-  const int high = (int)min((int64_t)kF8Band, g.m_tiles - band * kF8Band);
-  const int64_t n = in / high;
-  t.n0 = n * NT;
-  t.m0 = (band * kF8Band + in - n * high) * (PAIR ? 2 * BM : BM) +
+  const uint32_t band = r / ((uint32_t)kF8Band * (uint32_t)g.n_tiles);
+  const uint32_t in = r - band * kF8Band * (uint32_t)g.n_tiles;
+  const uint32_t high = min((uint32_t)kF8Band, (uint32_t)g.m_tiles - band * kF8Band);
+  const uint32_t n = in / high;
+  t.n0 = (int64_t)n * NT;
+  t.m0 = (int64_t)(band * kF8Band + in - n * high) * (PAIR ? 2 * BM : BM) +
          (PAIR ? (blockIdx.x & 1) * BM : 0);
-  t.kb0 = PAIR ? 0 : (int)(it - r * g.splits) * g.kb_per;
+  t.kb0 = PAIR ? 0 : (int)(i - r * (uint32_t)g.splits) * g.kb_per;
   t.kb1 = min(g.nkb, t.kb0 + g.kb_per);
   return t;
 }
@@ -401,7 +409,7 @@ __device__ __forceinline__ F8Item f8_item(const F8Args &g, int64_t it) {
 // Few tokens of a gated block: a CTA takes g.part rows of both weights, and all tokens.
 template <int NT, bool PAIR, int KIND, typename A>
 __device__ __forceinline__ F8Item f8_item_of(const A &g, int64_t it) {
-  if constexpr (KIND == F8_GATED && NT <= 64) return F8Item{it * g.part, 0, 0, g.nkb};
+  if constexpr (f8_gated(KIND) && NT <= 64) return F8Item{it * g.part, 0, 0, g.nkb};
   else return f8_item<NT, PAIR>(g, it);
 }
 
@@ -551,6 +559,11 @@ __device__ __forceinline__ void f8_join(const F8Args &g, int64_t it, const float
   }
 }
 
+// With codes, a gated block's epilogue has more to do for each accumulator: twice the warps, a
+// quarter of the columns each.
+template <int NT, int KIND>
+constexpr int kF8EpiOf = f8_gated_with_codes(KIND) && NT == 256 ? 2 * kF8EpiWarps : kF8EpiWarps;
+
 // of a gated block's projections (fqt_gated.cuh)
 template <int NT, bool PAIR>
 __device__ __forceinline__ void f8_load_gated(const F8Of<F8_GATED>::Maps &maps,
@@ -560,12 +573,17 @@ template <int NT>
 __device__ __forceinline__ uint32_t f8_gated_scales(const F8GatedArgs &g, const F8Item &t,
                                                     int64_t group, int i, int lane);
 template <int ACCS, bool PAIR, bool FOLD>
-__device__ __forceinline__ void f8_gated_epilogue(const F8Of<F8_GATED>::Maps &maps,
-                                                  const F8GatedArgs &g, uint32_t tmem,
-                                                  uint64_t *accf, uint64_t *acce,
-                                                  volatile int *abort_flag, float *box,
-                                                  uint32_t *tops, int q, int h, int lane,
-                                                  int64_t first, int64_t step);
+__device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
+                                               const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
+                                               uint64_t *acce, volatile int *abort_flag, float *box,
+                                               int q, int h, int lane, int64_t first,
+                                               int64_t step);
+template <int ACCS, bool PAIR, bool DENSE>
+__device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
+                                               const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
+                                               uint64_t *acce, volatile int *abort_flag,
+                                               uint8_t *boxes, uint32_t *tops, int q, int h,
+                                               int lane, int64_t first, int64_t step);
 template <int W>
 __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float *part);
 
@@ -579,10 +597,10 @@ __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float 
 // the products go on meanwhile.  FOLD: an accumulator holds g.chunk K blocks, and the
 // epilogue adds them up.
 template <int NT, int ACCS, bool PAIR, bool FOLD, int KIND>
-__global__ void __launch_bounds__(kF8Threads, 1)
+__global__ void __launch_bounds__(32 * (kF8Epi0 + kF8EpiOf<NT, KIND>), 1)
     k_f8_mm(const __grid_constant__ typename F8Of<KIND>::Maps maps,
             const typename F8Of<KIND>::Args g) {
-  constexpr bool kJoins = KIND == F8_GATED && NT <= 64;  // (few tokens)
+  constexpr bool kJoins = f8_gated(KIND) && NT <= 64;  // (few tokens)
   // columns of an epilogue warp: a multiple of 32 for the first half's
   constexpr int W0 = NT <= 64 ? NT / 2 : (NT / 2 + 31) / 32 * 32, W1 = NT - W0;
   constexpr int NB = PAIR ? NT / 2 : NT;    // rows of B that this CTA loads
@@ -612,7 +630,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&accf[i], 1);
-      mbar_init(&acce[i], (PAIR ? 2 : 1) * kF8EpiWarps);
+      mbar_init(&acce[i], (PAIR ? 2 : 1) * kF8EpiOf<NT, KIND>);
     }
     for (int i = 0; i < kF8Ring; ++i) {
       mbar_init(&sfull[i], PAIR ? 2 : 1);
@@ -644,15 +662,17 @@ __global__ void __launch_bounds__(kF8Threads, 1)
   const uint32_t tmem = *tmem_slot;
   wait_for_previous();
 
-  if (KIND == F8_GATED && NT == 256 && warp >= kF8Epi0) {
-    if constexpr (KIND == F8_GATED && NT == 256) {
-      uint8_t *tops = ops + (size_t)g.stages * kStage;
-      f8_gated_epilogue<ACCS, PAIR, FOLD>(
-          maps, g, tmem, accf, acce, abort_flag,
-          reinterpret_cast<float *>(tops + kF8TopBytes +
-                                    (size_t)(warp - kF8Epi0) * g.boxes_each * kF8BoxBytes),
-          reinterpret_cast<uint32_t *>(tops), warp & 3, (warp - kF8Epi0) >> 2, lane, first, step);
-    }
+  if (f8_gated(KIND) && NT == 256 && warp >= kF8Epi0) {
+    uint8_t *after = ops + (size_t)g.stages * kStage;
+    const int e = warp - kF8Epi0;
+    if constexpr (f8_gated_with_codes(KIND) && NT == 256)
+      f8_gated_codes<ACCS, PAIR, KIND == F8_GATED_BOTH>(maps, g, tmem, accf, acce, abort_flag, after + kF8TopBytes,
+                                       reinterpret_cast<uint32_t *>(after), warp & 3, e >> 2, lane,
+                                       first, step);
+    else if constexpr (KIND == F8_GATED_DENSE && NT == 256)
+      f8_gated_dense<ACCS, PAIR, FOLD>(maps, g, tmem, accf, acce, abort_flag,
+                                       reinterpret_cast<float *>(after + e * kF8BoxBytes), warp & 3,
+                                       e >> 2, lane, first, step);
   } else if (warp >= kF8Epi0) {
     const int q = warp & 3, h = (warp - kF8Epi0) >> 2;
     const int W = h ? W1 : W0;
@@ -763,7 +783,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
             break;
           }
           uint8_t *st = ops + (size_t)s * kStage;
-          if constexpr (KIND == F8_GATED) {
+          if constexpr (f8_gated(KIND)) {
             f8_load_gated<NT, PAIR>(maps, g, st, t, kb, rank, &full[s]);
           } else {
             const CUtensorMap *ma = &maps.a, *mb = &maps.b;
@@ -898,7 +918,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
         uint32_t w[4 + kSbCols];
 #pragma unroll
         for (int i = 0; i < 4 + kSbCols; ++i) {  // row 32 i + lane of A's, then of B's
-          if constexpr (KIND == F8_GATED) {
+          if constexpr (f8_gated(KIND)) {
             w[i] = f8_gated_scales<NT>(g, t, kg, i, lane);
           } else {
             const bool in_a = i < 4;
@@ -946,7 +966,7 @@ __global__ void __launch_bounds__(kF8Threads, 1)
     else if (g.part == 64) f8_gated_join<2>(g, reinterpret_cast<const float *>(ops));
     else f8_gated_join<1>(g, reinterpret_cast<const float *>(ops));
     __syncthreads();
-  } else if constexpr (!PAIR && KIND != F8_GATED) {
+  } else if constexpr (!PAIR && !f8_gated(KIND)) {
     if (g.splits > 1) {
       cluster_sync();  // the tile's parts are in the shared memory of the cluster
       f8_join<NT>(g, first, reinterpret_cast<const float *>(ops));
@@ -1007,24 +1027,26 @@ template <int NT, int ACCS, bool PAIR, bool FOLD, int KIND>
 static fqt_status launch_f8_as(const typename F8Of<KIND>::Maps &maps,
                                typename F8Of<KIND>::Args &g, int nsm, cudaStream_t st) {
   constexpr size_t stage = kTileBytes + (PAIR ? NT / 2 : NT) * kF8Block;
-  constexpr bool wide_gated = KIND == F8_GATED && NT == 256;
-  size_t boxes = NT >= 64 ? kF8EpiWarps * kF8BoxBytes : 0;
-  if constexpr (wide_gated) boxes = boxes * g.boxes_each + kF8TopBytes;
-  constexpr size_t most_smem = 227 * 1024;
-  const size_t room = most_smem - 1024 - kF8Fixed - boxes;
-  g.stages = (int)std::min<size_t>(room / stage, kMaxStages);
-  const size_t smem = 1024 + kF8Fixed + g.stages * stage + boxes;
+  constexpr int warps = kF8EpiOf<NT, KIND>;
+  // the epilogue's boxes, and a gated block's maxima
+  constexpr size_t boxes = f8_gated_with_codes(KIND) && NT == 256 ? 4 * kF8QuadBoxes + kF8TopBytes
+                           : NT >= 64                    ? warps * kF8BoxBytes
+                                                         : 0;
+  constexpr size_t room = 227 * 1024 - 1024 - kF8Fixed - boxes;
+  constexpr int stages = room / stage < kMaxStages ? (int)(room / stage) : kMaxStages;
+  constexpr size_t smem = 1024 + kF8Fixed + stages * stage + boxes;
+  g.stages = stages;
   auto kernel = k_f8_mm<NT, ACCS, PAIR, FOLD, KIND>;
   static DeviceOnce once;
-  cudaError_t e = allow_smem(kernel, wide_gated ? most_smem : smem, once);
+  cudaError_t e = allow_smem(kernel, smem, once);
   if (e != cudaSuccess) return cuda_fail(e, "FP8 product attribute");
   const int64_t ctas = g.items * (PAIR ? 2 : 1);
   const int most = PAIR ? nsm & ~1 : nsm;
   cudaLaunchConfig_t cfg = {};
   // (few tokens of a gated block: a CTA joins the sums of one item)
-  constexpr bool all = KIND == F8_GATED && NT <= 64;
+  constexpr bool all = f8_gated(KIND) && NT <= 64;
   cfg.gridDim = dim3((unsigned)(all || ctas < most ? ctas : most));
-  cfg.blockDim = dim3(kF8Threads);
+  cfg.blockDim = dim3(32 * (kF8Epi0 + warps));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
@@ -1045,9 +1067,12 @@ template <int NT, int ACCS, bool PAIR, int KIND>
 static fqt_status launch_f8(const typename F8Of<KIND>::Maps &maps, typename F8Of<KIND>::Args &g,
                             int nsm, cudaStream_t st) {
   g.chunk = g.bf16 ? kF8ChunkBf16 : kF8Chunk;
-  if (g.kb_per > g.chunk)
+  if constexpr (f8_gated_with_codes(KIND) && NT == 256) {
     return launch_f8_as<NT, ACCS, PAIR, true, KIND>(maps, g, nsm, st);
-  return launch_f8_as<NT, ACCS, PAIR, false, KIND>(maps, g, nsm, st);
+  } else {
+    if (g.kb_per > g.chunk) return launch_f8_as<NT, ACCS, PAIR, true, KIND>(maps, g, nsm, st);
+    return launch_f8_as<NT, ACCS, PAIR, false, KIND>(maps, g, nsm, st);
+  }
 }
 
 static bool f8_aligned(const void *p, size_t n) {

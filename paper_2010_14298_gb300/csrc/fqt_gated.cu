@@ -4,17 +4,9 @@
 
 namespace fqt {
 
-static bool make_map_f8_codes_out(CUtensorMap *m, const fqt_fp8 *q) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[2] = {(cuuint64_t)q->cols, (cuuint64_t)q->rows};
-  cuuint64_t strides[1] = {(cuuint64_t)q->pitch};
-  cuuint32_t box[2] = {64, 32};
-  cuuint32_t one[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, q->codes, dims, strides, box, one,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
-            CU_TENSOR_MAP_L2_PROMOTION_NONE,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+// Codes that leave in boxes of 32 rows x 128.
+static bool make_map_codes_out(CUtensorMap *m, const fqt_fp8 *q) {
+  return make_map_codes(m, q, 32);
 }
 
 static fqt_status fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fqt_fp8 *Bu,
@@ -36,7 +28,6 @@ static fqt_status fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fq
   g.up = codes_of(up);
   g.sp = scale_rows(M);
   g.splits = 1;
-  g.boxes_each = q || gate || up ? 2 : 1;
   const fqt_fp8 *w = Bg;
   g.s2 = reinterpret_cast<const uint32_t *>(Bu->scales);
   F8Of<F8_GATED>::Maps maps = {};
@@ -81,13 +72,20 @@ static fqt_status fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fq
             g.ldo < ((int64_t)1 << 40) / es;
   if (!make_map_codes(&maps.a, A, BM) || !make_map_codes(&maps.b, Bg, BM) ||
       !make_map_codes(&maps.b2, Bu, BM) ||
-      (g.boxes && !make_map_f8_out(&maps.out, out, bf16, M, N, g.ldo)) ||
-      (q && !make_map_f8_codes_out(&maps.q, q)) ||
-      (gate && !make_map_f8_codes_out(&maps.gate, gate)) ||
-      (up && !make_map_f8_codes_out(&maps.up, up)))
+      (g.boxes && !make_map_f8_out(&maps.out, out, bf16, M, N, g.ldo)))
     return cuda_fail(cudaErrorUnknown, "FP8 tensor map");
-  if (pair) return launch_f8<256, 1, true, F8_GATED>(maps, g, nsm, st);
-  return launch_f8<256, 1, false, F8_GATED>(maps, g, nsm, st);
+  if (q || gate || up) {
+    if ((q && !make_map_codes_out(&maps.q, q)) || (gate && !make_map_codes_out(&maps.gate, gate)) ||
+        (up && !make_map_codes_out(&maps.up, up)))
+      return cuda_fail(cudaErrorUnknown, "FP8 tensor map");
+    if (out)
+      return pair ? launch_f8<256, 1, true, F8_GATED_BOTH>(maps, g, nsm, st)
+                  : launch_f8<256, 1, false, F8_GATED_BOTH>(maps, g, nsm, st);
+    return pair ? launch_f8<256, 1, true, F8_GATED>(maps, g, nsm, st)
+                : launch_f8<256, 1, false, F8_GATED>(maps, g, nsm, st);
+  }
+  return pair ? launch_f8<256, 1, true, F8_GATED_DENSE>(maps, g, nsm, st)
+              : launch_f8<256, 1, false, F8_GATED_DENSE>(maps, g, nsm, st);
 }
 
 }  // namespace fqt

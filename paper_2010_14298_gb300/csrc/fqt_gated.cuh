@@ -256,41 +256,30 @@ __device__ __forceinline__ uint32_t f8_codes4(const uint32_t *v, float inv) {
   return f8_four(y[0], y[1], y[2], y[3]);
 }
 
-// 64 columns of a warp's 32 rows as codes, by way of its box and TMA.
+// A lane's 32 codes of its row (part h of the block's 128) in a box of 32 rows of 128 bytes with
+// the 128-byte swizzle: no bank conflicts.
 template <bool ODD>
-__device__ __forceinline__ void f8_box_codes(float *box, int lane, const uint32_t *v, float inv) {
+__device__ __forceinline__ void f8_box_codes(uint8_t *box, int lane, int h, const uint32_t *v,
+                                             float inv) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    *reinterpret_cast<uint4 *>(box + box_off(lane, k) / 4) =
+  for (int k = 0; k < 2; ++k)
+    *reinterpret_cast<uint4 *>(box + lane * 128 + (((2 * h + k) ^ (lane & 7)) << 4)) =
         make_uint4(f8_codes4<ODD>(v + 16 * k, inv), f8_codes4<ODD>(v + 16 * k + 4, inv),
                    f8_codes4<ODD>(v + 16 * k + 8, inv), f8_codes4<ODD>(v + 16 * k + 12, inv));
 }
-
-__device__ __forceinline__ void f8_store_codes(const CUtensorMap *map, float *&box, float *&spare,
-                                               int lane, int64_t m0, int64_t n, const uint32_t *v,
-                                               float inv, bool odd) {
-  if (lane == 0) bulk_wait_read(1);  // all but the last store, from the other box, have read theirs
-  __syncwarp();
-  if (__any_sync(0xffffffffu, odd)) f8_box_codes<true>(box, lane, v, inv);
-  else f8_box_codes<false>(box, lane, v, inv);
-  fence_proxy_async_smem();
-  __syncwarp();
-  if (lane == 0) {
-    tma_store_2d(map, (int32_t)n, (int32_t)m0, box);
-    bulk_commit();
-  }
-  float *const used = box;
-  box = spare;
-  spare = used;
+__device__ __forceinline__ void f8_put_box(uint8_t *box, int lane, int h, const uint32_t *v,
+                                           float inv, bool odd) {
+  if (__any_sync(0xffffffffu, odd)) f8_box_codes<true>(box, lane, h, v, inv);
+  else f8_box_codes<false>(box, lane, h, v, inv);
 }
 
-// A barrier of the two warps that hold a quadrant's rows; true if either says so.
-__device__ __forceinline__ bool f8_either(int quadrant, bool mine) {
+// A barrier of the four warps that hold a quadrant's rows; true if any says so.
+__device__ __forceinline__ bool f8_any(int quadrant, bool mine) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %2, 0;\n\t"
-      "barrier.cta.red.or.pred q, %1, 64, p;\n\t"
+      "barrier.cta.red.or.pred q, %1, 128, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
       : "r"(quadrant + 1), "r"((uint32_t)mine)
@@ -298,130 +287,223 @@ __device__ __forceinline__ bool f8_either(int quadrant, bool mine) {
   return r != 0;
 }
 
-// One super tile's (or tile's) accumulator holds g in its first 128 columns and u in the
-// others, for the same 128 hidden columns.  A warp takes 64 columns of both for its 32 rows
-// (a lane a row), so a is formed in registers, and a row's block of 128 is two lanes' 64,
-// which exchange their maxima through shared memory.  g and u leave first, then a takes g's
-// registers.  Both warps of a quadrant leave the loop together, whatever made one of them
-// stop: they meet at named barriers.
-template <int ACCS, bool PAIR, bool FOLD>
-__device__ __forceinline__ void f8_gated_epilogue(const F8Of<F8_GATED>::Maps &maps,
-                                                  const F8GatedArgs &g, uint32_t tmem,
-                                                  uint64_t *accf, uint64_t *acce,
-                                                  volatile int *abort_flag, float *box,
-                                                  uint32_t *tops, int q, int h, int lane,
-                                                  int64_t first, int64_t step) {
-  constexpr int NT = 256;
-  const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 64);
-  const bool keeps = g.gate.codes || g.up.codes, codes = keeps || g.q.codes;
-  // of a row's halves: tops[(tensor * 2 + half) * 128 + row]
-  float *spare = box + (g.boxes_each - 1) * (kF8BoxBytes / 4);
-  uint32_t *mine = tops + h * 128 + q * 32 + lane, *other = tops + (1 - h) * 128 + q * 32 + lane;
-  uint32_t c = 0;
-  for (int64_t it = first; it < g.items; it += step) {
-    if (codes ? f8_either(q, *abort_flag) : *abort_flag) break;
-    const F8Item t = f8_item<NT, PAIR>(g, it);
-    uint32_t v[4][32];  // 64 columns of g, 64 of u
-    bool ok = true;
-    if constexpr (FOLD)
+// The scale of a block of 128 columns from its four warps' maxima.
+__device__ __forceinline__ uint32_t f8_block_scale(const uint32_t *tops, float &inv) {
+  return f8_scale(max(max(tops[0], tops[BM]), max(tops[2 * BM], tops[3 * BM])), inv);
+}
+
+// A tile's sums of this warp's CW columns of g and of u, when they are there; false if they do
+// not come.  The accumulator is handed back.
+template <int CW, int ACCS, bool PAIR, bool FOLD>
+__device__ __forceinline__ bool f8_gated_sums(const F8GatedArgs &g, const F8Item &t,
+                                              uint32_t lane_base, uint64_t *accf, uint64_t *acce,
+                                              volatile int *abort_flag, int lane, uint32_t &c,
+                                              uint32_t (&v)[CW], uint32_t (&w)[CW]) {
+  if constexpr (FOLD)
 #pragma unroll
-      for (int i = 0; i < 128; ++i) v[i / 32][i % 32] = 0u;
-    for (int kb = t.kb0; kb < t.kb1; kb = FOLD ? kb + g.chunk : t.kb1, ++c) {
-      const int buf = c % ACCS;
-      if (!f8_wait(&accf[buf], (c / ACCS) & 1u, g.status)) {
-        *abort_flag = 1;
-        ok = false;
-        break;
+    for (int i = 0; i < CW; ++i) v[i] = w[i] = 0u;
+  for (int kb = t.kb0; kb < t.kb1; kb = FOLD ? kb + g.chunk : t.kb1, ++c) {
+    const int buf = c % ACCS;
+    if (!f8_wait(&accf[buf], (c / ACCS) & 1u, g.status)) {
+      *abort_flag = 1;
+      return false;
+    }
+    tc_fence_after();
+    const uint32_t from = lane_base + (uint32_t)(buf * 256);
+    if constexpr (!FOLD) {
+#pragma unroll
+      for (int j = 0; j < CW; j += 32) {
+        tmem_ld32_nw(from + j, *reinterpret_cast<uint32_t(*)[32]>(v + j));
+        tmem_ld32_nw(from + 128 + j, *reinterpret_cast<uint32_t(*)[32]>(w + j));
       }
-      tc_fence_after();
-      const uint32_t from = lane_base + (uint32_t)(buf * NT);
-      if constexpr (!FOLD) {
 #pragma unroll
-        for (int p = 0; p < 4; ++p) tmem_ld32_nw(from + (p >> 1) * 128 + (p & 1) * 32, v[p]);
+      for (int j = 0; j < CW; j += 32) {
+        tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(v + j));
+        tmem_wait_ld(*reinterpret_cast<uint32_t(*)[32]>(w + j));
+      }
+    } else {
 #pragma unroll
-        for (int p = 0; p < 4; ++p) tmem_wait_ld(v[p]);
-      } else {
+      for (int j = 0; j < 2 * CW; j += 16) {  // 16 columns at a time: registers
+        uint32_t r[16];
+        tmem_ld16_nw(from + (j < CW ? j : 128 + j - CW), r);
+        tmem_wait_ld(r);
 #pragma unroll
-        for (int j = 0; j < 128; j += 16) {  // 16 columns at a time: registers
-          uint32_t r[16];
-          tmem_ld16_nw(from + (j >> 6) * 128 + (j & 63), r);
-          tmem_wait_ld(r);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            uint32_t &x = v[j / 32][j % 32 + i];
-            x = __float_as_uint(__uint_as_float(x) + __uint_as_float(r[i]));
-          }
+        for (int i = 0; i < 16; ++i) {
+          uint32_t &x = j < CW ? v[j + i] : w[j - CW + i];
+          x = __float_as_uint(__uint_as_float(x) + __uint_as_float(r[i]));
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) f8_release<PAIR>(&acce[buf]);
     }
-    const int64_t m0 = t.m0 + q * 32, n0 = t.n0 / 2, n = n0 + h * 64;
-    const bool row = m0 + lane < g.M;
-    bool odd_g = false, odd_u = false, odd_a = false;
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) f8_release<PAIR>(&acce[buf]);
+  }
+  return true;
+}
+
+// v = act(v) w
+template <int CW>
+__device__ __forceinline__ void f8_form(int act, uint32_t (&v)[CW], const uint32_t (&w)[CW]) {
+  with_act(act, [&](auto a) {
+#pragma unroll
+    for (int i = 0; i < CW; i += 2) {
+      float x, y;
+      unpack2(mul2(act2<a.value>(pack2(__uint_as_float(v[i]), __uint_as_float(v[i + 1]))),
+                   pack2(__uint_as_float(w[i]), __uint_as_float(w[i + 1]))),
+              x, y);
+      v[i] = __float_as_uint(x), v[i + 1] = __float_as_uint(y);
+    }
+  });
+}
+
+// A warp's 32 rows x CW columns of the dense output, by way of its box.
+template <int CW>
+__device__ __forceinline__ void f8_put_dense(const F8Of<F8_GATED>::Maps &maps, const F8GatedArgs &g,
+                                             float *box, int lane, int64_t m0, int64_t n,
+                                             const uint32_t (&v)[CW]) {
+#pragma unroll
+  for (int j = 0; j < CW; j += 32) {
+    const auto &x = *reinterpret_cast<const uint32_t(*)[32]>(v + j);
+    if (g.boxes && g.bf16)
+      f8_store_box<__nv_bfloat16>(g, &maps.out, box, lane, m0, n + j, x);
+    else if (g.boxes)
+      f8_store_box<float>(g, &maps.out, box, lane, m0, n + j, x);
+    else if (g.bf16)
+      f8_store_rows<__nv_bfloat16>(g, static_cast<__nv_bfloat16 *>(g.out), g.ldo, box, lane, m0,
+                                   n + j, x);
+    else
+      f8_store_rows<float>(g, static_cast<float *>(g.out), g.ldo, box, lane, m0, n + j, x);
+  }
+}
+
+// One super tile's (or tile's) accumulator holds g in its first 128 columns and u in the
+// others, for the same 128 hidden columns.  A warp takes 64 columns of both for its 32 rows (a
+// lane a row), so a is formed in registers.  This one is for a dense output alone: its fewer
+// warps hand the accumulator back sooner than 16 (8192 x 4096 x 1024: 47 us and 54).
+template <int ACCS, bool PAIR, bool FOLD>
+__device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
+                                               const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
+                                               uint64_t *acce, volatile int *abort_flag, float *box,
+                                               int q, int h, int lane, int64_t first,
+                                               int64_t step) {
+  uint32_t c = 0;
+  for (int64_t it = first; it < g.items && !*abort_flag; it += step) {
+    const F8Item t = f8_item<256, PAIR>(g, it);
+    uint32_t v[64], w[64];  // g (then a) and u
+    if (!f8_gated_sums<64, ACCS, PAIR, FOLD>(
+            g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 64), accf, acce, abort_flag,
+            lane, c, v, w))
+      break;
+    f8_form<64>(g.act, v, w);
+    f8_put_dense<64>(maps, g, box, lane, t.m0 + q * 32, t.n0 / 2 + h * 64, v);
+  }
+  if (lane == 0) bulk_wait_all();
+}
+
+// With codes among the outputs a warp takes 32 columns, and a row's block of 128 is four
+// lanes', which exchange their maxima through shared memory: g and u leave first, then a takes
+// g's registers.  Codes leave by TMA in boxes of 32 rows x 128 bytes that a quadrant's four
+// warps fill (boxes of a warp's own 32 bytes a row: three kinds of codes of 8192 x 4096 x 1024
+// 68 us; straight from registers 90).  The warps meet at named barriers, for
+// the maxima: what is in a box by then leaves after it, so a's codes leave in the next round.
+// DENSE: a leaves densely as well.  Registers decide here (96 a thread): sums that are taken 16
+// columns at a time, as if they were to be added to others, leave the compiler more of them
+// than all at once (61 us and 73), and so do kernels without the dense output's code.
+// Whatever makes one of the warps stop, all four leave the loop at the same barrier.
+template <int ACCS, bool PAIR, bool DENSE>
+__device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
+                                               const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
+                                               uint64_t *acce, volatile int *abort_flag,
+                                               uint8_t *boxes, uint32_t *tops, int q, int h,
+                                               int lane, int64_t first, int64_t step) {
+  const bool keeps = g.gate.codes || g.up.codes, makes = g.q.codes, leads = h == 0 && lane == 0;
+  boxes += q * kF8QuadBoxes;
+  // a warp's box of a dense output, where those of g and u have been
+  [[maybe_unused]] float *dense = reinterpret_cast<float *>(boxes + h * kF8BoxBytes);
+  constexpr size_t kBox = kF8QuadBoxes / 3;
+  tops += q * 32 + lane;  // a row's maxima, tops[(slot * 4 + part) * 128]: g's, u's, a's, a's
+  uint32_t c = 0, parity = 0;
+  int32_t q_row = 0, q_col = -1;  // a's codes that have not left
+  uint8_t *q_box = nullptr;
+  bool bad = false;
+  auto send_q = [&]() {
+    if (leads && q_col >= 0 && q_row < g.M) {
+      tma_store_2d(&maps.q, q_col, q_row, q_box);
+      bulk_commit();
+    }
+    q_col = -1;
+  };
+  for (int64_t it = first; it < g.items; it += step, parity ^= 1u) {
+    const F8Item t = f8_item<256, PAIR>(g, it);
+    uint32_t v[32], w[32];  // g (then a) and u
+    const bool ok = f8_gated_sums<32, ACCS, PAIR, true>(
+        g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 32), accf, acce, abort_flag, lane,
+        c, v, w);
+    const int64_t m0 = t.m0 + q * 32, n0 = t.n0 / 2;
+    const bool row = h == 0 && m0 + lane < g.M;
+    const int64_t scale = scale_at(n0 / kF8Block, g.sp, m0 + lane);
+    float inv;
     if (keeps) {
-      const uint32_t mg = f8_top<64>(v[0], odd_g), mu = f8_top<64>(v[2], odd_u);
+      bool odd_g, odd_u;
+      tops[h * BM] = f8_top<32>(v, odd_g);
+      tops[(4 + h) * BM] = f8_top<32>(w, odd_u);
       if ((odd_g && g.gate.codes) || (odd_u && g.up.codes)) record_status(g.status, FQT_ENONFINITE);
-      mine[0] = mg;
-      mine[256] = mu;
-      if (f8_either(q, !ok)) break;
-      float ig, iu;
-      const uint32_t eg = f8_scale(max(mg, other[0]), ig), eu = f8_scale(max(mu, other[256]), iu);
+      if (lane == 0) bulk_wait_read(0);  // what left the boxes of g and u
+      if ((bad = f8_any(q, !ok || *abort_flag))) break;
+      send_q();
       if (g.gate.codes) {
-        if (m0 < g.M && n < g.N)
-          f8_store_codes(&maps.gate, box, spare, lane, m0, n, v[0], ig, odd_g);
-        if (row && h == 0) g.gate.scales[scale_at(n0 / kF8Block, g.sp, m0 + lane)] = (uint8_t)eg;
+        const uint32_t e = f8_block_scale(tops, inv);
+        f8_put_box(boxes, lane, h, v, inv, odd_g);
+        if (row) g.gate.scales[scale] = (uint8_t)e;
       }
       if (g.up.codes) {
-        if (m0 < g.M && n < g.N)
-          f8_store_codes(&maps.up, box, spare, lane, m0, n, v[2], iu, odd_u);
-        if (row && h == 0) g.up.scales[scale_at(n0 / kF8Block, g.sp, m0 + lane)] = (uint8_t)eu;
+        const uint32_t e = f8_block_scale(tops + 4 * BM, inv);
+        f8_put_box(boxes + kBox, lane, h, w, inv, odd_u);
+        if (row) g.up.scales[scale] = (uint8_t)e;
+      }
+      fence_proxy_async_smem();
+    }
+    f8_form<32>(g.act, v, w);
+    // (two slots in turn: without g and u there is one barrier a round)
+    uint32_t *top_a = tops + (8 + (keeps ? 0 : 4 * parity)) * BM;
+    bool odd = false;
+    if (makes) {
+      top_a[h * BM] = f8_top<32>(v, odd);
+      if (odd) record_status(g.status, FQT_ENONFINITE);
+    }
+    if (lane == 0) bulk_wait_read(0);  // what left a's box
+    if ((bad = f8_any(q, !ok || *abort_flag))) break;
+    if (!keeps) send_q();
+    if (keeps && leads && m0 < g.M) {
+      if (g.gate.codes) tma_store_2d(&maps.gate, (int32_t)n0, (int32_t)m0, boxes);
+      if (g.up.codes) tma_store_2d(&maps.up, (int32_t)n0, (int32_t)m0, boxes + kBox);
+      bulk_commit();
+    }
+    if constexpr (DENSE) {
+      if (keeps) {  // not before they have left
+        if (leads) bulk_wait_read(0);
+        f8_any(q, false);
+      }
+      f8_put_dense<32>(maps, g, dense, lane, m0, n0 + h * 32, v);
+    }
+    if (makes) {
+      // (alone, two boxes in turn: one may be leaving)
+      q_box = boxes + (keeps || DENSE || parity ? 2 : 0) * kBox;
+      q_row = (int32_t)m0;
+      q_col = (int32_t)n0;
+      const uint32_t e = f8_block_scale(top_a, inv);
+      f8_put_box(q_box, lane, h, v, inv, odd);
+      if (row) g.q.scales[scale] = (uint8_t)e;
+      fence_proxy_async_smem();
+      if (DENSE && !keeps) {
+        f8_any(q, false);
+        send_q();
       }
     }
-    if (!codes && !ok) break;
-    with_act(g.act, [&](auto act) {
-#pragma unroll
-      for (int i = 0; i < 64; i += 2) {
-        uint32_t *x = &v[i / 32][i % 32], *y = &v[2 + i / 32][i % 32];
-        float p, q;
-        unpack2(mul2(act2<act.value>(pack2(__uint_as_float(x[0]), __uint_as_float(x[1]))),
-                     pack2(__uint_as_float(y[0]), __uint_as_float(y[1]))),
-                p, q);
-        x[0] = __float_as_uint(p), x[1] = __float_as_uint(q);
-      }
-    });
-    if (g.out && ok) {
-      if (!g.boxes && lane == 0) bulk_wait_read(0);  // (the box is written without asking)
-      float *fp32 = static_cast<float *>(g.out);
-      __nv_bfloat16 *bf16 = static_cast<__nv_bfloat16 *>(g.out);
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int64_t np = n + 32 * p;
-        if (g.boxes && g.bf16)
-          f8_store_box<__nv_bfloat16>(g, &maps.out, box, lane, m0, np, v[p]);
-        else if (g.boxes)
-          f8_store_box<float>(g, &maps.out, box, lane, m0, np, v[p]);
-        else if (g.bf16)
-          f8_store_rows<__nv_bfloat16>(g, bf16, g.ldo, box, lane, m0, np, v[p]);
-        else
-          f8_store_rows<float>(g, fp32, g.ldo, box, lane, m0, np, v[p]);
-      }
-      float *const used = box;
-      box = spare;
-      spare = used;
-    }
-    if (g.q.codes) {
-      const uint32_t ma = f8_top<64>(v[0], odd_a);
-      if (odd_a) record_status(g.status, FQT_ENONFINITE);
-      mine[512] = ma;
-      if (f8_either(q, !ok)) break;
-      float ia;
-      const uint32_t ea = f8_scale(max(ma, other[512]), ia);
-      if (m0 < g.M && n < g.N)
-        f8_store_codes(&maps.q, box, spare, lane, m0, n, v[0], ia, odd_a);
-      if (row && h == 0) g.q.scales[scale_at(n0 / kF8Block, g.sp, m0 + lane)] = (uint8_t)ea;
-    }
+  }
+  if (!bad && makes) {
+    f8_any(q, false);
+    send_q();
   }
   if (lane == 0) bulk_wait_all();
 }

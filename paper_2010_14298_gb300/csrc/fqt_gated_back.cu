@@ -14,7 +14,7 @@ struct F8BackArgs {
   void *dgate, *dup;
   int64_t lddg, lddu;
   F8Codes q[2], qt[3];  // dg, du; their transposes and a's
-  int64_t row_tiles, tiles;
+  int row_tiles, tiles;  // (rows and columns pass 2^22 by no more than a tile, tiles 2^30)
   int *status;
 };
 
@@ -177,6 +177,17 @@ struct F8BackMaps {
   CUtensorMap da, gate, up;
 };
 
+__device__ __forceinline__ float half_of(f32x2 v, int i) {
+  float x, y;
+  unpack2(v, x, y);
+  return i ? y : x;
+}
+// Its magnitude, 0 if it is no finite number.
+__device__ __forceinline__ float finite_of(f32x2 v, int i) {
+  const float x = half_of(v, i);
+  return is_odd(x) ? 0.0f : fabsf(x);
+}
+
 // Bytes (a multiple of 16, both ends on 16) into shared memory, counted by a barrier.
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes,
                                           uint64_t *bar) {
@@ -189,27 +200,31 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
 
 template <typename T>
 __device__ __forceinline__ void back_fetch(const F8BackMaps &maps, const F8BackArgs &a,
-                                           F8BackShared<T> &s, int stage, int64_t tile, bool vec) {
-  const int64_t ct = tile / a.row_tiles, rt = tile - ct * a.row_tiles;
+                                           F8BackShared<T> &s, int stage, int tile, bool vec) {
+  const int ct = tile / a.row_tiles, rt = tile - ct * a.row_tiles;
   auto &in = s.in[stage];
   uint64_t *bar = &s.full[stage];
   mbar_expect_tx(bar, (uint32_t)((vec ? sizeof(in.da) : 0) + sizeof(in.gate) + sizeof(in.up) +
                                  sizeof(in.sg) + sizeof(in.su)));
-  const int32_t r0 = (int32_t)(rt * kF8Block), c0 = (int32_t)(ct * kF8Block);
+  const int r0 = rt * kF8Block, c0 = ct * kF8Block;
   if (vec) tma_load_2d(in.da, &maps.da, c0, r0, bar);
   tma_load_2d(in.gate, &maps.gate, c0, r0, bar);
   tma_load_2d(in.up, &maps.up, c0, r0, bar);
-  const int64_t at = ((ct >> 2) * a.sp + r0) * 4;
+  const int64_t at = ((int64_t)(ct >> 2) * a.sp + r0) * 4;
   bulk_load(in.sg, a.gate.scales + at, sizeof(in.sg), bar);
   bulk_load(in.su, a.up.scales + at, sizeof(in.su), bar);
 }
 
-template <typename T, int ACT>
+// ALL: the five matrices of codes, and no dense output (what a training step asks for).
+template <typename T, int ACT, bool ALL>
 __global__ void __launch_bounds__(kF8BackThreads, 1)
     k_f8_gated_back(const __grid_constant__ F8BackMaps maps, const F8BackArgs a, const bool vec) {
   extern __shared__ __align__(1024) uint8_t raw[];
   F8BackShared<T> &s = *reinterpret_cast<F8BackShared<T> *>(raw);
   constexpr int S = F8BackShared<T>::stages;
+  // which outputs there are
+  auto has_q = [&](int k) { return ALL || a.q[k].codes; };
+  auto has_qt = [&](int k) { return ALL || a.qt[k].codes; };
   let_next_start();
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   if (t == 0) {
@@ -220,22 +235,22 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
   wait_for_previous();
   if (t == 0)
     for (int i = 0; i < S; ++i)
-      if (blockIdx.x + (int64_t)i * gridDim.x < a.tiles)
-        back_fetch(maps, a, s, i, blockIdx.x + (int64_t)i * gridDim.x, vec);
+      if ((int)(blockIdx.x + i * gridDim.x) < a.tiles)
+        back_fetch(maps, a, s, i, (int)(blockIdx.x + i * gridDim.x), vec);
   int n = 0;
   bool ok = true;
-  for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++n) {
-    const int64_t ct = tile / a.row_tiles, rt = tile - ct * a.row_tiles;
-    const int64_t r0 = rt * kF8Block, c0 = ct * kF8Block;
-    const int64_t row = r0 + warp * 8, col = c0 + lane * 4;
-    const int rows = (int)min((int64_t)8, a.rows - row);  // of the warp's (it may have none)
+  for (int tile = (int)blockIdx.x; tile < a.tiles; tile += (int)gridDim.x, ++n) {
+    const int ct = tile / a.row_tiles, rt = tile - ct * a.row_tiles;
+    const int r0 = rt * kF8Block, c0 = ct * kF8Block;
+    const int row = r0 + warp * 8, col = c0 + lane * 4;
+    const int rows = min(8, (int)a.rows - row);  // of the warp's (it may have none)
     auto &in = s.in[n % S];
     if (!vec) {  // the warp's 8 rows, entry by entry, but neighbouring lanes read neighbours
       T e[8][kF8Block / 32];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int64_t r = r0 + warp * 8 + i;
-        f8_fetch<T, kF8Block>(e[i], static_cast<const T *>(a.da) + r * a.ldda + c0,
+        const int r = row + i;
+        f8_fetch<T, kF8Block>(e[i], static_cast<const T *>(a.da) + (int64_t)r * a.ldda + c0,
                               r < a.rows ? a.cols - c0 : 0, lane);
       }
 #pragma unroll
@@ -285,7 +300,7 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       T *out = static_cast<T *>(k ? a.dup : a.dgate);
-      if (!out) continue;
+      if (ALL || !out) continue;
       const int64_t ld = k ? a.lddu : a.lddg;
       const bool wide = f8_pitch_aligned<T>(out, ld) && col + 4 <= a.cols;
 #pragma unroll
@@ -294,7 +309,7 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
         float x[4];
         unpack2(v[k][i][0], x[0], x[1]);
         unpack2(v[k][i][1], x[2], x[3]);
-        T *p = out + (row + i) * ld + col;
+        T *p = out + (int64_t)(row + i) * ld + col;
         if (wide && sizeof(T) == 4) {
           *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
         } else if (wide) {
@@ -309,11 +324,13 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
         }
       }
     }
-    // Column maxima.  Entries that are not finite count for none and become NaN, whose code
-    // is NaN's.
+    // Column maxima.  Entries that are not finite count for none; infinities' codes are put
+    // right where they are written (v changes for none of this: the copies that the compiler
+    // kept for two ways through cost 80 bytes of spilled registers).
+    bool odd[3] = {false, false, false};
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      if (!a.qt[k].codes && (k == 2 || !a.q[k].codes)) continue;
+      if (!has_qt(k) && (k == 2 || !has_q(k < 2 ? k : 0))) continue;
       float cm[4];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -323,36 +340,32 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
         cm[2 * j] = top3(top3(top3(x[0], x[1], x[2]), x[3], x[4]), top3(x[5], x[6], x[7]), 0.0f);
         cm[2 * j + 1] = top3(top3(top3(y[0], y[1], y[2]), y[3], y[4]), top3(y[5], y[6], y[7]), 0.0f);
       }
-      if (is_odd(top3(top3(cm[0], cm[1], cm[2]), cm[3], 0.0f))) {
+      odd[k] = is_odd(top3(top3(cm[0], cm[1], cm[2]), cm[3], 0.0f));
+      if (odd[k]) {
         record_status(a.status, FQT_ENONFINITE);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          cm[2 * j] = cm[2 * j + 1] = 0.0f;
+        for (int j = 0; j < 4; ++j) {
+          cm[j] = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float x[2];
-            unpack2(v[k][i][j], x[0], x[1]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (is_odd(x[h])) x[h] = __uint_as_float(0x7FFFFFFFu);
-              else cm[2 * j + h] = fmaxf(cm[2 * j + h], fabsf(x[h]));
-            }
-            v[k][i][j] = pack2(x[0], x[1]);
-          }
+          for (int i = 0; i < 8; ++i) cm[j] = fmaxf(cm[j], finite_of(v[k][i][j / 2], j % 2));
         }
       }
       *reinterpret_cast<float4 *>(&s.top[k][warp][lane * 4]) =
           make_float4(cm[0], cm[1], cm[2], cm[3]);
     }
-    // row maxima (of what are numbers now): lane c keeps row c % 8 of tensor c / 8
-    if (a.q[0].codes || a.q[1].codes) {
+    // row maxima: lane c keeps row c % 8 of tensor c / 8
+    if (has_q(0) || has_q(1)) {
       uint32_t mine = 0u;
 #pragma unroll
       for (int c = 0; c < 16; ++c) {
-        float x[4];
-        unpack2(v[c / 8][c % 8][0], x[0], x[1]);
-        unpack2(v[c / 8][c % 8][1], x[2], x[3]);
-        const float m = top3_number(top3_number(x[0], x[1], x[2]), x[3], 0.0f);
+        const f32x2(&x)[2] = v[c / 8][c % 8];
+        float e[4], m;
+        unpack2(x[0], e[0], e[1]);
+        unpack2(x[1], e[2], e[3]);
+        m = top3(top3(e[0], e[1], e[2]), e[3], 0.0f);
+        if (odd[c / 8])
+          m = top3(top3(finite_of(x[0], 0), finite_of(x[0], 1), finite_of(x[1], 0)),
+                   finite_of(x[1], 1), 0.0f);
         const uint32_t r = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
         if (lane == c) mine = r;
       }
@@ -362,9 +375,9 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
     // the scales: three quarters of the threads a column of one tensor each, the others two
     // rows; one of the others also asks for the next tile, as everybody has read this one's
     // stage
-    if (t == kF8BackThreads - 1 && tile + (int64_t)S * gridDim.x < a.tiles)
-      back_fetch(maps, a, s, n % S, tile + (int64_t)S * gridDim.x, vec);
-    if (t < 3 * kF8Block && a.qt[t / kF8Block].codes) {
+    if (t == kF8BackThreads - 1 && tile + S * (int)gridDim.x < a.tiles)
+      back_fetch(maps, a, s, n % S, tile + S * (int)gridDim.x, vec);
+    if (t < 3 * kF8Block && has_qt(t / kF8Block)) {
       const int k = t / kF8Block, j = t % kF8Block;
       float m = 0.0f;
 #pragma unroll
@@ -376,7 +389,7 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int r = t - 3 * kF8Block;  // of the tile's
-        if (!a.q[k].codes) continue;
+        if (!has_q(k)) continue;
         const uint32_t e = f8_scale(s.row_top[r / 8][k * 8 + r % 8], s.row_inv[r / 8][k * 8 + r % 8]);
         if (r0 + r < a.rows) a.q[k].scales[scale_at(ct, a.sp, r0 + r)] = (uint8_t)e;
       }
@@ -386,7 +399,7 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
 #pragma unroll
     for (int kk = 0; kk < 3; ++kk) {
       const int k = 2 - kk;  // a first, which has no rows
-      if (a.qt[k].codes) {
+      if (has_qt(k)) {
         const float4 f = *reinterpret_cast<const float4 *>(&s.inv[k][lane * 4]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -399,29 +412,41 @@ __global__ void __launch_bounds__(kF8BackThreads, 1)
           s.tr[k][back_at(lane * 4 + 2 * j + 1, warp)] =
               make_uint2(f8_four(y[0], y[1], y[2], y[3]), f8_four(y[4], y[5], y[6], y[7]));
         }
+        if (odd[k])
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (is_odd(half_of(v[k][i][j / 2], j % 2)))
+                reinterpret_cast<uint8_t *>(&s.tr[k][back_at(lane * 4 + j, warp)])[i] = 0x7Fu;
       }
-      if (k < 2 && a.q[k < 2 ? k : 0].codes) {
+      if (k < 2 && has_q(k < 2 ? k : 0)) {
         const F8Codes &q = a.q[k < 2 ? k : 0];
-        uint8_t *to = q.codes + row * q.pitch + col;
+        uint8_t *to = q.codes + (int64_t)row * q.pitch + col;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const f32x2 f = both(s.row_inv[warp][k * 8 + i]);
           float x[4];
           unpack2(mul2(v[k][i][0], f), x[0], x[1]);
           unpack2(mul2(v[k][i][1], f), x[2], x[3]);
-          if (there && i < rows) *reinterpret_cast<uint32_t *>(to) = f8_four(x[0], x[1], x[2], x[3]);
+          uint32_t code = f8_four(x[0], x[1], x[2], x[3]);
+          if (odd[k])
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (is_odd(half_of(v[k][i][j / 2], j % 2))) code |= 0x7Fu << 8 * j;
+          if (there && i < rows) *reinterpret_cast<uint32_t *>(to) = code;
           to += q.pitch;
         }
       }
     }
-    if (!a.qt[0].codes && !a.qt[1].codes && !a.qt[2].codes) continue;
+    if (!has_qt(0) && !has_qt(1) && !has_qt(2)) continue;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      if (!a.qt[k].codes) continue;
+      if (!has_qt(k)) continue;
       const int j = t >> 3, ch = t & 7;
       const uint2 *from[2] = {&s.tr[k][back_at(j, 2 * ch)], &s.tr[k][back_at(j, 2 * ch + 1)]};
-      uint8_t *to = a.qt[k].codes + (c0 + j) * a.qt[k].pitch + r0 + ch * 16;
+      uint8_t *to = a.qt[k].codes + (int64_t)(c0 + j) * a.qt[k].pitch + r0 + ch * 16;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {  // columns j and j + 64: the same places of their words
         const uint2 lo = from[0][64 * 16 * h], hi = from[1][64 * 16 * h];
@@ -456,9 +481,11 @@ template <typename T, int ACT>
 static fqt_status launch_back(F8BackArgs &a, const fqt_fp8 *gate, const fqt_fp8 *up,
                               cudaStream_t st) {
   const bool vec = f8_pitch_aligned<T>(a.da, a.ldda);
-  bool codes = false;
-  for (const F8Codes &c : a.q) codes |= c.codes != nullptr;
-  for (const F8Codes &c : a.qt) codes |= c.codes != nullptr;
+  bool codes = false, all = !a.dgate && !a.dup;
+  for (const F8Codes &c : {a.q[0], a.q[1], a.qt[0], a.qt[1], a.qt[2]}) {
+    codes |= c.codes != nullptr;
+    all &= c.codes != nullptr;
+  }
   if (!codes) {
     const bool wide = vec && (!a.dgate || f8_pitch_aligned<T>(a.dgate, a.lddg)) &&
                       (!a.dup || f8_pitch_aligned<T>(a.dup, a.lddu));
@@ -479,13 +506,13 @@ static fqt_status launch_back(F8BackArgs &a, const fqt_fp8 *gate, const fqt_fp8 
       (ahead && !make_map_dense(&maps.da, a.da, sizeof(T) == 2, a.rows, a.cols,
                               a.rows > 1 ? a.ldda : (a.cols + 7) / 8 * 8)))
     return cuda_fail(cudaErrorUnknown, "gated backward tensor map");
-  a.row_tiles = (a.rows + kF8Block - 1) / kF8Block;
-  a.tiles = a.row_tiles * (((int64_t)a.cols + kF8Block - 1) / kF8Block);
-  auto kernel = k_f8_gated_back<T, ACT>;
-  static DeviceOnce once;
-  const cudaError_t e = allow_smem(kernel, sizeof(F8BackShared<T>), once);
+  a.row_tiles = (int)((a.rows + kF8Block - 1) / kF8Block);
+  a.tiles = a.row_tiles * ((a.cols + kF8Block - 1) / kF8Block);
+  auto kernel = all ? k_f8_gated_back<T, ACT, true> : k_f8_gated_back<T, ACT, false>;
+  static DeviceOnce once[2];
+  const cudaError_t e = allow_smem(kernel, sizeof(F8BackShared<T>), once[all]);
   if (e != cudaSuccess) return cuda_fail(e, "gated backward attribute");
-  const dim3 grid((unsigned)std::min<int64_t>(a.tiles, device_sm_count()));
+  const dim3 grid((unsigned)std::min(a.tiles, device_sm_count()));
   return cuda_fail(launch_behind(kernel, grid, kF8BackThreads, sizeof(F8BackShared<T>), st, maps,
                                  (const F8BackArgs &)a, ahead),
                    "gated backward launch");

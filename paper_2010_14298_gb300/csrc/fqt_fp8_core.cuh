@@ -255,6 +255,7 @@ struct F8Codes {
 struct F8GatedArgs : F8Args {
   const uint32_t *s2;
   int act, part;
+  int holds;  // CTAs of a cluster that hold a block of 128 columns (few tokens)
   F8Codes q, gate, up;  // outputs as codes, where asked for
   int64_t sp;           // rows of their scales
 };
@@ -409,8 +410,14 @@ __device__ __forceinline__ F8Item f8_item(const F8Args &g, int64_t it) {
 // Few tokens of a gated block: a CTA takes g.part rows of both weights, and all tokens.
 template <int NT, bool PAIR, int KIND, typename A>
 __device__ __forceinline__ F8Item f8_item_of(const A &g, int64_t it) {
-  if constexpr (f8_gated(KIND) && NT <= 64) return F8Item{it * g.part, 0, 0, g.nkb};
-  else return f8_item<NT, PAIR>(g, it);
+  if constexpr (f8_gated(KIND) && NT <= 64) {
+    const int cluster = (int)it / g.splits, r = (int)it - cluster * g.splits, k = r / g.holds;
+    const int kb0 = k * g.kb_per;
+    return F8Item{(int64_t)(cluster * g.holds + r - k * g.holds) * g.part, 0, kb0,
+                  min(g.nkb, kb0 + g.kb_per)};
+  } else {
+    return f8_item<NT, PAIR>(g, it);
+  }
 }
 
 template <typename T>
@@ -576,7 +583,7 @@ template <int ACCS, bool PAIR, bool FOLD>
 __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
                                                const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
                                                uint64_t *acce, volatile int *abort_flag, float *box,
-                                               int q, int h, int lane, int64_t first,
+                                               float *part, int q, int h, int lane, int64_t first,
                                                int64_t step);
 template <int ACCS, bool PAIR, bool DENSE>
 __device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
@@ -584,7 +591,7 @@ __device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
                                                uint64_t *acce, volatile int *abort_flag,
                                                uint8_t *boxes, uint32_t *tops, int q, int h,
                                                int lane, int64_t first, int64_t step);
-template <int W>
+template <int NT>
 __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float *part);
 
 // One CTA per 128 x NT tile (and part of the K blocks), persistent, or a pair of CTAs
@@ -600,7 +607,8 @@ template <int NT, int ACCS, bool PAIR, bool FOLD, int KIND>
 __global__ void __launch_bounds__(32 * (kF8Epi0 + kF8EpiOf<NT, KIND>), 1)
     k_f8_mm(const __grid_constant__ typename F8Of<KIND>::Maps maps,
             const typename F8Of<KIND>::Args g) {
-  constexpr bool kJoins = f8_gated(KIND) && NT <= 64;  // (few tokens)
+  // a gated block's few tokens, or shared K blocks
+  constexpr bool kFew = f8_gated(KIND) && NT <= 64, kJoins = kFew || (KIND == F8_GATED_DENSE && !PAIR);
   // columns of an epilogue warp: a multiple of 32 for the first half's
   constexpr int W0 = NT <= 64 ? NT / 2 : (NT / 2 + 31) / 32 * 32, W1 = NT - W0;
   constexpr int NB = PAIR ? NT / 2 : NT;    // rows of B that this CTA loads
@@ -671,8 +679,9 @@ __global__ void __launch_bounds__(32 * (kF8Epi0 + kF8EpiOf<NT, KIND>), 1)
                                        first, step);
     else if constexpr (KIND == F8_GATED_DENSE && NT == 256)
       f8_gated_dense<ACCS, PAIR, FOLD>(maps, g, tmem, accf, acce, abort_flag,
-                                       reinterpret_cast<float *>(after + e * kF8BoxBytes), warp & 3,
-                                       e >> 2, lane, first, step);
+                                       reinterpret_cast<float *>(after + e * kF8BoxBytes),
+                                       reinterpret_cast<float *>(ops), warp & 3, e >> 2, lane,
+                                       first, step);
   } else if (warp >= kF8Epi0) {
     const int q = warp & 3, h = (warp - kF8Epi0) >> 2;
     const int W = h ? W1 : W0;
@@ -721,7 +730,7 @@ __global__ void __launch_bounds__(32 * (kF8Epi0 + kF8EpiOf<NT, KIND>), 1)
       }
       if (!ok) break;
       if constexpr (!PAIR) {
-        if (kJoins || g.splits > 1) {  // the products are done with the operand stages
+        if (kFew || g.splits > 1) {  // the products are done with the operand stages
           float *part = reinterpret_cast<float *>(ops);
           const int r = q * 32 + lane, j = h * W0;
 #pragma unroll
@@ -961,11 +970,11 @@ __global__ void __launch_bounds__(32 * (kF8Epi0 + kF8EpiOf<NT, KIND>), 1)
   tc_fence_before();
   __syncthreads();
   if constexpr (kJoins) {
-    if (g.splits > 1) cluster_sync();  // (CTAs that share blocks of hidden columns)
-    if (g.splits > 1) f8_gated_join<4>(g, reinterpret_cast<const float *>(ops));
-    else if (g.part == 64) f8_gated_join<2>(g, reinterpret_cast<const float *>(ops));
-    else f8_gated_join<1>(g, reinterpret_cast<const float *>(ops));
-    __syncthreads();
+    if (NT <= 64 || g.splits > 1) {
+      if (g.splits > 1) cluster_sync();
+      f8_gated_join<NT>(g, reinterpret_cast<const float *>(ops));
+      __syncthreads();
+    }
   } else if constexpr (!PAIR && !f8_gated(KIND)) {
     if (g.splits > 1) {
       cluster_sync();  // the tile's parts are in the shared memory of the cluster

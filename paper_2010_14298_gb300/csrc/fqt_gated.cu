@@ -9,6 +9,33 @@ static bool make_map_codes_out(CUtensorMap *m, const fqt_fp8 *q) {
   return make_map_codes(m, q, 32);
 }
 
+// CTAs of a cluster that share the K blocks of each of `ctas` CTAs (which themselves come in
+// clusters of `holds`), of which the estimate is least: a K block takes ns nanoseconds, meeting
+// in shared memory `meet` (which clusters that hold blocks together do anyway), and not all SMs
+// have a place in a large cluster.  Few tokens: 0.22 us and 2.3 (1 x 1024 x 4096 7.5 us shared
+// by four, 11.3 unshared; 1 x 4096 x 1024 6.2 unshared).  Tiles of 128 tokens: 0.4 and 3.5 (128
+// x 1024 x 4096 12.7 shared by eight and 13.7; 300 x 100 x 4000 12.4 and 16.4; 1523 x 336 x 1201
+// 8.9 unshared, 11.0 by three).  Sets the K blocks of one, whole groups of scales.
+static int share_blocks(int64_t ctas, int holds, int nkb, int ns, int meet, int nsm, int *kb_per) {
+  const int groups = (nkb + kF8Group - 1) / kF8Group;
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int splits = 1; splits * holds <= kF8Parts && splits <= groups; ++splits) {
+    const int per = (groups + splits - 1) / splits * kF8Group, cluster = splits * holds;
+    if ((nkb + per - 1) / per != splits) continue;  // as many as another number's
+    const int room = cluster > 4 ? nsm * 3 / 4 : cluster > 2 ? nsm * 7 / 8 : nsm;
+    if (splits > 1 && ctas * splits > room) break;
+    const int64_t rounds = (ctas * splits + nsm - 1) / nsm;
+    const int64_t cost = rounds * std::min(per, nkb) * ns + (splits > 1 && holds == 1 ? meet : 0);
+    if (cost < least) {
+      least = cost;
+      best = splits;
+      *kb_per = per;
+    }
+  }
+  return best;
+}
+
 static fqt_status fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fqt_fp8 *Bu,
                                    fqt_act act, bool bf16, void *out, int64_t ldo,
                                    const fqt_fp8 *q, const fqt_fp8 *gate, const fqt_fp8 *up,
@@ -36,9 +63,11 @@ static fqt_status fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fq
     // 32 columns of each projection to a CTA, 64 where that would be more CTAs than SMs
     g.part = (N + 31) / 32 <= nsm ? 32 : 64;
     // CTAs that hold blocks of 128 columns together
-    if (q || gate || up) g.splits = kF8Block / g.part;
-    const int64_t run = (int64_t)g.part * g.splits;
-    g.items = (N + run - 1) / run * g.splits;
+    g.holds = q || gate || up ? kF8Block / g.part : 1;
+    const int64_t run = (int64_t)g.part * g.holds, runs = (N + run - 1) / run;
+    const int splits = share_blocks(runs * g.holds, g.holds, g.nkb, 220, 2300, nsm, &g.kb_per);
+    g.splits = splits * g.holds;
+    g.items = runs * g.splits;
     g.swap = 1;
     g.sa = reinterpret_cast<const uint32_t *>(w->scales);
     g.sb = reinterpret_cast<const uint32_t *>(A->scales);
@@ -74,6 +103,11 @@ static fqt_status fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fq
       !make_map_codes(&maps.b2, Bu, BM) ||
       (g.boxes && !make_map_f8_out(&maps.out, out, bf16, M, N, g.ldo)))
     return cuda_fail(cudaErrorUnknown, "FP8 tensor map");
+  if (!pair) {
+    g.splits = share_blocks(g.items, 1, g.nkb, 400, 3500, nsm, &g.kb_per);
+    g.items *= g.splits;
+    if (g.splits > 1) return launch_f8<256, 1, false, F8_GATED_DENSE>(maps, g, nsm, st);
+  }
   if (q || gate || up) {
     if ((q && !make_map_codes_out(&maps.q, q)) || (gate && !make_map_codes_out(&maps.gate, gate)) ||
         (up && !make_map_codes_out(&maps.up, up)))

@@ -379,12 +379,13 @@ __device__ __forceinline__ void f8_put_dense(const F8Of<F8_GATED>::Maps &maps, c
 // One super tile's (or tile's) accumulator holds g in its first 128 columns and u in the
 // others, for the same 128 hidden columns.  A warp takes 64 columns of both for its 32 rows (a
 // lane a row), so a is formed in registers.  This one is for a dense output alone: its fewer
-// warps hand the accumulator back sooner than 16 (8192 x 4096 x 1024: 47 us and 54).
+// warps hand the accumulator back sooner than 16 (8192 x 4096 x 1024: 47 us and 54); and for
+// tiles whose K blocks a cluster shares, with any outputs.
 template <int ACCS, bool PAIR, bool FOLD>
 __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
                                                const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
                                                uint64_t *acce, volatile int *abort_flag, float *box,
-                                               int q, int h, int lane, int64_t first,
+                                               float *part, int q, int h, int lane, int64_t first,
                                                int64_t step) {
   uint32_t c = 0;
   for (int64_t it = first; it < g.items && !*abort_flag; it += step) {
@@ -394,6 +395,16 @@ __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
             g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 64), accf, acce, abort_flag,
             lane, c, v, w))
       break;
+    if constexpr (!PAIR)
+      if (g.splits > 1) {  // the products are done with the operand stages
+        float *to = part + (q * 32 + lane) * (256 + 4) + h * 64;
+#pragma unroll
+        for (int i = 0; i < 64; i += 4) {
+          *reinterpret_cast<uint4 *>(to + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+          *reinterpret_cast<uint4 *>(to + 128 + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        }
+        break;
+      }
     f8_form<64>(g.act, v, w);
     f8_put_dense<64>(maps, g, box, lane, t.m0 + q * 32, t.n0 / 2 + h * 64, v);
   }
@@ -525,39 +536,85 @@ __device__ __forceinline__ void f8_remote(const float *p, int cta, uint32_t (&v)
     asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v[0]) : "r"(a) : "memory");
 }
 
-// W consecutive codes of lane's values, whose block (the warp's) has the maximum m.
+// The sums over a cluster's K splits of W consecutive entries at p and at q, in their order
+// (all on their way at once: one after the other, 1523 x 336 x 1201 took 12.4 us).
 template <int W>
+__device__ __forceinline__ void f8_parts(const float *p, const float *q, int cta, int step,
+                                         int splits, uint32_t (&a)[W], uint32_t (&u)[W]) {
+  if (splits == 1) {
+    f8_remote<W>(p, cta, a);
+    f8_remote<W>(q, cta, u);
+    return;
+  }
+  uint32_t x[kF8Parts][W], y[kF8Parts][W];
+#pragma unroll
+  for (int k = 0; k < kF8Parts; ++k)
+    if (k < splits) {
+      f8_remote<W>(p, cta + k * step, x[k]);
+      f8_remote<W>(q, cta + k * step, y[k]);
+    }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    float s = __uint_as_float(x[0][i]), t = __uint_as_float(y[0][i]);
+#pragma unroll
+    for (int k = 1; k < kF8Parts; ++k)
+      if (k < splits) {
+        s += __uint_as_float(x[k][i]);
+        t += __uint_as_float(y[k][i]);
+      }
+    a[i] = __float_as_uint(s);
+    u[i] = __float_as_uint(t);
+  }
+}
+
+// A lane's four codes of a block of 128 columns that the warp holds.
 __device__ __forceinline__ void f8_put_codes(const F8Codes &o, const F8GatedArgs &g, int64_t token,
-                                             int64_t j, const uint32_t (&v)[W], int lane) {
-  static_assert(W == 4, "a block of 128 entries is a warp's");
+                                             int64_t j, int64_t cols, const uint32_t (&v)[4],
+                                             int lane) {
   if (!o.codes) return;
   bool odd;
-  const uint32_t m = __reduce_max_sync(0xffffffffu, f8_top<W>(v, odd));
+  const uint32_t m = __reduce_max_sync(0xffffffffu, f8_top<4>(v, odd));
   if (odd) record_status(g.status, FQT_ENONFINITE);
   float inv;
   const uint32_t e = f8_scale(m, inv);
   // (rows of codes are whole 16 bytes)
-  if (j < g.M)
+  if (j < cols)
     *reinterpret_cast<uint32_t *>(o.codes + token * o.pitch + j) = f8_codes4<true>(v, inv);
   if (lane == 0) o.scales[scale_at(j / kF8Block, g.sp, token)] = (uint8_t)e;
 }
 
-// Few tokens: g and u of this CTA's hidden columns (g.part each) lie in its shared memory,
-// a token's 128 sums in a row (g, then u).  The CTAs of a cluster hold the 32 W columns of
-// whole blocks; a warp takes a token, a lane W columns.
-template <int W>
+// What is left to do where sums of g and u lie in the shared memory of a cluster's CTAs, which
+// share a tile's K blocks (g.splits / g.holds of them) and, with few tokens, blocks of 128
+// hidden columns (g.holds CTAs of g.part columns each).  A warp takes a token, a lane W of its
+// 32 W columns.  With few tokens a token's sums lie in a row of 128 (g, then u), else in a row
+// of 256 and four more (bank conflicts).
+template <int W, bool FEW>
 __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float *part) {
-  const int parts = 32 * W / g.part, self = (int)(blockIdx.x % parts);
+  const int ctas = g.splits, self = (int)(blockIdx.x % (unsigned)ctas);
+  const int holds = FEW ? g.holds : 1, splits = ctas / holds;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t j = (int64_t)(blockIdx.x / parts) * 32 * W + lane * W;
-  const int cta = lane * W / g.part, at = lane * W % g.part;
-  for (int64_t token = self + parts * warp; token < g.N; token += parts * (kF8Threads / 32)) {
+  const int64_t cols = FEW ? g.M : g.N;
+  int64_t t0 = 0, j = (int64_t)(blockIdx.x / (unsigned)ctas) * 32 * W, tokens = g.N;
+  int pitch = BM, second = g.part, cta = 0, at = lane * W;
+  if constexpr (FEW) {
+    cta = at / g.part;
+    at %= g.part;
+  } else {
+    const F8Item t = f8_item<256, false>(g, blockIdx.x);
+    t0 = t.m0;
+    j = t.n0 / 2;
+    tokens = min((int64_t)BM, g.M - t0);
+    pitch = 256 + 4;
+    second = 128;
+  }
+  j += lane * W;
+  for (int64_t r = self + ctas * warp; r < tokens; r += ctas * (kF8Threads / 32)) {
     uint32_t a[W], u[W];
-    f8_remote<W>(part + token * BM + at, cta, a);
-    f8_remote<W>(part + token * BM + g.part + at, cta, u);
+    f8_parts<W>(part + r * pitch + at, part + r * pitch + second + at, cta, holds, splits, a, u);
+    const int64_t token = t0 + r;
     if constexpr (W == 4) {
-      f8_put_codes<W>(g.gate, g, token, j, a, lane);
-      f8_put_codes<W>(g.up, g, token, j, u, lane);
+      f8_put_codes(g.gate, g, token, j, cols, a, lane);
+      f8_put_codes(g.up, g, token, j, cols, u, lane);
     }
     with_act(g.act, [&](auto act) {
 #pragma unroll
@@ -571,14 +628,25 @@ __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float 
       const int64_t o = token * g.ldo + j;
 #pragma unroll
       for (int i = 0; i < W; ++i)
-        if (j + i < g.M) {
+        if (j + i < cols) {
           if (g.bf16)
             static_cast<__nv_bfloat16 *>(g.out)[o + i] = __float2bfloat16_rn(__uint_as_float(a[i]));
           else
             static_cast<float *>(g.out)[o + i] = __uint_as_float(a[i]);
         }
     }
-    if constexpr (W == 4) f8_put_codes<W>(g.q, g, token, j, a, lane);
+    if constexpr (W == 4) f8_put_codes(g.q, g, token, j, cols, a, lane);
+  }
+}
+
+template <int NT>
+__device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float *part) {
+  if constexpr (NT == 256) {
+    f8_gated_join<4, false>(g, part);
+  } else {
+    if (g.holds * g.part == kF8Block) f8_gated_join<4, true>(g, part);
+    else if (g.part == 64) f8_gated_join<2, true>(g, part);
+    else f8_gated_join<1, true>(g, part);
   }
 }
 

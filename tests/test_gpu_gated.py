@@ -90,8 +90,9 @@ def _codes_equal(q, x):
     _same(q, _f8(x))
 
 
-# few tokens; single CTAs; pairs of CTAs
-SIZES = [(1, 1, 1), (1, 4096, 1024), (2, 130, 27), (5, 5000, 300), (31, 335, 129), (33, 40, 700),
+# few tokens; single CTAs; both with K blocks that a cluster shares; pairs of CTAs
+SIZES = [(3, 300, 4000), (50, 40, 3000), (64, 1500, 1100), (130, 130, 4100), (70, 257, 2000),
+         (400, 300, 1300), (1, 1, 1), (1, 4096, 1024), (2, 130, 27), (5, 5000, 300), (31, 335, 129), (33, 40, 700),
          (64, 128, 1201), (64, 700, 128), (65, 128, 64), (100, 17, 513), (129, 257, 1025),
          (300, 335, 1201), (700, 1000, 40), (2000, 1001, 200), (4111, 600, 96)]
 

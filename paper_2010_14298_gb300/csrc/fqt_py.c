@@ -17,14 +17,14 @@ enum {
   A_CODES, A_CODES16, A_INV_S, A_ZERO, A_ROW_SUM, A_COL_SUM, A_LEAD, A_HZ, A_HR, A_PERM,
   A_GSTART, A_GSIZE, A_SHIFT16, A_SHIFT, A_SHIFT_COL_SUM, A_SHIFT_SCALE, A_POINTERS,
   A_BITS = A_POINTERS, A_KIND, A_BLOCK, A_ROWS_PER_SAMPLE, A_CONV, A_LOGICAL, A_SHAPE,
-  A_DATA_PTR, A_SCALES, A_ROWS, A_COLS, A_PITCH, A_BLOCK_ROWS, A_COUNT
+  A_DATA_PTR, A_SCALES, A_ROWS, A_COLS, A_SIZE, A_BLOCK_ROWS, A_COUNT
 };
 static const char *const kNames[A_COUNT] = {
     "codes", "codes16", "inv_s", "zero", "row_sum", "col_sum", "lead", "hz", "hr", "perm",
     "gstart", "gsize", "shift16", "shift", "shift_col_sum", "shift_scale", "bits", "kind",
     "block", "rows_per_sample", "conv", "logical", "shape", "data_ptr",
-    "scales", "rows", "cols", "pitch", "block_rows"};
-static PyObject *g_name[A_COUNT];
+    "scales", "rows", "cols", "size", "block_rows"};
+static PyObject *g_name[A_COUNT], *g_one;
 
 /* data_ptr() of a tensor; -1 with an exception set on failure (AttributeError
  * for None) */
@@ -155,10 +155,19 @@ static int fill_fp8(PyObject *q, fqt_fp8 *s, fqt_fp8 **out) {
   memset(s, 0, sizeof(*s));
   *out = NULL;
   if (q == Py_None) return 0;
+  /* the pitch is codes.size(1), asked of the tensor: Fp8Tensor's property took 0.2 us */
   void *codes, *scales;
-  if (ptr_attr(q, A_CODES, &codes) || ptr_attr(q, A_SCALES, &scales) ||
-      i64_attr(q, A_ROWS, &s->rows) || i64_attr(q, A_COLS, &s->cols) ||
-      i64_attr(q, A_PITCH, &s->pitch) || int_attr(q, A_BLOCK_ROWS, &s->block_rows))
+  PyObject *t = PyObject_GetAttr(q, g_name[A_CODES]);
+  if (!t) return -1;
+  PyObject *pitch = needed_ptr(t, &codes)
+                        ? NULL
+                        : PyObject_CallMethodOneArg(t, g_name[A_SIZE], g_one);
+  Py_DECREF(t);
+  if (!pitch) return -1;
+  s->pitch = PyLong_AsLongLong(pitch);
+  Py_DECREF(pitch);
+  if (PyErr_Occurred() || ptr_attr(q, A_SCALES, &scales) || i64_attr(q, A_ROWS, &s->rows) ||
+      i64_attr(q, A_COLS, &s->cols) || int_attr(q, A_BLOCK_ROWS, &s->block_rows))
     return -1;
   s->codes = codes;
   s->scales = scales;
@@ -484,5 +493,6 @@ static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fqt_py", NULL, -1,
 PyMODINIT_FUNC PyInit__fqt_py(void) {
   for (int i = 0; i < A_COUNT; ++i)
     if (!(g_name[i] = PyUnicode_InternFromString(kNames[i]))) return NULL;
+  if (!(g_one = PyLong_FromLong(1))) return NULL;
   return PyModule_Create(&kModule);
 }

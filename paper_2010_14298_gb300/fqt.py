@@ -870,12 +870,14 @@ def fp8_matmul_sum_workspace_size(M: int, N: int, K1: int, K2: int) -> int:
     return int(load().fqt_fp8_matmul_sum_workspace_size(M, N, K1, K2))
 
 
-def _fp8_in(t, name, dev):
-    """An 8-bit matrix to read, on that GPU (None: on any)."""
-    there = t.codes.get_device()
-    if there < 0 or (dev is not None and there != dev):
-        raise _elsewhere(t.codes, name, -1 if there < 0 else dev)
-    return there
+def _fp8_gpu(names, *tensors):
+    """The GPU that all of these 8-bit matrices are on."""
+    dev = tensors[0].codes.get_device()
+    for t in tensors:
+        if t.codes.get_device() != dev or dev < 0:
+            name = names.split()[[t is x for x in tensors].index(True)]
+            raise _elsewhere(t.codes, name, dev)
+    return dev
 
 
 def fp8_matmul_sum(A1: Fp8Tensor, B1: Fp8Tensor, A2: Fp8Tensor, B2: Fp8Tensor,
@@ -887,9 +889,7 @@ def fp8_matmul_sum(A1: Fp8Tensor, B1: Fp8Tensor, A2: Fp8Tensor, B2: Fp8Tensor,
         raise ValueError(f"the pairs have {A1.cols} and {B1.cols}, {A2.cols} and {B2.cols} columns")
     if A1.rows != A2.rows or B1.rows != B2.rows:
         raise ValueError(f"the products are {A1.rows} x {B1.rows} and {A2.rows} x {B2.rows}")
-    dev = _fp8_in(A1, "A1", None)
-    for t, name in ((B1, "B1"), (A2, "A2"), (B2, "B2")):
-        _fp8_in(t, name, dev)
+    dev = _fp8_gpu("A1 B1 A2 B2", A1, B1, A2, B2)
     if out is not None:
         dtype = out.dtype
     out, ldo = _rows_out(out, "out", A1.rows, B1.rows, dtype, dev, A1.codes, stream)
@@ -930,22 +930,17 @@ def fp8_gated_matmul(A: Fp8Tensor, Bg: Fp8Tensor, Bu: Fp8Tensor, act: str = "sil
     fp8_gated_backward reads (a tensor given for one does too); None stands for one that
     was not asked for."""
     act = _act(act)
-    if A.cols != Bg.cols or A.cols != Bu.cols:
-        raise ValueError(f"A has {A.cols} columns, the weights {Bg.cols} and {Bu.cols}")
-    if Bg.rows != Bu.rows:
-        raise ValueError(f"the weights have {Bg.rows} and {Bu.rows} rows")
-    M, N = A.rows, Bg.rows
-    dev = _fp8_in(A, "A", None)
-    _fp8_in(Bg, "Bg", dev)
-    _fp8_in(Bu, "Bu", dev)
-    ldo, like = N, A.codes
-    if out is not None:
-        dtype = out.dtype
+    M, N, K = A.rows, Bg.rows, A.cols
+    if Bg.cols != K or Bu.cols != K:
+        raise ValueError(f"A has {K} columns, the weights {Bg.cols} and {Bu.cols}")
+    if Bu.rows != N:
+        raise ValueError(f"the weights have {N} and {Bu.rows} rows")
+    dev = _fp8_gpu("A Bg Bu", A, Bg, Bu)
+    ldo, like, kind = N, A.codes, BF16
     if dense or out is not None:
-        out, ldo = _rows_out(out, "out", M, N, dtype, dev, like, stream)
+        out, ldo = _rows_out(out, "out", M, N, dtype if out is None else out.dtype, dev, like,
+                             stream)
         kind = _dtype_code(out)
-    else:
-        kind = BF16
     if codes or q is not None:
         q = _fp8_out(q, "q", M, N, 1, dev, like, stream)
     if keep or gate is not None:
@@ -960,9 +955,12 @@ def fp8_gated_matmul(A: Fp8Tensor, Bg: Fp8Tensor, Bu: Fp8Tensor, act: str = "sil
                                    _raw_stream(stream))
     if st:
         _check(st, "fqt_fp8_gated_matmul")
-    for t in (q, gate, up):
-        if t is not None:
-            t.block_rows = 1
+    if q is not None:
+        q.block_rows = 1
+    if gate is not None:
+        gate.block_rows = 1
+    if up is not None:
+        up.block_rows = 1
     return out, q, gate, up
 
 
@@ -999,7 +997,8 @@ def fp8_gated_backward(dA: torch.Tensor, gate: Fp8Tensor, up: Fp8Tensor, act: st
     act = _act(act)
     dA, rows, cols, ldda, dev = _rows_in(dA, "dA", stream)
     for t, name in ((gate, "gate"), (up, "up")):
-        _fp8_in(t, name, dev)
+        if t.codes.get_device() != dev:
+            raise _elsewhere(t.codes, name, dev)
         if t.rows != rows or t.cols != cols:
             raise ValueError(f"{name} is {t.rows} x {t.cols}, dA {rows} x {cols}")
     if out is None:

@@ -530,6 +530,60 @@ def test_new_inputs_in_a_graph():
     assert torch.equal(out, fqt.fp8_gated_matmul(b, bg, bu)[0])
 
 
+def test_offsets_past_32_bits():
+    """2^20 tokens of 4112 hidden columns, 4.3 GB of codes: the last rows are those of a call on
+    them alone (rows of codes and of dense outputs, and the last 128 tokens' columns of a
+    transpose, depend on no other rows)."""
+    T, H, K, few = 1 << 20, 4112, 64, 256
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    codes = lambda r, c: torch.randint(0, 126, (r, c), generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    shape = fqt.Fp8Tensor.scale_shape
+    scales = lambda r, c: torch.randint(115, 120, shape(r, c), generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    rand = lambda r, c: fqt.Fp8Tensor(codes(r, -(-c // 16) * 16), scales(r, c), r, c)  # noqa: E731
+    last = lambda q: fqt.Fp8Tensor(q.codes[T - few:].clone(), q.scales[:, T - few:].contiguous(), few, q.cols)  # noqa: E731
+    a, bg, bu = rand(T, K), rand(H, K), rand(H, K)
+    out = torch.empty((T, H), dtype=torch.bfloat16, device="cuda")
+    E = fqt.Fp8Tensor.empty
+    ws = fqt.Workspace.of_size(256)
+    q, gate, up = E(T, H), E(T, H), E(T, H)
+    fqt.fp8_gated_matmul(a, bg, bu, "relu", out=out, q=q, gate=gate, up=up, ws=ws)
+    _, _, want, bound = _expected(last(a), bg, bu, "relu")
+    assert ((out[T - few:].double() - want).abs() <= bound + 2.0 ** -8 * (want.abs() + bound)).all()
+    for t, i in ((gate, 0), (up, 1)):
+        x, e = _sums(last(a), (bg, bu)[i])
+        assert ((last(t).dequantize().double() - x).abs() <= 2.0 ** -4 * x.abs() + 1.07 * e
+                + 2.0 ** -10 * x.abs().amax(1, keepdim=True)).all()
+    dA = out
+    r = fqt.fp8_gated_backward(dA, gate, up, "relu", ws=ws)
+    alone = fqt.fp8_gated_backward(dA[T - few:], last(gate), last(up), "relu")
+    _same(last(r.qgate), alone.qgate)
+    _same(last(r.qup), alone.qup)
+    for name in ("qgate_t", "qup_t", "product_t"):
+        big, small = getattr(r, name), getattr(alone, name)
+        assert torch.equal(big.codes[:, T - few:], small.codes[:, :few])
+    del r, q
+    dense = fqt.GatedGrads(dgate=torch.empty_like(dA), dup=torch.empty_like(dA))
+    fqt.fp8_gated_backward(dA, gate, up, "relu", out=dense, ws=ws)
+    small = fqt.fp8_gated_backward(dA[T - few:], last(gate), last(up), "relu", out=fqt.GatedGrads(
+        dgate=torch.empty_like(dA[T - few:]), dup=torch.empty_like(dA[T - few:])))
+    assert torch.equal(dense.dgate[T - few:], small.dgate)
+    assert torch.equal(dense.dup[T - few:], small.dup)
+    out = fqt.fp8_matmul_sum(a, bg, a, bu, dtype=torch.bfloat16, ws=ws)
+    (x, e), (y, f) = _sums(last(a), bg), _sums(last(a), bu)
+    assert ((out[T - few:].double() - x - y).abs() <= (e + f) + 2.0 ** -8 * ((x + y).abs() + e + f)).all()
+    assert fqt.sync_status(ws) == 0
+
+
+def test_gradients_that_are_laid_out_otherwise():
+    """A transposed or every other column of a gradient is read as it is."""
+    gate, up, dA = _kept(130, 96)
+    ref = fqt.fp8_gated_backward(dA, gate, up)
+    for x in (dA.t().contiguous().t(), torch.stack([dA, dA], 2).flatten(1)[:, ::2]):
+        r = fqt.fp8_gated_backward(x, gate, up)
+        _same(r.qgate, ref.qgate), _same(r.qup_t, ref.qup_t)
+
+
 def test_empty_sizes():
     none, few = fqt.Fp8Tensor.empty(0, 64), _f8(torch.ones((8, 64), device="cuda"))
     assert fqt.fp8_gated_matmul(none, few, few)[0].shape == (0, 8)

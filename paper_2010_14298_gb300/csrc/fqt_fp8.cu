@@ -398,7 +398,9 @@ fqt_status fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, bool bf16, void *out, 
 }
 
 // The K blocks of both pairs in one list, the second's from a group of scales on: the sums
-// stay in one accumulator, so the second product adds no pass over the output.
+// stay in one accumulator, so the second product adds no pass over the output.  8192 x 1024
+// with K 4096 twice: 46 us, as one product of 8192 (3.0 PFLOP/s: 128 super tiles on 76 pairs
+// are two rounds); two products of 4096 take 54 and need their outputs added.
 fqt_status fp8_matmul_sum(const fqt_fp8 *A1, const fqt_fp8 *B1, const fqt_fp8 *A2,
                           const fqt_fp8 *B2, bool bf16, void *out, int64_t ldo, void *ws,
                           cudaStream_t st) {

@@ -379,8 +379,9 @@ __device__ __forceinline__ void f8_put_dense(const F8Of<F8_GATED>::Maps &maps, c
 // One super tile's (or tile's) accumulator holds g in its first 128 columns and u in the
 // others, for the same 128 hidden columns.  A warp takes 64 columns of both for its 32 rows (a
 // lane a row), so a is formed in registers.  This one is for a dense output alone: its fewer
-// warps hand the accumulator back sooner than 16 (8192 x 4096 x 1024: 47 us and 54); and for
-// tiles whose K blocks a cluster shares, with any outputs.
+// warps hand the accumulator back sooner than 16 (8192 x 4096 x 1024: 47 us, 2.9 PFLOP/s, and
+// 54; an item's products take 4500 of the 5100 cycles from one to the next, its epilogue 3200
+// under them); and for tiles whose K blocks a cluster shares, with any outputs.
 template <int ACCS, bool PAIR, bool FOLD>
 __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
                                                const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
@@ -414,13 +415,19 @@ __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
 // With codes among the outputs a warp takes 32 columns, and a row's block of 128 is four
 // lanes', which exchange their maxima through shared memory: g and u leave first, then a takes
 // g's registers.  Codes leave by TMA in boxes of 32 rows x 128 bytes that a quadrant's four
-// warps fill (boxes of a warp's own 32 bytes a row: three kinds of codes of 8192 x 4096 x 1024
-// 68 us; straight from registers 90).  The warps meet at named barriers, for
-// the maxima: what is in a box by then leaves after it, so a's codes leave in the next round.
-// DENSE: a leaves densely as well.  Registers decide here (96 a thread): sums that are taken 16
-// columns at a time, as if they were to be added to others, leave the compiler more of them
-// than all at once (61 us and 73), and so do kernels without the dense output's code.
-// Whatever makes one of the warps stop, all four leave the loop at the same barrier.
+// warps fill (straight from registers, 32 bytes a row, they took 90 us).  The warps meet at
+// named barriers, for the maxima: what is in a box by then leaves after it, so a's codes leave
+// in the next round.  Whatever makes one of the warps stop, all four leave the loop at the same
+// barrier.  DENSE: a leaves densely as well.
+//
+// 8192 x 4096 x 1024: a's codes 50 us, those of a, g and u 59 (2.3 PFLOP/s), 67 with gelu,
+// where a dense output takes 47.  An item's products take 5000 cycles; this epilogue, next to
+// them, 7000: 16 warps issue at 44% of the rate, waiting for their own arithmetic, the shared
+// memory and one another.  Registers decide (96 a thread): with eight
+// warps and twice the columns 78 us; sums taken all at once instead of 16 columns at a time 72,
+// with spilled registers; kernels without a dense output are without its code.  Maxima taken
+// along with the sums, or 8 columns at a time while the next are on their way: 62; half of the
+// reciprocals by Newton's iteration: no difference.
 template <int ACCS, bool PAIR, bool DENSE>
 __device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
                                                const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
@@ -587,7 +594,8 @@ __device__ __forceinline__ void f8_put_codes(const F8Codes &o, const F8GatedArgs
 // share a tile's K blocks (g.splits / g.holds of them) and, with few tokens, blocks of 128
 // hidden columns (g.holds CTAs of g.part columns each).  A warp takes a token, a lane W of its
 // 32 W columns.  With few tokens a token's sums lie in a row of 128 (g, then u), else in a row
-// of 256 and four more (bank conflicts).
+// of 256 and four more (bank conflicts).  A token of 4096 x 1024: 5.3 us, with codes, for which
+// four CTAs meet, 6.6; what a call of one K block takes is 5.
 template <int W, bool FEW>
 __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float *part) {
   const int ctas = g.splits, self = (int)(blockIdx.x % (unsigned)ctas);

@@ -579,7 +579,7 @@ __device__ __forceinline__ void f8_load_gated(const F8Of<F8_GATED>::Maps &maps,
 template <int NT>
 __device__ __forceinline__ uint32_t f8_gated_scales(const F8GatedArgs &g, const F8Item &t,
                                                     int64_t group, int i, int lane);
-template <int ACCS, bool PAIR, bool FOLD>
+template <int NT, int ACCS, bool PAIR, bool FOLD>
 __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
                                                const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
                                                uint64_t *acce, volatile int *abort_flag, float *box,
@@ -608,7 +608,8 @@ __global__ void __launch_bounds__(32 * (kF8Epi0 + kF8EpiOf<NT, KIND>), 1)
     k_f8_mm(const __grid_constant__ typename F8Of<KIND>::Maps maps,
             const typename F8Of<KIND>::Args g) {
   // a gated block's few tokens, or shared K blocks
-  constexpr bool kFew = f8_gated(KIND) && NT <= 64, kJoins = kFew || (KIND == F8_GATED_DENSE && !PAIR);
+  constexpr bool kFew = f8_gated(KIND) && NT <= 64;
+  constexpr bool kJoins = kFew || (KIND == F8_GATED_DENSE && NT == 256 && !PAIR);
   // columns of an epilogue warp: a multiple of 32 for the first half's
   constexpr int W0 = NT <= 64 ? NT / 2 : (NT / 2 + 31) / 32 * 32, W1 = NT - W0;
   constexpr int NB = PAIR ? NT / 2 : NT;    // rows of B that this CTA loads
@@ -670,15 +671,15 @@ __global__ void __launch_bounds__(32 * (kF8Epi0 + kF8EpiOf<NT, KIND>), 1)
   const uint32_t tmem = *tmem_slot;
   wait_for_previous();
 
-  if (f8_gated(KIND) && NT == 256 && warp >= kF8Epi0) {
+  if (f8_gated(KIND) && !kFew && warp >= kF8Epi0) {
     uint8_t *after = ops + (size_t)g.stages * kStage;
     const int e = warp - kF8Epi0;
     if constexpr (f8_gated_with_codes(KIND) && NT == 256)
       f8_gated_codes<ACCS, PAIR, KIND == F8_GATED_BOTH>(maps, g, tmem, accf, acce, abort_flag, after + kF8TopBytes,
                                        reinterpret_cast<uint32_t *>(after), warp & 3, e >> 2, lane,
                                        first, step);
-    else if constexpr (KIND == F8_GATED_DENSE && NT == 256)
-      f8_gated_dense<ACCS, PAIR, FOLD>(maps, g, tmem, accf, acce, abort_flag,
+    else if constexpr (KIND == F8_GATED_DENSE && !kFew)
+      f8_gated_dense<NT, ACCS, PAIR, FOLD>(maps, g, tmem, accf, acce, abort_flag,
                                        reinterpret_cast<float *>(after + e * kF8BoxBytes),
                                        reinterpret_cast<float *>(ops), warp & 3, e >> 2, lane,
                                        first, step);

@@ -153,8 +153,8 @@ __device__ __forceinline__ void with_act(int act, F f) {
 // ---------------------------------------------------------------------------
 // The product kernel's operands
 // ---------------------------------------------------------------------------
-// The right operand of a tile are 128 rows of the gate's weights and the same 128 of the up
-// projection's (of a pair's CTAs, each loads one).  With few tokens the left operand are
+// The right operand of a tile are 128 rows of the gate's weights (64 in a narrow tile) and the
+// same of the up projection's (of a pair's CTAs, each loads one).  With few tokens the left operand are
 // g.part rows of each, and what is left of its 128 rows is not used.
 template <int NT, bool PAIR>
 __device__ __forceinline__ void f8_load_gated(const F8Of<F8_GATED>::Maps &maps,
@@ -173,10 +173,10 @@ __device__ __forceinline__ void f8_load_gated(const F8Of<F8_GATED>::Maps &maps,
     tma_load_2d_pair(stage, &maps.a, k, m, bar);
     tma_load_2d_pair(stage + kTileBytes, rank ? &maps.b2 : &maps.b, k, n, bar);
   } else {
-    mbar_expect_tx(full, (uint32_t)(3 * kTileBytes));
+    mbar_expect_tx(full, (uint32_t)kTileBytes + NT * kF8Block);
     tma_load_2d(stage, &maps.a, k, m, full);
     tma_load_2d(stage + kTileBytes, &maps.b, k, n, full);
-    tma_load_2d(stage + 2 * kTileBytes, &maps.b2, k, n, full);
+    tma_load_2d(stage + kTileBytes + NT / 2 * kF8Block, &maps.b2, k, n, full);
   }
 }
 
@@ -199,7 +199,9 @@ __device__ __forceinline__ uint32_t f8_gated_scales(const F8GatedArgs &g, const 
   } else if (i < 4) {
     from = g.sa, pitch = g.spa, rows = g.M, r = t.m0 + 32 * i + lane;
   } else {
-    from = i < 8 ? g.sb : g.s2, pitch = g.spb, rows = g.N, r = t.n0 / 2 + 32 * (i & 3) + lane;
+    const int at = 32 * (i - 4);
+    from = at < NT / 2 ? g.sb : g.s2, pitch = g.spb, rows = g.N;
+    r = t.n0 / 2 + at % (NT / 2) + lane;
   }
   return r < rows ? __ldg(from + group * pitch + r) : 0x7F7F7F7Fu;
 }
@@ -294,7 +296,7 @@ __device__ __forceinline__ uint32_t f8_block_scale(const uint32_t *tops, float &
 
 // A tile's sums of this warp's CW columns of g and of u, when they are there; false if they do
 // not come.  The accumulator is handed back.
-template <int CW, int ACCS, bool PAIR, bool FOLD>
+template <int NT, int CW, int ACCS, bool PAIR, bool FOLD>
 __device__ __forceinline__ bool f8_gated_sums(const F8GatedArgs &g, const F8Item &t,
                                               uint32_t lane_base, uint64_t *accf, uint64_t *acce,
                                               volatile int *abort_flag, int lane, uint32_t &c,
@@ -309,12 +311,12 @@ __device__ __forceinline__ bool f8_gated_sums(const F8GatedArgs &g, const F8Item
       return false;
     }
     tc_fence_after();
-    const uint32_t from = lane_base + (uint32_t)(buf * 256);
+    const uint32_t from = lane_base + (uint32_t)(buf * NT);
     if constexpr (!FOLD) {
 #pragma unroll
       for (int j = 0; j < CW; j += 32) {
         tmem_ld32_nw(from + j, *reinterpret_cast<uint32_t(*)[32]>(v + j));
-        tmem_ld32_nw(from + 128 + j, *reinterpret_cast<uint32_t(*)[32]>(w + j));
+        tmem_ld32_nw(from + NT / 2 + j, *reinterpret_cast<uint32_t(*)[32]>(w + j));
       }
 #pragma unroll
       for (int j = 0; j < CW; j += 32) {
@@ -325,7 +327,7 @@ __device__ __forceinline__ bool f8_gated_sums(const F8GatedArgs &g, const F8Item
 #pragma unroll
       for (int j = 0; j < 2 * CW; j += 16) {  // 16 columns at a time: registers
         uint32_t r[16];
-        tmem_ld16_nw(from + (j < CW ? j : 128 + j - CW), r);
+        tmem_ld16_nw(from + (j < CW ? j : NT / 2 + j - CW), r);
         tmem_wait_ld(r);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -376,38 +378,39 @@ __device__ __forceinline__ void f8_put_dense(const F8Of<F8_GATED>::Maps &maps, c
   }
 }
 
-// One super tile's (or tile's) accumulator holds g in its first 128 columns and u in the
-// others, for the same 128 hidden columns.  A warp takes 64 columns of both for its 32 rows (a
-// lane a row), so a is formed in registers.  This one is for a dense output alone: its fewer
-// warps hand the accumulator back sooner than 16 (8192 x 4096 x 1024: 47 us, 2.9 PFLOP/s, and
-// 54; an item's products take 4500 of the 5100 cycles from one to the next, its epilogue 3200
-// under them); and for tiles whose K blocks a cluster shares, with any outputs.
-template <int ACCS, bool PAIR, bool FOLD>
+// One super tile's (or tile's) accumulator holds g in its first half of columns and u in the
+// others, for the same 128 hidden columns (64 in a narrow tile).  A warp takes half of them of
+// both for its 32 rows (a lane a row), so a is formed in registers.  This one is for a dense
+// output alone: its fewer warps hand the accumulator back sooner than 16 (8192 x 4096 x 1024: 47
+// us, 2.9 PFLOP/s, and 54; an item's products take 4500 of the 5100 cycles from one to the next,
+// its epilogue 3200 under them); and for tiles whose K blocks a cluster shares, with any outputs.
+template <int NT, int ACCS, bool PAIR, bool FOLD>
 __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
                                                const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,
                                                uint64_t *acce, volatile int *abort_flag, float *box,
                                                float *part, int q, int h, int lane, int64_t first,
                                                int64_t step) {
+  constexpr int CW = NT / 4;
   uint32_t c = 0;
   for (int64_t it = first; it < g.items && !*abort_flag; it += step) {
-    const F8Item t = f8_item<256, PAIR>(g, it);
-    uint32_t v[64], w[64];  // g (then a) and u
-    if (!f8_gated_sums<64, ACCS, PAIR, FOLD>(
-            g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 64), accf, acce, abort_flag,
+    const F8Item t = f8_item<NT, PAIR>(g, it);
+    uint32_t v[CW], w[CW];  // g (then a) and u
+    if (!f8_gated_sums<NT, CW, ACCS, PAIR, FOLD>(
+            g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * CW), accf, acce, abort_flag,
             lane, c, v, w))
       break;
-    if constexpr (!PAIR)
+    if constexpr (!PAIR && NT == 256)
       if (g.splits > 1) {  // the products are done with the operand stages
-        float *to = part + (q * 32 + lane) * (256 + 4) + h * 64;
+        float *to = part + (q * 32 + lane) * (256 + 4) + h * CW;
 #pragma unroll
-        for (int i = 0; i < 64; i += 4) {
+        for (int i = 0; i < CW; i += 4) {
           *reinterpret_cast<uint4 *>(to + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
           *reinterpret_cast<uint4 *>(to + 128 + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
         }
         break;
       }
-    f8_form<64>(g.act, v, w);
-    f8_put_dense<64>(maps, g, box, lane, t.m0 + q * 32, t.n0 / 2 + h * 64, v);
+    f8_form<CW>(g.act, v, w);
+    f8_put_dense<CW>(maps, g, box, lane, t.m0 + q * 32, t.n0 / 2 + h * CW, v);
   }
   if (lane == 0) bulk_wait_all();
 }
@@ -454,7 +457,7 @@ __device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
   for (int64_t it = first; it < g.items; it += step, parity ^= 1u) {
     const F8Item t = f8_item<256, PAIR>(g, it);
     uint32_t v[32], w[32];  // g (then a) and u
-    const bool ok = f8_gated_sums<32, ACCS, PAIR, true>(
+    const bool ok = f8_gated_sums<256, 32, ACCS, PAIR, true>(
         g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 32), accf, acce, abort_flag, lane,
         c, v, w);
     const int64_t m0 = t.m0 + q * 32, n0 = t.n0 / 2;
@@ -651,7 +654,7 @@ template <int NT>
 __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float *part) {
   if constexpr (NT == 256) {
     f8_gated_join<4, false>(g, part);
-  } else {
+  } else if constexpr (NT <= 64) {
     if (g.holds * g.part == kF8Block) f8_gated_join<4, true>(g, part);
     else if (g.part == 64) f8_gated_join<2, true>(g, part);
     else f8_gated_join<1, true>(g, part);

@@ -155,7 +155,7 @@ static int fill_fp8(PyObject *q, fqt_fp8 *s, fqt_fp8 **out) {
   memset(s, 0, sizeof(*s));
   *out = NULL;
   if (q == Py_None) return 0;
-  /* the pitch is codes.size(1), asked of the tensor: Fp8Tensor's property took 0.2 us */
+  /* the pitch is codes.size(1), asked of the tensor and not by way of the property */
   void *codes, *scales;
   PyObject *t = PyObject_GetAttr(q, g_name[A_CODES]);
   if (!t) return -1;

@@ -645,6 +645,9 @@ def _rows_in(t, name, stream):
     dev = t.get_device()
     if dev < 0:
         raise _elsewhere(t, name, dev)
+    shape = t.shape
+    if len(shape) == 2 and t.is_contiguous():
+        return t, shape[0], shape[1], shape[1], dev
     rows, cols = _matrix(t, name)
     ld = _row_stride(t, rows, cols)
     if ld is None:
@@ -658,6 +661,9 @@ def _rows_out(t, name, rows, cols, dtype, dev, like, stream):
     """A matrix to write (a new one for None), and its row pitch."""
     if t is None:
         return _new((rows, cols), dtype, like, stream), cols
+    if (t.shape == (rows, cols) and t.is_contiguous() and t.dtype is dtype
+            and t.get_device() == dev):
+        return t, cols
     if t.get_device() != dev:
         raise _elsewhere(t, name, dev)
     if t.dtype != dtype or _matrix(t, name) != (rows, cols):
@@ -870,14 +876,12 @@ def fp8_matmul_sum_workspace_size(M: int, N: int, K1: int, K2: int) -> int:
     return int(load().fqt_fp8_matmul_sum_workspace_size(M, N, K1, K2))
 
 
-def _fp8_gpu(names, *tensors):
-    """The GPU that all of these 8-bit matrices are on."""
+def _fp8_apart(names, *tensors):
+    """Why 8-bit matrices are not all on one GPU."""
     dev = tensors[0].codes.get_device()
-    for t in tensors:
-        if t.codes.get_device() != dev or dev < 0:
-            name = names.split()[[t is x for x in tensors].index(True)]
-            raise _elsewhere(t.codes, name, dev)
-    return dev
+    for name, t in zip(names.split(), tensors):
+        if dev < 0 or t.codes.get_device() != dev:
+            return _elsewhere(t.codes, name, dev)
 
 
 def fp8_matmul_sum(A1: Fp8Tensor, B1: Fp8Tensor, A2: Fp8Tensor, B2: Fp8Tensor,
@@ -889,7 +893,10 @@ def fp8_matmul_sum(A1: Fp8Tensor, B1: Fp8Tensor, A2: Fp8Tensor, B2: Fp8Tensor,
         raise ValueError(f"the pairs have {A1.cols} and {B1.cols}, {A2.cols} and {B2.cols} columns")
     if A1.rows != A2.rows or B1.rows != B2.rows:
         raise ValueError(f"the products are {A1.rows} x {B1.rows} and {A2.rows} x {B2.rows}")
-    dev = _fp8_gpu("A1 B1 A2 B2", A1, B1, A2, B2)
+    dev = A1.codes.get_device()
+    if (dev < 0 or B1.codes.get_device() != dev or A2.codes.get_device() != dev
+            or B2.codes.get_device() != dev):
+        raise _fp8_apart("A1 B1 A2 B2", A1, B1, A2, B2)
     if out is not None:
         dtype = out.dtype
     out, ldo = _rows_out(out, "out", A1.rows, B1.rows, dtype, dev, A1.codes, stream)
@@ -935,8 +942,10 @@ def fp8_gated_matmul(A: Fp8Tensor, Bg: Fp8Tensor, Bu: Fp8Tensor, act: str = "sil
         raise ValueError(f"A has {K} columns, the weights {Bg.cols} and {Bu.cols}")
     if Bu.rows != N:
         raise ValueError(f"the weights have {N} and {Bu.rows} rows")
-    dev = _fp8_gpu("A Bg Bu", A, Bg, Bu)
     ldo, like, kind = N, A.codes, BF16
+    dev = like.get_device()
+    if dev < 0 or Bg.codes.get_device() != dev or Bu.codes.get_device() != dev:
+        raise _fp8_apart("A Bg Bu", A, Bg, Bu)
     if dense or out is not None:
         out, ldo = _rows_out(out, "out", M, N, dtype if out is None else out.dtype, dev, like,
                              stream)
@@ -996,37 +1005,49 @@ def fp8_gated_backward(dA: torch.Tensor, gate: Fp8Tensor, up: Fp8Tensor, act: st
     GatedGrads.empty."""
     act = _act(act)
     dA, rows, cols, ldda, dev = _rows_in(dA, "dA", stream)
-    for t, name in ((gate, "gate"), (up, "up")):
-        if t.codes.get_device() != dev:
-            raise _elsewhere(t.codes, name, dev)
-        if t.rows != rows or t.cols != cols:
-            raise ValueError(f"{name} is {t.rows} x {t.cols}, dA {rows} x {cols}")
+    if gate.rows != rows or gate.cols != cols or up.rows != rows or up.cols != cols:
+        raise ValueError(f"dA is {rows} x {cols}, gate {gate.rows} x {gate.cols}, "
+                         f"up {up.rows} x {up.cols}")
+    if gate.codes.get_device() != dev or up.codes.get_device() != dev:
+        name, t = ("gate", gate) if gate.codes.get_device() != dev else ("up", up)
+        raise _elsewhere(t.codes, name, dev)
     if out is None:
         with _on(stream):
             out = GatedGrads.empty(rows, cols, dA.device)
-    lddg = lddu = cols
-    if out.dgate is not None:
-        _, lddg = _rows_out(out.dgate, "dgate", rows, cols, dA.dtype, dev, dA, stream)
-    if out.dup is not None:
-        _, lddu = _rows_out(out.dup, "dup", rows, cols, dA.dtype, dev, dA, stream)
-    codes = ((out.qgate, "qgate", rows, cols), (out.qup, "qup", rows, cols),
-             (out.qgate_t, "qgate_t", cols, rows), (out.qup_t, "qup_t", cols, rows),
-             (out.product_t, "product_t", cols, rows))
-    for t, name, r, c in codes:
-        if t is not None:
-            _fp8_out(t, name, r, c, 1, dev, dA, stream)
+    dgate, dup, lddg, lddu = out.dgate, out.dup, cols, cols
+    if dgate is not None:
+        lddg = _rows_out(dgate, "dgate", rows, cols, dA.dtype, dev, dA, stream)[1]
+    if dup is not None:
+        lddu = _rows_out(dup, "dup", rows, cols, dA.dtype, dev, dA, stream)[1]
+    qg, qu, qgt, qut, qat = out.qgate, out.qup, out.qgate_t, out.qup_t, out.product_t
+    if qg is not None:
+        _fp8_out(qg, "qgate", rows, cols, 1, dev, dA, stream)
+    if qu is not None:
+        _fp8_out(qu, "qup", rows, cols, 1, dev, dA, stream)
+    if qgt is not None:
+        _fp8_out(qgt, "qgate_t", cols, rows, 1, dev, dA, stream)
+    if qut is not None:
+        _fp8_out(qut, "qup_t", cols, rows, 1, dev, dA, stream)
+    if qat is not None:
+        _fp8_out(qat, "product_t", cols, rows, 1, dev, dA, stream)
     if ws is None:
         with _on(stream):
             ws = Workspace.of_size(fp8_gated_backward_workspace_size(rows, cols), dA.device)
     buf, nbytes = _scratch(ws, dev)
-    st = native().fp8_gated_backward(dA, ldda, _dtype_code(dA), gate, up, act, out.dgate, lddg,
-                                     out.dup, lddu, out.qgate, out.qup, out.qgate_t, out.qup_t,
-                                     out.product_t, buf, nbytes, _raw_stream(stream))
+    st = native().fp8_gated_backward(dA, ldda, _dtype_code(dA), gate, up, act, dgate, lddg, dup,
+                                     lddu, qg, qu, qgt, qut, qat, buf, nbytes, _raw_stream(stream))
     if st:
         _check(st, "fqt_fp8_gated_backward")
-    for t, _, _, _ in codes:
-        if t is not None:
-            t.block_rows = 1
+    if qg is not None:
+        qg.block_rows = 1
+    if qu is not None:
+        qu.block_rows = 1
+    if qgt is not None:
+        qgt.block_rows = 1
+    if qut is not None:
+        qut.block_rows = 1
+    if qat is not None:
+        qat.block_rows = 1
     return out
 
 

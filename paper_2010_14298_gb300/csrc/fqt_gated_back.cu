@@ -153,8 +153,8 @@ __global__ void __launch_bounds__(256) k_f8_gated_back_dense(const F8BackArgs a,
 // (they are there when a tile begins) but a tile's steps, one after the other: its 9800 cycles
 // are values 2650, maxima 1500, the columns' scales and two barriers 900, codes 2800, the
 // transposes' way out 2000.  Registers hold 16 warps an SM, which issue at 46% of the rate.
-// A thread with 4 rows x 8 columns spent 23 of 63 instructions an entry on the rows' scales
-// (94 us); spilled registers cost 11 us; rows' codes before the first barrier, or the
+// Rows' scales worked out by every lane took 23 of 63 instructions an entry (94 us), 4 rows x 8
+// columns a thread with shuffles 90 us; spilled registers cost 11 us; rows' codes before the first barrier, or the
 // transposes' way out along with the next tile's values, gained nothing in bf16 and lost 5 us in
 // fp32.  Two CTAs an SM, each with half of a tile's rows and the columns' maxima exchanged in a
 // cluster: 91 us (and as long as before where no columns are asked for, so it is the warps'

@@ -172,6 +172,51 @@ def test_codes_are_those_of_the_dense_output(T, H, K, act):
         assert ((t.dequantize().double() - x).abs() <= half + 1.07 * e).all()
 
 
+@pytest.mark.parametrize("T,H,K", [(7, 200, 100), (7, 200, 3000), (64, 5000, 64), (130, 300, 200),
+                                   (130, 300, 4200), (2100, 1000, 300)])
+def test_any_choice_of_outputs(T, H, K):
+    """Each of the 15 choices among a, its codes, g's and u's gives what all of them together
+    give.  Its tiles may be others and sum in another order, so a sum's last bits may differ, by
+    2^-20 of it or so, and a code where that much decides: one entry in 2^15, and by one step.
+    Two and one in 1000 are allowed."""
+    a, bg, bu = _operands(T, H, K)
+    out, *ref = fqt.fp8_gated_matmul(a, bg, bu, "gelu_tanh", codes=True, keep=True)
+    _, _, want, bound = _expected(a, bg, bu, "gelu_tanh")
+    for choice in range(1, 16):
+        qs = [fqt.Fp8Tensor.empty(T, H) if choice >> i & 1 else None for i in range(3)]
+        wide = torch.full((T + 1, H + 5), 7.0, device="cuda") if choice & 8 else None
+        dense = None if wide is None else wide[:T, :H]
+        got = fqt.fp8_gated_matmul(a, bg, bu, "gelu_tanh", out=dense, q=qs[0], gate=qs[1], up=qs[2],
+                                   dense=False)
+        assert [x is None for x in got] == [not choice & b for b in (8, 1, 2, 4)]
+        if wide is not None:
+            assert ((dense.double() - want).abs() <= bound).all()
+            assert (wide[T:] == 7).all() and (wide[:, H:] == 7).all()
+        for t, r in zip(qs, ref):
+            if t is not None:
+                x, y = t.dequantize(), r.dequantize()
+                assert (x != y).sum() <= 2 + T * H // 1000
+                # (a step is 2^-9 of the scale near zero, and the scale at most a block's
+                # largest entry / 224)
+                step = 2.0 ** -3 * torch.maximum(x.abs(), y.abs()) + 2.0 ** -9 / 224 * y.abs().amax(1, keepdim=True)
+                assert ((x - y).abs() <= step).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,H,K", [(70, 45, 300), (100, 59, 27), (300, 335, 330), (900, 1001, 64),
+                                   (70, 45, 2000), (2100, 1005, 130), (20, 45, 2000)])
+def test_dense_outputs_alone_in_wider_rows(T, H, K, dtype):
+    a, bg, bu = _operands(T, H, K)
+    _, _, want, bound = _expected(a, bg, bu, "silu")
+    if dtype == "bf16":
+        bound = bound + 2.0 ** -8 * (want.abs() + bound)
+    for gap in (1, 3, 8):
+        wide = torch.full((T + 1, H + gap), 7.0, dtype=DTYPES[dtype], device="cuda")
+        fqt.fp8_gated_matmul(a, bg, bu, "silu", out=wide[:T, :H])
+        assert ((wide[:T, :H].double() - want).abs() <= bound).all(), gap
+        assert (wide[T:] == 7).all() and (wide[:, H:] == 7).all(), gap
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,H,K", [(3, 131, 27), (60, 45, 129), (130, 59, 27), (300, 1201, 330),
                                    (2100, 1005, 130)])

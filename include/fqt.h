@@ -435,8 +435,8 @@ typedef enum fqt_act {
  * out (M x N, fp32 or bf16): a, rounded once.  q: a, gate: g, up: u as 8-bit matrices
  * with blocks of 128 entries of a row, each rounded once from fp32; q is the next
  * layer's operand, gate and up are what fqt_fp8_gated_backward reads.  Each output may
- * be NULL, not all; the caller sets the pointers and the pitch of the 8-bit ones, the
- * call their sizes.  Entries of an 8-bit output that are not finite record
+ * be NULL, not all, and overlaps neither another nor an operand; the caller sets the
+ * pointers and the pitch of the 8-bit ones, the call their sizes.  Entries of an 8-bit output that are not finite record
  * FQT_ENONFINITE, take the NaN code and count for no scale.  K = 0: zeros.
  * `dtype` is out's, and with it (or where out is NULL, as for bf16) the number of
  * terms to an accumulator.  Workspace: fqt_fp8_gated_matmul_workspace_size bytes.
@@ -455,7 +455,8 @@ FQT_API fqt_status fqt_fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, con
  * matrices (for the input's gradient); qgate_t, qup_t: their transposes (cols x rows,
  * for the two weights' gradients); product_t: a's transpose (for the gradient of the
  * next layer's weight).  Blocks of 128 entries of a row, entries that are not finite as
- * in fqt_fp8_gated_matmul.  Each output may be NULL, not all.  act'(0) of FQT_RELU is 0.
+ * in fqt_fp8_gated_matmul.  Each output may be NULL, not all, and overlaps neither
+ * another nor dA, gate or up.  act'(0) of FQT_RELU is 0.
  * Workspace: fqt_fp8_gated_backward_workspace_size bytes.
  */
 FQT_API size_t fqt_fp8_gated_backward_workspace_size(int64_t rows, int64_t cols);

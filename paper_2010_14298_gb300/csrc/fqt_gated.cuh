@@ -693,5 +693,13 @@ inline bool all_apart(const fqt_fp8 *const (&q)[N]) {
       if (q[i] && q[j] && (q[i]->codes == q[j]->codes || q[i]->scales == q[j]->scales)) return false;
   return true;
 }
+// And none where an operand is, which other CTAs may still read.
+template <int N, int R>
+inline bool all_apart_from(const fqt_fp8 *const (&q)[N], const fqt_fp8 *const (&read)[R]) {
+  for (const fqt_fp8 *x : q)
+    for (const fqt_fp8 *r : read)
+      if (x && (x->codes == r->codes || x->scales == r->scales)) return false;
+  return true;
+}
 
 }  // namespace fqt

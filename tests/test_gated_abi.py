@@ -64,6 +64,12 @@ def test_forward_refusals():
     assert _gated(q=_f8(10, 20, 7), gate=_f8(10, 20, 7)) == EINVAL
     assert _gated(gate=_f8(10, 20, 7), up=_f8(10, 20, 8, codes=_at(7))) == EINVAL
     assert _gated(gate=_f8(10, 20, 7), up=_f8(10, 20, 8, scales=_at(7) + 2048)) == EINVAL
+    # an output where an operand is
+    for k in range(3):
+        for name in ("q", "gate", "up"):
+            assert _gated(**{name: _f8(10, 20, 7, codes=_at(k))}) == EINVAL, (name, k)
+            assert _gated(**{name: _f8(10, 20, 7, scales=_at(k) + 2048)}) == EINVAL, (name, k)
+        assert _gated(out=_at(k)) == EINVAL
     assert _gated(ws=None) == EWORKSPACE and _gated(nbytes=128) == EWORKSPACE
     assert _gated(ws=_at(6) + 16) == EWORKSPACE
     # nothing to do: the sizes of the outputs are set
@@ -110,6 +116,14 @@ def test_backward_refusals():
         q = [None] * 5
         q[i], q[j] = _f8(0, 0, 7, pitch=64), _f8(0, 0, 7, pitch=64)
         assert _back(q=q) == EINVAL
+    # an output where dA, g or u are
+    assert _back(dgate=_at(0)) == EINVAL and _back(dup=_at(0)) == EINVAL
+    for i in range(5):
+        for k in (1, 2):
+            for place in (dict(codes=_at(k)), dict(scales=_at(k) + 2048)):
+                q = [None] * 5
+                q[i] = _f8(0, 0, 7, pitch=64, **place)
+                assert _back(q=q) == EINVAL, (i, k)
     assert _back(ws=None) == EWORKSPACE and _back(nbytes=16) == EWORKSPACE
     assert _back(ws=_at(12) + 8) == EWORKSPACE
     q = [_f8(9, 9, i) for i in range(5)]

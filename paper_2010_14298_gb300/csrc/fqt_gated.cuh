@@ -60,9 +60,11 @@ __device__ __forceinline__ float cdf_of(float g, float &bell) {
   return g < 0.0f ? q : __fsub_rn(1.0f, q);
 }
 
-// act(g) and act'(g).  1 - sigma is e^-z sigma where it is the slope's factor on its own
-// (e^-z held below 2^126, so that neither loses digits where it is small); silu's slope is
-// s + a (1 - s), which a rounded 1 - s does not harm.
+// act(g) and act'(g).  1 - sigma is e^-z sigma where it is the slope's factor on its own, so
+// that it loses no digits where it is small.  e^-z is held at 2^126 there, and only there:
+// past it sigma is 0, and a value that kept 2^-126 would be g 2^-126 far to the left (-3.5 at
+// g = -3e38).  silu's slope is s + a (1 - s), which a rounded 1 - s does not harm.
+constexpr float kPow126 = 8.507059173023462e37f;
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
   if constexpr (ACT == FQT_RELU) {
@@ -80,8 +82,8 @@ __device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
   } else {
     const float c = ACT == FQT_GELU_TANH ? tanh_arg(g) : g;
     const float z = ACT == FQT_GELU_TANH ? tanh_z(c) : g;
-    const float t = exp2_of(fminf(__fmul_rn(z, -kLog2E), 126.0f));
-    const float s = inverse_of(__fadd_rn(1.0f, t)), r = __fmul_rn(t, s);  // r = 1 - s
+    const float t = exp2_of(__fmul_rn(z, -kLog2E)), s = inverse_of(__fadd_rn(1.0f, t));
+    const float r = __fmul_rn(fminf(t, kPow126), s);  // 1 - s, and 0 where s is 0
     if constexpr (ACT == FQT_SIGMOID) {
       a = s;
       d = __fmul_rn(s, r);
@@ -89,8 +91,8 @@ __device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
       a = __fmul_rn(g, s);
       const float dz = __fmul_rn(kTanhScale, fmaf(__fmul_rn(3.0f * kTanhCube, c), c, 1.0f));
       d = fmaf(__fmul_rn(__fmul_rn(c, r), s), dz, s);
+      if (g != g) d = g;  // the limits take NaN away
     }
-    if (g != g) a = d = g;  // the limits take NaN away
   }
 }
 

@@ -69,7 +69,7 @@ template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
   if constexpr (ACT == FQT_RELU) {
     a = g <= 0.0f ? 0.0f : g;  // NaN stays
-    d = g > 0.0f ? 1.0f : 0.0f;
+    d = g > 0.0f ? 1.0f : a;   // (as here: a checkpoint that is no number shows in dg)
   } else if constexpr (ACT == FQT_GELU) {
     float bell;
     const float cdf = cdf_of(g, bell);

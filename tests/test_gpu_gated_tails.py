@@ -130,3 +130,30 @@ def test_forward_over_the_range(T, H, act):
     tol = (24 + 10 * z) * 2.0 ** -24
     least = 2.0 ** -125 * (1 + g.abs())
     assert ((out.double() - want).abs() <= tol * want.abs() + least).all()
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_checkpoint_that_is_no_number(dtype, act):
+    """A NaN code among g's: dg, du and a are no numbers there, whichever of them is asked
+    for, and it is recorded where they leave as codes."""
+    T, H, i, j = 150, 300, 131, 290
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    g, u, dA = torch.randn((3, T, H), generator=gen, device="cuda")
+    dA = dA.to(DTYPES[dtype])
+    gate, up = fqt.quantize_fp8(g)[0], fqt.quantize_fp8(u)[0]
+    gate.codes[i, j] = 0x7F
+    ws = fqt.Workspace.of_size(256)
+    r = fqt.fp8_gated_backward(dA, gate, up, act, ws=ws, out=fqt.GatedGrads(
+        dgate=torch.empty_like(dA), dup=torch.empty_like(dA)))
+    assert fqt.sync_status(ws) == 0  # as other dense outputs
+    there = torch.zeros((T, H), dtype=torch.bool, device="cuda")
+    there[i, j] = True
+    assert torch.equal(r.dgate.isnan(), there) and torch.equal(r.dup.isnan(), there)
+    for name in ("qgate", "qup", "qgate_t", "qup_t", "product_t"):
+        n, k, at = (T, H, there) if name in ("qgate", "qup") else (H, T, there.t())
+        q = fqt.Fp8Tensor.empty(n, k)
+        fqt.fp8_gated_backward(dA, gate, up, act, out=fqt.GatedGrads(**{name: q}), ws=ws)
+        assert fqt.sync_status(ws) == 4, name
+        assert torch.equal(q.codes[:, :k] & 127 == 127, at), name

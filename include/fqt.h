@@ -412,7 +412,8 @@ FQT_API fqt_status fqt_fp8_matmul(const fqt_fp8 *A, const fqt_fp8 *B, fqt_dtype 
  * out = A1 B1^T + A2 B2^T (M x N) of A1 (M x K1), B1 (N x K1), A2 (M x K2), B2
  * (N x K2): one product whose K blocks are those of both pairs, summed and rounded as
  * fqt_fp8_matmul's.  The gradient of an input that two projections share, for the
- * gradients of their outputs and W^T of each.  Either K may be 0.
+ * gradients of their outputs and W^T of each.  Either K may be 0.  An out that shares a
+ * byte with an operand is refused (FQT_EINVAL).
  */
 FQT_API size_t fqt_fp8_matmul_sum_workspace_size(int64_t M, int64_t N, int64_t K1, int64_t K2);
 FQT_API fqt_status fqt_fp8_matmul_sum(const fqt_fp8 *A1, const fqt_fp8 *B1, const fqt_fp8 *A2,
@@ -435,8 +436,9 @@ typedef enum fqt_act {
  * out (M x N, fp32 or bf16): a, rounded once.  q: a, gate: g, up: u as 8-bit matrices
  * with blocks of 128 entries of a row, each rounded once from fp32; q is the next
  * layer's operand, gate and up are what fqt_fp8_gated_backward reads.  Each output may
- * be NULL, not all, and overlaps neither another nor an operand; the caller sets the
- * pointers and the pitch of the 8-bit ones, the call their sizes.  Entries of an 8-bit output that are not finite record
+ * be NULL, not all, and shares no byte with another or with an operand (FQT_EINVAL; its
+ * rows may lie between another's).  The caller sets the pointers and the pitch of the
+ * 8-bit ones, the call their sizes.  Entries of an 8-bit output that are not finite record
  * FQT_ENONFINITE, take the NaN code and count for no scale.  K = 0: zeros.
  * `dtype` is out's, and with it (or where out is NULL, as for bf16) the number of
  * terms to an accumulator.  Workspace: fqt_fp8_gated_matmul_workspace_size bytes.
@@ -455,8 +457,8 @@ FQT_API fqt_status fqt_fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, con
  * matrices (for the input's gradient); qgate_t, qup_t: their transposes (cols x rows,
  * for the two weights' gradients); product_t: a's transpose (for the gradient of the
  * next layer's weight).  Blocks of 128 entries of a row, entries that are not finite as
- * in fqt_fp8_gated_matmul.  Each output may be NULL, not all, and overlaps neither
- * another nor dA, gate or up.  act'(0) of FQT_RELU is 0.
+ * in fqt_fp8_gated_matmul.  Each output may be NULL, not all, and shares no byte with
+ * another or with dA, gate or up, as there.  act'(0) of FQT_RELU is 0.
  * Workspace: fqt_fp8_gated_backward_workspace_size bytes.
  */
 FQT_API size_t fqt_fp8_gated_backward_workspace_size(int64_t rows, int64_t cols);

@@ -515,8 +515,14 @@ fqt_status fqt_fp8_matmul_sum(const fqt_fp8 *A1, const fqt_fp8 *B1, const fqt_fp
   if (!f8_out_fits(out, ldo, dtype, M, N)) return FQT_EINVAL;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (K1 == 0 && K2 == 0) return f8_no_terms(out, ldo, dtype, M, N, st);
-  for (const fqt_fp8 *q : {A1, B1, A2, B2})
-    if (q->cols > 0 && !f8_good(q)) return FQT_EINVAL;
+  F8Apart apart;
+  apart.writes(out, M, N, dtype == FQT_BF16 ? 2 : 4, ldo);
+  for (const fqt_fp8 *q : {A1, B1, A2, B2}) {
+    if (q->cols == 0) continue;
+    if (!f8_good(q)) return FQT_EINVAL;
+    apart.reads(q);
+  }
+  if (!apart.ok()) return FQT_EINVAL;
   if (!workspace || !f8_aligned(workspace, 256) ||
       ws_bytes < fqt_fp8_matmul_sum_workspace_size(M, N, K1, K2))
     return FQT_EWORKSPACE;

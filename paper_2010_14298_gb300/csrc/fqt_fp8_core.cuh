@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "fqt.h"
 #include "fqt_common.cuh"
@@ -1096,5 +1097,65 @@ static bool f8_good(const fqt_fp8 *q) {
   return q->codes && q->scales && f8_aligned(q->codes, 16) && f8_aligned(q->scales, 16) &&
          q->pitch % 16 == 0 && q->pitch >= q->cols && q->pitch < ((int64_t)1 << 40);
 }
+
+// Where a matrix lies: `rows` of `row` bytes, `pitch` bytes apart.
+struct F8Place {
+  uint64_t at;
+  int64_t rows, row, pitch;
+};
+
+// Whether two matrices share a byte.  (Rows may lie between another's: halves of one buffer.)
+inline bool f8_meet(F8Place a, F8Place b) {
+  if (b.at < a.at) std::swap(a, b);
+  const uint64_t d = b.at - a.at;
+  if (d >= (uint64_t)(a.rows - 1) * a.pitch + a.row) return false;
+  if (a.rows == 1) return true;
+  if (b.rows > 1 && b.pitch != a.pitch) {
+    for (int64_t i = 0; i < b.rows; ++i)
+      if (f8_meet(a, F8Place{b.at + (uint64_t)i * b.pitch, 1, b.row, b.row})) return true;
+    return false;
+  }
+  // b begins r bytes after the beginning of a's row q, and its other rows do so after later ones
+  const int64_t q = d / a.pitch, r = d % a.pitch;
+  return r < a.row || (r + b.row > a.pitch && q + 1 < a.rows);
+}
+
+// The matrices that a call writes and those that it reads: CTAs read while others write, so no
+// two may share a byte but two that are read.
+class F8Apart {
+ public:
+  void writes(const void *p, int64_t rows, int64_t cols, size_t es, int64_t ld) {
+    if (p && rows > 0 && cols > 0) w_[nw_++] = place(p, rows, cols, es, ld);
+  }
+  void reads(const void *p, int64_t rows, int64_t cols, size_t es, int64_t ld) {
+    if (p && rows > 0 && cols > 0) r_[nr_++] = place(p, rows, cols, es, ld);
+  }
+  // an output of rows x cols codes (its own sizes are not set yet), in whole 16 bytes
+  void writes(const fqt_fp8 *q, int64_t rows, int64_t cols) {
+    if (!q) return;
+    writes(q->codes, rows, (cols + 15) / 16 * 16, 1, q->pitch);
+    writes(q->scales, 1, (cols + 511) / 512 * scale_rows(rows) * 4, 1, 0);
+  }
+  void reads(const fqt_fp8 *q) {
+    reads(q->codes, q->rows, q->cols, 1, q->pitch);
+    reads(q->scales, 1, (q->cols + 511) / 512 * scale_rows(q->rows) * 4, 1, 0);
+  }
+  bool ok() const {
+    for (int i = 0; i < nw_; ++i) {
+      for (int j = i + 1; j < nw_; ++j)
+        if (f8_meet(w_[i], w_[j])) return false;
+      for (int j = 0; j < nr_; ++j)
+        if (f8_meet(w_[i], r_[j])) return false;
+    }
+    return true;
+  }
+
+ private:
+  static F8Place place(const void *p, int64_t rows, int64_t cols, size_t es, int64_t ld) {
+    return F8Place{reinterpret_cast<uintptr_t>(p), rows, cols * (int64_t)es, ld * (int64_t)es};
+  }
+  F8Place w_[12], r_[8];  // (two dense outputs and five of codes; four operands)
+  int nw_ = 0, nr_ = 0;
+};
 
 }  // namespace fqt

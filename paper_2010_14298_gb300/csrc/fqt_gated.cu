@@ -167,12 +167,15 @@ fqt_status fqt_fp8_gated_matmul(const fqt_fp8 *A, const fqt_fp8 *Bg, const fqt_f
     if (out && (!f8_aligned(out, es) || (M > 1 && (ldo < N || ldo > ((int64_t)1 << 40)))))
       return FQT_EINVAL;
     if (!codes_fit(q, M, N) || !codes_fit(gate, M, N) || !codes_fit(up, M, N)) return FQT_EINVAL;
-    if (!all_apart({q, gate, up})) return FQT_EINVAL;
-    if (K > 0) {
-      for (const fqt_fp8 *x : {A, Bg, Bu})
-        if (!f8_good(x) || (out && out == x->codes)) return FQT_EINVAL;
-      if (!all_apart_from({q, gate, up}, {A, Bg, Bu})) return FQT_EINVAL;
-    }
+    F8Apart apart;
+    apart.writes(out, M, N, es, ldo);
+    for (const fqt_fp8 *x : {q, gate, up}) apart.writes(x, M, N);
+    if (K > 0)
+      for (const fqt_fp8 *x : {A, Bg, Bu}) {
+        if (!f8_good(x)) return FQT_EINVAL;
+        apart.reads(x);
+      }
+    if (!apart.ok()) return FQT_EINVAL;
     if (!workspace || !f8_aligned(workspace, 256) ||
         ws_bytes < fqt_fp8_gated_matmul_workspace_size(M, N, K))
       return FQT_EWORKSPACE;

@@ -687,21 +687,4 @@ inline void set_codes(fqt_fp8 *q, int64_t rows, int64_t cols) {
   q->block_rows = 1;
 }
 
-// No two outputs in the same place.
-template <int N>
-inline bool all_apart(const fqt_fp8 *const (&q)[N]) {
-  for (int i = 0; i < N; ++i)
-    for (int j = i + 1; j < N; ++j)
-      if (q[i] && q[j] && (q[i]->codes == q[j]->codes || q[i]->scales == q[j]->scales)) return false;
-  return true;
-}
-// And none where an operand is, which other CTAs may still read.
-template <int N, int R>
-inline bool all_apart_from(const fqt_fp8 *const (&q)[N], const fqt_fp8 *const (&read)[R]) {
-  for (const fqt_fp8 *x : q)
-    for (const fqt_fp8 *r : read)
-      if (x && (x->codes == r->codes || x->scales == r->scales)) return false;
-  return true;
-}
-
 }  // namespace fqt

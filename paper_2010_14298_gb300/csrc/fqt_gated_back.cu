@@ -579,12 +579,18 @@ fqt_status fqt_fp8_gated_backward(const void *dA, int64_t ldda, fqt_dtype dtype,
       return FQT_EINVAL;
     if (dup && (!f8_aligned(dup, es) || (rows > 1 && (lddu < cols || lddu > most))))
       return FQT_EINVAL;
-    if ((dgate && dgate == dup) || dgate == dA || dup == dA) return FQT_EINVAL;
     if (!codes_fit(qgate, rows, cols) || !codes_fit(qup, rows, cols) ||
         !codes_fit(qgate_t, cols, rows) || !codes_fit(qup_t, cols, rows) ||
-        !codes_fit(product_t, cols, rows) || !all_apart({qgate, qup, qgate_t, qup_t, product_t}) ||
-        !all_apart_from({qgate, qup, qgate_t, qup_t, product_t}, {gate, up}))
+        !codes_fit(product_t, cols, rows))
       return FQT_EINVAL;
+    F8Apart apart;
+    apart.writes(dgate, rows, cols, es, lddg);
+    apart.writes(dup, rows, cols, es, lddu);
+    for (const fqt_fp8 *x : {qgate, qup}) apart.writes(x, rows, cols);
+    for (const fqt_fp8 *x : {qgate_t, qup_t, product_t}) apart.writes(x, cols, rows);
+    apart.reads(dA, rows, cols, es, ldda);
+    for (const fqt_fp8 *x : {gate, up}) apart.reads(x);
+    if (!apart.ok()) return FQT_EINVAL;
     if (!workspace || !f8_aligned(workspace, 256) ||
         ws_bytes < fqt_fp8_gated_backward_workspace_size(rows, cols))
       return FQT_EWORKSPACE;

@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "fqt.h"
@@ -390,20 +391,25 @@ struct F8Item {
   int kb0, kb1;
 };
 
-template <int NT, bool PAIR>
+// I: what a place is worked out in.  32 bits hold it (at most 2^31 tiles, and 2^15 parts of
+// few).  Where pairs add up two products' sums in registers, 60 bytes of those were spilled
+// for it, and 64 bits take less time: 8192 x 1024 with K 4096 twice in fp32 57.3 us and 57.8,
+// 4096 x 4096 107.8 and 108.7.  One product's pairs spill 56 bytes for it, but lose no time:
+// 4096 x 1024 x 8192 in fp32 31.7 us either way, 8192 x 4096 x 4096 102.6, and 103.2 in 64 bits
+// with none; its single CTAs 1024 x 1024 x 65536 70 us, and 79.
+template <int NT, bool PAIR, typename I>
 __device__ __forceinline__ F8Item f8_item(const F8Args &g, int64_t it) {
   F8Item t;
-  // (in 32 bits: at most 2^31 tiles, and 2^15 parts of few)
-  const uint32_t i = (uint32_t)it, r = PAIR ? i : i / (uint32_t)g.splits;
+  const I i = (I)it, r = PAIR ? i : i / (I)g.splits;
   // bands of kF8Band row tiles, so that the tiles in flight share rows of both operands
-  const uint32_t band = r / ((uint32_t)kF8Band * (uint32_t)g.n_tiles);
-  const uint32_t in = r - band * kF8Band * (uint32_t)g.n_tiles;
-  const uint32_t high = min((uint32_t)kF8Band, (uint32_t)g.m_tiles - band * kF8Band);
-  const uint32_t n = in / high;
+  const I band = r / ((I)kF8Band * (I)g.n_tiles);
+  const I in = r - band * kF8Band * (I)g.n_tiles;
+  const I high = min((I)kF8Band, (I)g.m_tiles - band * kF8Band);
+  const I n = in / high;
   t.n0 = (int64_t)n * NT;
   t.m0 = (int64_t)(band * kF8Band + in - n * high) * (PAIR ? 2 * BM : BM) +
          (PAIR ? (blockIdx.x & 1) * BM : 0);
-  t.kb0 = PAIR ? 0 : (int)(i - r * (uint32_t)g.splits) * g.kb_per;
+  t.kb0 = PAIR ? 0 : (int)(i - r * (I)g.splits) * g.kb_per;
   t.kb1 = min(g.nkb, t.kb0 + g.kb_per);
   return t;
 }
@@ -417,7 +423,8 @@ __device__ __forceinline__ F8Item f8_item_of(const A &g, int64_t it) {
     return F8Item{(int64_t)(cluster * g.holds + r - k * g.holds) * g.part, 0, kb0,
                   min(g.nkb, kb0 + g.kb_per)};
   } else {
-    return f8_item<NT, PAIR>(g, it);
+    constexpr bool wide = PAIR && KIND == F8_SUM;
+    return f8_item<NT, PAIR, std::conditional_t<wide, int64_t, uint32_t>>(g, it);
   }
 }
 
@@ -530,7 +537,7 @@ __device__ __forceinline__ void f8_store_box(const F8Args &g, const CUtensorMap 
 // rows of NT + 4 entries or (swapped) columns of 128, and each CTA adds up its share.
 template <int NT>
 __device__ __forceinline__ void f8_join(const F8Args &g, int64_t it, const float *part) {
-  const F8Item t = f8_item<NT, false>(g, it);
+  const F8Item t = f8_item<NT, false, uint32_t>(g, it);
   const int parts = g.splits, self = (int)(it % parts);
   const int run = g.swap ? BM : NT, pitch = g.swap ? BM : NT + 4;  // of outputs in a row
   // rows and entries of a row that the output has

@@ -395,7 +395,7 @@ __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
   constexpr int CW = NT / 4;
   uint32_t c = 0;
   for (int64_t it = first; it < g.items && !*abort_flag; it += step) {
-    const F8Item t = f8_item<NT, PAIR>(g, it);
+    const F8Item t = f8_item<NT, PAIR, uint32_t>(g, it);
     uint32_t v[CW], w[CW];  // g (then a) and u
     if (!f8_gated_sums<NT, CW, ACCS, PAIR, FOLD>(
             g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * CW), accf, acce, abort_flag,
@@ -457,7 +457,7 @@ __device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
     q_col = -1;
   };
   for (int64_t it = first; it < g.items; it += step, parity ^= 1u) {
-    const F8Item t = f8_item<256, PAIR>(g, it);
+    const F8Item t = f8_item<256, PAIR, uint32_t>(g, it);
     uint32_t v[32], w[32];  // g (then a) and u
     const bool ok = f8_gated_sums<256, 32, ACCS, PAIR, true>(
         g, t, tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(h * 32), accf, acce, abort_flag, lane,
@@ -613,7 +613,7 @@ __device__ __forceinline__ void f8_gated_join(const F8GatedArgs &g, const float 
     cta = at / g.part;
     at %= g.part;
   } else {
-    const F8Item t = f8_item<256, false>(g, blockIdx.x);
+    const F8Item t = f8_item<256, false, uint32_t>(g, blockIdx.x);
     t0 = t.m0;
     j = t.n0 / 2;
     tokens = min((int64_t)BM, g.M - t0);

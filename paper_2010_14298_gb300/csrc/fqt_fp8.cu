@@ -63,15 +63,14 @@ __global__ void __launch_bounds__(256) k_f8_rows(const F8QuantArgs a, const bool
     for (int r = 0; r < R; ++r) m[r] = max(m[r], __shfl_xor_sync(0xffffffffu, m[r], o));
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int e = f8_exponent(m[r]);
+    float inv;
     // the four blocks' bytes, from lanes 0, 8, 16 and 24
-    uint32_t w = (uint32_t)(e + 127) << (lane >> 3) * 8;
+    uint32_t w = f8_scale(m[r], inv) << (lane >> 3) * 8;
     w |= __shfl_xor_sync(0xffffffffu, w, 8);
     w |= __shfl_xor_sync(0xffffffffu, w, 16);
     if (row + r >= a.rows) continue;
     if (lane == 0) reinterpret_cast<uint32_t *>(a.s)[blockIdx.y * a.sp + row + r] = w;
     if (col >= a.cols) continue;
-    const float inv = pow2(-e);
     uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) c[i] = v[r].pair(2 * i, inv) | v[r].pair(2 * i + 1, inv) << 16;
@@ -176,7 +175,8 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
 #pragma unroll
     for (int i = 0; i < 4; ++i) rm[i] = max(rm[i], __shfl_xor_sync(0xffffffffu, rm[i], o));
   __syncthreads();
-  int e_col = 0;
+  uint32_t e_col = 0;
+  float inv_col;
   if (t < kF8Block) {
     uint32_t m = 0u;
 #pragma unroll
@@ -185,8 +185,7 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
       m = __reduce_max_sync(0xffffffffu, m);
       if (lane == 0) wmax[warp] = m;
     } else {
-      e_col = f8_exponent(m);
-      cinv[t] = pow2(-e_col);
+      e_col = f8_scale(m, cinv[t]);
     }
   }
   __syncthreads();
@@ -194,16 +193,16 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
     const uint32_t m = max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3]));
 #pragma unroll
     for (int i = 0; i < 4; ++i) rm[i] = m;
-    e_col = f8_exponent(m);
+    e_col = f8_scale(m, inv_col);
   }
-  if (a.ct && t < kF8Block) a.st[scale_at(blockIdx.x, a.spt, c0 + t)] = (uint8_t)(e_col + 127);
+  if (a.ct && t < kF8Block) a.st[scale_at(blockIdx.x, a.spt, c0 + t)] = (uint8_t)e_col;
   if (a.c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int e = f8_exponent(rm[i]);
-      if (cg == 0) a.s[scale_at(blockIdx.y, a.sp, row + i)] = (uint8_t)(e + 127);
+      float inv;
+      const uint32_t e = f8_scale(rm[i], inv);
+      if (cg == 0) a.s[scale_at(blockIdx.y, a.sp, row + i)] = (uint8_t)e;
       if (row + i >= a.rows || col >= a.cols) continue;
-      const float inv = pow2(-e);
       *reinterpret_cast<uint2 *>(a.c + (row + i) * a.pitch + col) =
           make_uint2(v[i].pair(0, inv) | v[i].pair(1, inv) << 16,
                      v[i].pair(2, inv) | v[i].pair(3, inv) << 16);
@@ -213,7 +212,7 @@ __global__ void __launch_bounds__(kF8TileThreads, sizeof(T) == 4 ? 2 : 3)
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
       float2 inv = *reinterpret_cast<const float2 *>(&cinv[cg * 8 + j]);
-      if (a.whole) inv.x = inv.y = pow2(-e_col);
+      if (a.whole) inv.x = inv.y = inv_col;
       uint32_t c[2];
       if constexpr (sizeof(T) == 4) {
 #pragma unroll

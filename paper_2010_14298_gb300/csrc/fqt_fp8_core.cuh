@@ -25,25 +25,20 @@ constexpr int64_t kF8MaxSize = 1 << 22;  // of any dimension (32768 blocks: a gr
 // A block's scale 2^e: the least power of two for which amax <= 448 2^e (448 =
 // 1.75 2^8, E4M3's largest value), e in [-127, 127]; e = 0 for a block of zeros.
 // Division by it is exact, so a code is one rounding of the entry (to nearest, ties
-// to even) in any arithmetic, and the value code 2^e is exact in fp32.  amax as
-// fp32 bits; returns e.
-__device__ __forceinline__ int f8_exponent(uint32_t amax) {
-  if (amax == 0u) return 0;
-  const int e = (int)(amax >> 23) - 127 - 8 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-  return max(e, -127);  // subnormal amax too
-}
-// 2^e, -127 <= e <= 127
-__device__ __forceinline__ float pow2(int e) {
-  return __uint_as_float(e > -127 ? (uint32_t)(e + 127) << 23 : 1u << 22);
-}
-
-// The same scale as its byte, and 2^-e: 2^e (the least with amax <= 1.75 2^(e + 8)) has amax's
-// exponent less 8, and one more where amax's significand passes 1.75, which a carry finds.
+// to even) in any arithmetic, and the value code 2^e is exact in fp32 (but for entries
+// of 1.9375 2^127 and more, which round to 2^128: infinite there).
+//
+// amax as fp32 bits; returns e + 127, and 2^-e.  e is amax's exponent less 8, and one more
+// where amax's significand passes 1.75, which a carry finds.
 __device__ __forceinline__ uint32_t f8_scale(uint32_t amax, float &inv) {
   uint32_t field = (uint32_t)min(262 - (int)((amax + 0x1FFFFFu) >> 23), 254);  // of 2^-e
   if (amax == 0u) field = 127u;
   inv = __uint_as_float(field << 23);
   return 254u - field;
+}
+// 2^e, -127 <= e <= 127
+__device__ __forceinline__ float pow2(int e) {
+  return __uint_as_float(e > -127 ? (uint32_t)(e + 127) << 23 : 1u << 22);
 }
 
 // Codes of two values (lo, hi in the low and high byte), |.| <= 448 or NaN.

@@ -217,12 +217,6 @@ __device__ __forceinline__ float top3(float a, float b, float c) {
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// The same of the numbers among them.
-__device__ __forceinline__ float top3_number(float a, float b, float c) {
-  float r;
-  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 __device__ __forceinline__ bool is_odd(float top) {
   return (__float_as_uint(top) & 0x7FFFFFFFu) >= 0x7F800000u;
 }

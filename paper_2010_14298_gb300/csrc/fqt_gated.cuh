@@ -11,9 +11,11 @@ namespace fqt {
 // ---------------------------------------------------------------------------
 // Activations
 // ---------------------------------------------------------------------------
-// sigma(z) = 1 / (1 + 2^(-z log2 e)) by the hardware's base-2 exponential and reciprocal:
-// the exponential's argument is rounded (relative error |z| 2^-24 of the result), they
-// themselves are 2 units off; tanh.approx would leave 5e-4.
+// sigma(z) = 1 / (1 + 2^(-z log2 e)) by the hardware's base-2 exponential and reciprocal, for
+// fp32 outputs too: the epilogue that waits for them bounds the kernel with codes.  They
+// themselves are 2 units off, and the exponential's argument is rounded, which counts where
+// sigma is small (measured: 2e-7 of sigma at z > -2, 9e-7 at -20, 3.6e-6 at -87).  Below
+// 2^-126 (z < -87.3) sigma is 0.  tanh.approx would leave 5e-4.
 constexpr float kLog2E = 1.4426950408889634f;
 __device__ __forceinline__ float exp2_of(float x) {
   float r;
@@ -39,9 +41,11 @@ __device__ __forceinline__ float tanh_z(float c) {
 
 // gelu's Phi(-x) e^(x^2/2), x >= 0, is t P(t) with t = 1 / (1 + 0.35 x): P, of degree 8, is the
 // polynomial whose largest relative error over 0 <= x <= 14 is least (3.2e-8, 3e-7 in fp32
-// arithmetic; found by reweighted least squares).  Unlike an approximation of erf, it loses no
-// digits in the tail, and its factor e^(-x^2/2) is the density that the slope needs.  (With
-// CUDA's normcdff 8192 x 4096 x 1024 took 139 us.)
+// arithmetic; found by reweighted least squares).  Unlike an approximation of erf, it is as good
+// in the tail, and its factor e^(-x^2/2) is the density that the slope needs.  That factor's
+// argument is rounded like sigma's: gelu is off by 4e-7 of itself for |g| < 2, 1.3e-6 at -6,
+// 3.6e-6 at -12 (0.5 erfc(-g / sqrt 2) in fp32 by 3e-7, 1.6e-6 and 1e-5).  (With CUDA's
+// normcdff 8192 x 4096 x 1024 took 139 us.)
 constexpr float kCdfScale = 0.35f;
 constexpr int kCdfTerms = 9;
 __device__ constexpr float kCdf[kCdfTerms] = {
@@ -63,7 +67,8 @@ __device__ __forceinline__ float cdf_of(float g, float &bell) {
 // act(g) and act'(g).  1 - sigma is e^-z sigma where it is the slope's factor on its own, so
 // that it loses no digits where it is small.  e^-z is held at 2^126 there, and only there:
 // past it sigma is 0, and a value that kept 2^-126 would be g 2^-126 far to the left (-3.5 at
-// g = -3e38).  silu's slope is s + a (1 - s), which a rounded 1 - s does not harm.
+// g = -3e38).  silu's slope is s + a (1 - s): there 1 - s is a difference, which is off by
+// 2^-24 where the slope is next to 1.
 constexpr float kPow126 = 8.507059173023462e37f;
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float &a, float &d) {
@@ -419,14 +424,14 @@ __device__ __forceinline__ void f8_gated_dense(const F8Of<F8_GATED>::Maps &maps,
 // in the next round.  Whatever makes one of the warps stop, all four leave the loop at the same
 // barrier.  DENSE: a leaves densely as well.
 //
-// 8192 x 4096 x 1024: a's codes 50 us, those of a, g and u 59 (2.3 PFLOP/s), 67 with gelu,
-// where a dense output takes 47.  An item's products take 5000 cycles; this epilogue, next to
-// them, 7000: 16 warps issue at 44% of the rate, waiting for their own arithmetic, the shared
-// memory and one another.  Registers decide (96 a thread): with eight
-// warps and twice the columns 78 us; sums taken all at once instead of 16 columns at a time 72,
-// with spilled registers; kernels without a dense output are without its code.  Maxima taken
-// along with the sums, or 8 columns at a time while the next are on their way: 62; half of the
-// reciprocals by Newton's iteration: no difference.
+// 8192 x 4096 x 1024: a's codes 50 us, those of a, g and u 59 (2.3 PFLOP/s), 67 with gelu, 62
+// with gelu_tanh, where a dense output takes 47.  An item's products take 5000 cycles; this
+// epilogue, next to them, 7000: 16 warps issue at 43% of the rate, waiting for their own
+// arithmetic, the shared memory and one another.  Registers decide (96 a thread, 20 to 40 bytes
+// of others spilled): with eight warps and twice the columns 78 us; sums taken all at once
+// instead of 16 columns at a time 72, with more spilled; kernels without a dense output are
+// without its code.  Maxima taken along with the sums, or 8 columns at a time while the next are
+// on their way: 62; half of the reciprocals by Newton's iteration: no difference.
 template <int ACCS, bool PAIR, bool DENSE>
 __device__ __forceinline__ void f8_gated_codes(const F8Of<F8_GATED>::Maps &maps,
                                                const F8GatedArgs &g, uint32_t tmem, uint64_t *accf,

@@ -45,8 +45,10 @@ __device__ __forceinline__ void back_two(f32x2 da, f32x2 g, f32x2 u, float sg, f
 // 2^shift lanes take 8 neighbouring columns each of a row, a thread 4 rows (on their way at
 // once).  Rows of da or of an output that lie on no 16 bytes (WIDE false) go by way of shared
 // memory: entry by entry, but neighbouring lanes' are neighbours.  Bound by memory traffic:
-// 8192 x 4096 in bf16 43 us, 6.2 TB/s, in fp32 77, 6.1 TB/s; 8192 x 4095, which lies on no 16
-// bytes, 61 and 92 (each lane its own 8 entries 187).
+// 8192 x 4096 in bf16 43 us, 6.2 TB/s, in fp32 77, 6.1 TB/s.  8192 x 4095, which lies on no 16
+// bytes, 61 and 92 (each lane its own 8 entries 187): every entry of da, dg and du is an access
+// of its own, of 2 bytes in bf16, 38 instructions an entry for 25; the issue slots and the shared
+// memory's wavefronts are at 54% each, memory at 47%.
 constexpr int kBackRows = 4;
 
 template <typename T, int ACT, bool WIDE>
@@ -153,10 +155,11 @@ __global__ void __launch_bounds__(256) k_f8_gated_back_dense(const F8BackArgs a,
 // (they are there when a tile begins) but a tile's steps, one after the other: its 9800 cycles
 // are values 2650, maxima 1500, the columns' scales and two barriers 900, codes 2800, the
 // transposes' way out 2000.  Registers hold 16 warps an SM, which issue at 46% of the rate.
+// (gelu_tanh 83 us, relu 66.)
 // Rows' scales worked out by every lane took 23 of 63 instructions an entry (94 us), 4 rows x 8
-// columns a thread with shuffles 90 us; spilled registers cost 11 us; rows' codes before the first barrier, or the
-// transposes' way out along with the next tile's values, gained nothing in bf16 and lost 5 us in
-// fp32.  Two CTAs an SM, each with half of a tile's rows and the columns' maxima exchanged in a
+// columns a thread with shuffles 90 us; spilled registers cost 11 us (39 instructions an entry
+// now); rows' codes before the first barrier, or the transposes' way out along with the next
+// tile's values, gained nothing in bf16 and lost 5 us in fp32.  Two CTAs an SM, each with half of a tile's rows and the columns' maxima exchanged in a
 // cluster: 91 us (and as long as before where no columns are asked for, so it is the warps'
 // own instructions that wait, four warps to a scheduler).
 constexpr int kF8BackThreads = 512, kF8BackWarps = kF8BackThreads / 32;
